@@ -533,6 +533,133 @@ psc_status psc_compute_and_argmax_dense(const psc_handle *h, const int32_t *stac
                                         const void *logits, psc_dtype dtype, int32_t V, int32_t *out_tokens,
                                         void *stream);
 
+/*
+ * Operators around a step's logits: the output projection that makes them
+ * (psc_quantize_rows, psc_head_logits), what a request changes in them
+ * (psc_penalize, psc_append_tokens), and the token that is drawn from them
+ * (psc_sample).  They need no handle.  Rows are `stride` elements apart
+ * (>= V), their elements adjacent and at their own alignment; `bitmask` is
+ * uint32 [B][ceil(V/32)] as psc_compute_masks writes it, or NULL for no mask.
+ * Device pointers, asynchronous on `stream`, on the current device; nothing
+ * is allocated: a workspace is the caller's, not shared by calls that overlap
+ * in time, and holds nothing from one call to the next.
+ */
+
+/*
+ * Rows of float32 or bfloat16 in 8 bits with one scale each:
+ *   scales[r] = max_d |x[r][d]| / 127,  q[r][d] = rint(x[r][d] / scales[r])
+ * (both quotients float32, ties to even), so that x is about scales * q.  A
+ * row of zeros has scale 0; a row with an infinity or NaN has scale NaN and
+ * zeros, so that every product with it is NaN.  Rows of x are x_stride
+ * elements apart; rows of q are q_stride bytes apart, a multiple of 16 and
+ * >= D, start at 16-byte addresses, and their bytes from D up to the next
+ * multiple of 16 become zeros.  For the weights of psc_head_logits (once, a
+ * row per token) and other operands of the kind.  n_rows == 0 is a no-op.
+ * Errors: PSC_E_INVALID_ARG, PSC_E_DEVICE.
+ */
+psc_status psc_quantize_rows(const void *x, psc_dtype dtype, int64_t x_stride, int64_t n_rows, int32_t D,
+                             int8_t *q, int64_t q_stride, float *scales, void *stream);
+
+/*
+ * Hidden states to logits, in 8-bit integers:
+ *   logits[b][v] = s_b * w_scales[v] * sum_d q[b][d] * w[v][d] + bias[v]
+ * where (q, s) are the rows of x quantised as by psc_quantize_rows; -inf where
+ * `bitmask` forbids v.  The sum is exact (32-bit integers); scales and bias are
+ * float32, and the result is rounded once, to `dtype`.
+ *  x          [B] rows of D elements, float32 or bfloat16, x_stride apart.
+ *  w          int8 [V] rows of D, w_stride bytes apart (a multiple of 16,
+ *             >= D, at most 4,194,303), starting at 16-byte addresses; what
+ *             lies between D and w_stride does not matter.
+ *  w_scales   float32 [V];  bias  float32 [V] or NULL.
+ *  workspace  psc_head_workspace(B, D, V) bytes, 16-byte aligned.
+ * 1 <= D <= 131,072 (up to there no sum can overflow).  B == 0 or V == 0 is a
+ * no-op.  Errors: PSC_E_INVALID_ARG, PSC_E_DEVICE.
+ */
+size_t psc_head_workspace(int32_t B, int32_t D, int32_t V);
+psc_status psc_head_logits(const void *x, psc_dtype x_dtype, int64_t x_stride, int32_t B, int32_t D,
+                           const int8_t *w, int64_t w_stride, const float *w_scales, int32_t V,
+                           const float *bias, const uint32_t *bitmask, void *logits, psc_dtype dtype,
+                           int64_t stride, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * What the requests of a batch change in their logits.  Row b's history is
+ * history[b][0 .. lens[b]) (lengths outside [0, cap] are clamped), of which
+ * the first prompt_lens[b] tokens are the prompt; tokens outside [0, V) are
+ * ignored.  A NULL pointer stands for what is in brackets.
+ */
+typedef struct {
+    const int32_t *history;     /* [B][cap]; needed, with lens, where cap > 0          */
+    const int32_t *lens;        /* [B]                                                 */
+    const int32_t *prompt_lens; /* [B]                                             [0] */
+    int32_t cap;                /* <= 2^30                                             */
+    int32_t n_bias;             /* entries a row, <= 1,024                             */
+    const float *repetition;    /* [B], > 0                                        [1] */
+    const float *presence;      /* [B]                                             [0] */
+    const float *frequency;     /* [B]                                             [0] */
+    const int32_t *bias_ids;    /* [B][n_bias]; an id outside [0, V) is no entry, and of
+                                   a token's entries the last one counts               */
+    const float *bias_values;   /* [B][n_bias], finite                                 */
+} psc_penalties;
+
+/*
+ * In place on logits [B][V], for every token v of row b:
+ *   v in the history:                   x = x > 0 ? x / repetition : x * repetition
+ *   n > 0 times in it after the prompt: x = x - n * frequency - presence
+ *   v among the biases:                 x = x + value
+ *   forbidden by `bitmask`:             x = -inf
+ * in float32, rounded once to `dtype`.  A logit that is -inf stays so; logits
+ * of which none of this is true are neither read nor written.  `penalties`
+ * may be NULL.  B == 0 or V == 0 is a no-op.  Errors: PSC_E_INVALID_ARG,
+ * PSC_E_DEVICE.
+ */
+psc_status psc_penalize(void *logits, psc_dtype dtype, int64_t stride, int32_t B, int32_t V,
+                        const psc_penalties *penalties, const uint32_t *bitmask, void *stream);
+
+/*
+ * Appends tokens[b] to row b's history and adds 1 to lens[b].  status[b]
+ * (may be NULL): PSC_ADV_OK; PSC_ADV_SKIPPED, tokens[b] < 0; PSC_ADV_OVERFLOW,
+ * the row is full; PSC_ADV_BAD_INPUT, lens[b] < 0; a row that is not
+ * PSC_ADV_OK stays as it is.  Errors: PSC_E_INVALID_ARG, PSC_E_DEVICE.
+ */
+psc_status psc_append_tokens(int32_t *history, int32_t cap, int32_t *lens, int32_t B, const int32_t *tokens,
+                             int32_t *status, void *stream);
+
+/* How each row draws its token ([B] each; a NULL pointer stands for what is in brackets). */
+typedef struct {
+    const float *temperature; /* not > 0: the best token                             [1] */
+    const int32_t *top_k;     /* <= 0 or > k: k                                      [k] */
+    const float *top_p;       /* >= 1: no cut                                        [1] */
+    const float *min_p;       /*                                                     [0] */
+    const float *noise;       /* [B][k], samples of the unit exponential distribution
+                                 (> 0)                                  [the best token] */
+} psc_sampling;
+
+/*
+ * Log-probabilities and a drawn token of every row, over its allowed tokens
+ * with a logit above -inf, at the row's temperature T (at 1 where T is not > 0):
+ *   p(v) = exp(x[v] / T) / sum_u exp(x[u] / T)
+ *  ids          int32 [B][k], the k tokens with the largest logits, best
+ *               first, ties to the lower id; -1 where there are fewer.
+ *  id_logprobs  float32 [B][k], log p of each; -inf where the id is -1.
+ *  tokens       int32 [B], one of them: of the first top_k, those whose
+ *               predecessors' share of these top_k tokens' probability is below
+ *               top_p (the best one always) and whose p is at least min_p times
+ *               the best one's; of them the one with the largest p / noise, which
+ *               draws each with its share of the probability.  -1 in a row
+ *               without tokens.
+ *  logprobs     float32 [B], log p of tokens[b].
+ * ids, id_logprobs and logprobs may be NULL.  A NaN counts above every number,
+ * as in psc_compute_and_argmax; in a row whose best logit is NaN or +inf the
+ * log-probabilities are NaN and the best token is taken.  1 <= k <= 64, B <=
+ * 65,535, rows of at most 2 MiB; workspace: psc_sample_workspace bytes,
+ * 16-byte aligned.  B == 0 is a no-op.  Errors: PSC_E_INVALID_ARG, PSC_E_DEVICE.
+ */
+size_t psc_sample_workspace(int32_t B, int32_t V, psc_dtype dtype);
+psc_status psc_sample(const void *logits, psc_dtype dtype, int64_t stride, int32_t B, int32_t V,
+                      const uint32_t *bitmask, const psc_sampling *sampling, int32_t k, int32_t *tokens,
+                      float *logprobs, int32_t *ids, float *id_logprobs, void *workspace,
+                      size_t workspace_bytes, void *stream);
+
 /* Read (synchronously, on `stream`) and optionally reset the device counter
  * of sequences that psc_compute_masks rejected as out of range. */
 psc_status psc_device_error_count(const psc_handle *h, uint32_t *out, int32_t reset, void *stream);

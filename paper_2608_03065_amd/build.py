@@ -20,6 +20,7 @@ HIP_FLAGS = [
     # never let the compiler form packed-fp32 instructions
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]
+DEVICE_SOURCES = ["psc_device", "psc_head", "psc_penalize", "psc_sample"]
 HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function"]
 
 
@@ -33,15 +34,16 @@ def _run(cmd):
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD_DIR, exist_ok=True)
     host_obj = os.path.join(BUILD_DIR, "psc_build.o")
-    dev_obj = os.path.join(BUILD_DIR, "psc_device.o")
+    dev_objs = [os.path.join(BUILD_DIR, name + ".o") for name in DEVICE_SOURCES]
     store_obj = os.path.join(BUILD_DIR, "psc_store.o")
     gram_obj = os.path.join(BUILD_DIR, "psc_grammar.o")
     _run(["g++", *HOST_FLAGS, f"-I{ROCM}/include", "-c", os.path.join(CSRC, "psc_build.cpp"), "-o", host_obj])
     _run(["g++", *HOST_FLAGS, f"-I{ROCM}/include", "-c", os.path.join(CSRC, "psc_store.cpp"), "-o", store_obj])
     _run(["g++", *HOST_FLAGS, f"-I{ROCM}/include", "-c", os.path.join(CSRC, "psc_grammar.cpp"), "-o", gram_obj])
-    _run([HIPCC, *HIP_FLAGS, "-c", os.path.join(CSRC, "psc_device.hip"), "-o", dev_obj])
+    for name, obj in zip(DEVICE_SOURCES, dev_objs):
+        _run([HIPCC, *HIP_FLAGS, "-c", os.path.join(CSRC, name + ".hip"), "-o", obj])
     tmp = LIB + ".tmp"
-    _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", host_obj, store_obj, gram_obj, dev_obj, "-lz", "-o", tmp])
+    _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", host_obj, store_obj, gram_obj, *dev_objs, "-lz", "-o", tmp])
     os.replace(tmp, LIB)
     # the measurement aid beside it (dependent-load latency; bench.py --latency-probe)
     tmp = PROBE_LIB + ".tmp"

@@ -29,7 +29,9 @@ EXPORTED = ["psc_build", "psc_info", "psc_device_bytes", "psc_bind_device", "psc
             "psc_compute_masks_n", "psc_compute_classes_n", "psc_compute_and_apply_n", "psc_compute_and_argmax_n",
             "psc_predictor_fill", "psc_predictor_updates", "psc_timeline_records", "psc_compute_and_apply_timeline",
             "psc_set_options", "psc_compute_and_argmax_noalloc", "psc_grammar_compile", "psc_grammar_view",
-            "psc_grammar_symbol_name", "psc_grammar_free", "psc_build_from_text"]
+            "psc_grammar_symbol_name", "psc_grammar_free", "psc_build_from_text", "psc_quantize_rows",
+            "psc_head_workspace", "psc_head_logits", "psc_penalize", "psc_append_tokens", "psc_sample_workspace",
+            "psc_sample"]
 
 BIND_FLAT, BIND_SLICED = 1, 2
 OPT_SPECULATE = 1
@@ -62,7 +64,9 @@ def _torch_types():
         _T.update(tensor=torch.Tensor, i32=torch.int32,
                   codes={torch.float32: PSC_F32, torch.bfloat16: PSC_BF16},
                   stream=(lambda: raw(device())) if raw and device
-                  else lambda: torch.cuda.current_stream().cuda_stream)
+                  else lambda: torch.cuda.current_stream().cuda_stream,
+                  f32=torch.float32, bf16=torch.bfloat16, i8=torch.int8, u8=torch.uint8, empty=torch.empty,
+                  device=device or torch.cuda.current_device)
     return _T
 
 
@@ -158,6 +162,17 @@ class Info(C.Structure):
         return {k: getattr(self, k) for k, _ in self._fields_}
 
 
+class _Penalties(C.Structure):
+    _fields_ = [("history", C.c_void_p), ("lens", C.c_void_p), ("prompt_lens", C.c_void_p), ("cap", C.c_int32),
+                ("n_bias", C.c_int32), ("repetition", C.c_void_p), ("presence", C.c_void_p),
+                ("frequency", C.c_void_p), ("bias_ids", C.c_void_p), ("bias_values", C.c_void_p)]
+
+
+class _Sampling(C.Structure):
+    _fields_ = [("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p),
+                ("noise", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -214,6 +229,16 @@ def lib() -> C.CDLL:
         L.psc_timeline_records.argtypes = [P, I32, C.c_int]
         L.psc_timeline_records.restype = I64
         L.psc_compute_and_apply_timeline.argtypes = [P, P, I64, P, P, I32, P, P, C.c_int, I32, P, I64, P]
+        L.psc_quantize_rows.argtypes = [P, C.c_int, I64, I64, I32, P, I64, P, P]
+        L.psc_head_workspace.argtypes = [I32, I32, I32]
+        L.psc_head_workspace.restype = C.c_size_t
+        L.psc_head_logits.argtypes = [P, C.c_int, I64, I32, I32, P, I64, P, I32, P, P, P, C.c_int, I64, P,
+                                      C.c_size_t, P]
+        L.psc_penalize.argtypes = [P, C.c_int, I64, I32, I32, P, P, P]
+        L.psc_append_tokens.argtypes = [P, I32, P, I32, P, P, P]
+        L.psc_sample_workspace.argtypes = [I32, I32, C.c_int]
+        L.psc_sample_workspace.restype = C.c_size_t
+        L.psc_sample.argtypes = [P, C.c_int, I64, I32, I32, P, P, I32, P, P, P, P, P, C.c_size_t, P]
         L.psc_free.argtypes = [P]
         L.psc_free.restype = None
         L.psc_last_error.restype = C.c_char_p
@@ -225,7 +250,8 @@ def lib() -> C.CDLL:
                      "psc_compute_masks_n", "psc_compute_classes_n", "psc_compute_and_apply_n",
                      "psc_compute_and_argmax_n", "psc_predictor_fill", "psc_predictor_updates",
                      "psc_compute_and_apply_timeline", "psc_set_options", "psc_compute_and_argmax_noalloc",
-                     "psc_grammar_compile", "psc_grammar_view", "psc_build_from_text"):
+                     "psc_grammar_compile", "psc_grammar_view", "psc_build_from_text", "psc_quantize_rows",
+                     "psc_head_logits", "psc_penalize", "psc_append_tokens", "psc_sample"):
             getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -663,3 +689,164 @@ def apply_mask(logits, bitmask, stream=None):
     _i32(bitmask, "bitmask", logits.get_device(), shape=(B, (V + 31) // 32))
     _check(lib().psc_apply_mask(logits.data_ptr(), dt, bitmask.data_ptr(), B, V, _stream_ptr(stream)))
     return logits
+
+
+# ---------------------------------------------------------------- operators around the logits
+
+SAMPLE_MAX_K = 64
+
+
+def _rows(t, name: str, dev: int | None = None, shape: tuple | None = None):
+    """(dtype code, row stride) of t, a float32 or bfloat16 matrix on the
+    current device whose rows do not overlap and whose elements are adjacent."""
+    T = _T or _torch_types()
+    _require(isinstance(t, T["tensor"]) and t.dim() == 2, f"{name} to be a matrix")
+    code = T["codes"].get(t.dtype)
+    _require(code is not None, f"float32 or bfloat16 {name}, not {t.dtype}")
+    _require(shape is None or tuple(t.shape) == tuple(shape), f"{name} of shape {shape and tuple(shape)}, not {tuple(t.shape)}")
+    rows, cols = t.shape
+    _require(cols <= 1 or t.stride(1) == 1, f"{name} whose rows' elements are adjacent")
+    stride = t.stride(0) if rows > 1 else cols
+    _require(rows <= 1 or stride >= cols, f"{name} whose rows do not overlap")
+    at = t.get_device()
+    _require(at >= 0 and at == T["device"]() and (dev is None or at == dev), f"{name} on the current device")
+    return code, stride
+
+
+def _vector(t, name: str, dtype: str, dev: int, shape: tuple):
+    """The address of t, a contiguous tensor of `shape`; None for None."""
+    if t is None:
+        return None
+    T = _T or _torch_types()
+    if not (type(t) is T["tensor"] and t.dtype is T[dtype] and t.shape == shape and t.get_device() == dev
+            and t.is_contiguous()):
+        _require(isinstance(t, T["tensor"]) and t.dtype is T[dtype] and tuple(t.shape) == tuple(shape)
+                 and t.is_contiguous(), f"{name} to be a contiguous {T[dtype]} tensor of shape {tuple(shape)}")
+        _require(t.get_device() == dev, f"{name} on device {dev}, not {t.get_device()}")
+    return t.data_ptr()
+
+
+def _new(shape, dtype: str, device, stream):
+    """An uninitialised tensor for a call on `stream` (None: the current one),
+    out of that stream's memory."""
+    T = _T or _torch_types()
+    if stream is None:
+        return T["empty"](shape, dtype=T[dtype], device=device)
+    import torch
+    with torch.cuda.stream(stream):
+        return T["empty"](shape, dtype=T[dtype], device=device)
+
+
+def quantize_rows(x, stream=None):
+    """(q, scales): the rows of x [N, D] in 8 bits, int8 [N, D] whose rows start
+    at multiples of 16 bytes, with a scale each, float32 [N] (psc_quantize_rows)."""
+    code, stride = _rows(x, "x")
+    n, D = x.shape
+    q_stride = (D + 15) // 16 * 16
+    q, scales = _new((n, q_stride), "i8", x.device, stream), _new(n, "f32", x.device, stream)
+    _check(lib().psc_quantize_rows(x.data_ptr(), code, stride, n, D, q.data_ptr(), q_stride, scales.data_ptr(),
+                                   _stream_ptr(stream)))
+    return q[:, :D], scales
+
+
+def head_logits(x, w, w_scales, dtype=None, bias=None, bitmask=None, out=None, stream=None):
+    """Logits [B, V] of hidden states x [B, D] by 8-bit weights w [V, D] with a
+    scale per token (quantize_rows), forbidden tokens -inf (psc_head_logits).
+    `out`: where to write them (its rows may lie apart); else a new tensor of
+    `dtype`, that of x by default."""
+    T = _T or _torch_types()
+    x_code, x_stride = _rows(x, "x")
+    B, D = x.shape
+    dev = x.get_device()
+    _require(isinstance(w, T["tensor"]) and w.dtype is T["i8"] and w.dim() == 2 and w.shape[1] == D and D > 0,
+             f"w to be an int8 matrix of rows of {D} elements")
+    V = w.shape[0]
+    w_stride = w.stride(0) if V > 1 else (D + 15) // 16 * 16
+    _require(w.get_device() == dev and (D == 1 or w.stride(1) == 1) and w_stride >= D and w_stride % 16 == 0
+             and w.data_ptr() % 16 == 0, "w on x's device, with adjacent elements and rows that start at 16 bytes")
+    if out is None:
+        code, y_stride = T["codes"].get(x.dtype if dtype is None else dtype), V
+        _require(code is not None, f"float32 or bfloat16 logits, not {dtype}")
+        out = _new((B, V), ("f32", "bf16")[code], x.device, stream)
+    else:
+        _require(dtype is None or dtype == out.dtype, "dtype to be that of out")
+        code, y_stride = _rows(out, "out", dev, (B, V))
+    L = lib()
+    scales = _vector(w_scales, "w_scales", "f32", dev, (V,))
+    _require(scales is not None, "w_scales")
+    bias = _vector(bias, "bias", "f32", dev, (V,))
+    words = _vector(bitmask, "bitmask", "i32", dev, (B, (V + 31) // 32))
+    n = L.psc_head_workspace(B, D, V)
+    ws = _new(n, "u8", x.device, stream)
+    _check(L.psc_head_logits(x.data_ptr(), x_code, x_stride, B, D, w.data_ptr(), w_stride, scales, V, bias, words,
+                             out.data_ptr(), code, y_stride, ws.data_ptr(), n, _stream_ptr(stream)))
+    return out
+
+
+def penalize(logits, history=None, lens=None, prompt_lens=None, repetition=None, presence=None, frequency=None,
+             bias_ids=None, bias_values=None, bitmask=None, stream=None):
+    """In place on logits [B, V]: penalties of the tokens in history [B, cap]
+    (int32; lens [B] of them, the first prompt_lens [B] the prompt), biases
+    (ids int32 [B, n], -1 for none; values float32), -inf where the bitmask
+    forbids (psc_penalize).  Returns logits."""
+    code, stride = _rows(logits, "logits")
+    (B, V), dev = logits.shape, logits.get_device()
+    cap = n_bias = 0
+    if history is not None:
+        _require(history.dim() == 2 and lens is not None, "history to be a matrix, with lens")
+        cap = history.shape[1]
+    if bias_ids is not None:
+        _require(bias_ids.dim() == 2 and bias_values is not None, "bias_ids to be a matrix, with bias_values")
+        n_bias = bias_ids.shape[1]
+    rows = (B,)
+    p = _Penalties(_vector(history, "history", "i32", dev, (B, cap)), _vector(lens, "lens", "i32", dev, rows),
+                   _vector(prompt_lens, "prompt_lens", "i32", dev, rows), cap, n_bias,
+                   _vector(repetition, "repetition", "f32", dev, rows),
+                   _vector(presence, "presence", "f32", dev, rows),
+                   _vector(frequency, "frequency", "f32", dev, rows),
+                   _vector(bias_ids, "bias_ids", "i32", dev, (B, n_bias)),
+                   _vector(bias_values, "bias_values", "f32", dev, (B, n_bias)))
+    words = _vector(bitmask, "bitmask", "i32", dev, (B, (V + 31) // 32))
+    _check(lib().psc_penalize(logits.data_ptr(), code, stride, B, V, C.byref(p), words, _stream_ptr(stream)))
+    return logits
+
+
+def append_tokens(history, lens, tokens, status=None, stream=None):
+    """tokens [B] (int32, < 0: none) to the ends of the histories [B, cap], in
+    place (psc_append_tokens); status [B], if given, receives ADV_OK,
+    ADV_SKIPPED, ADV_OVERFLOW or ADV_BAD_INPUT."""
+    T = _T or _torch_types()
+    _require(isinstance(history, T["tensor"]) and history.dim() == 2 and history.get_device() >= 0
+             and history.get_device() == T["device"](), "history to be a matrix on the current device")
+    (B, cap), dev = history.shape, history.get_device()
+    at = [_vector(t, name, "i32", dev, shape) for t, name, shape in
+          ((history, "history", (B, cap)), (lens, "lens", (B,)), (tokens, "tokens", (B,)), (status, "status", (B,)))]
+    _require(at[1] is not None and at[2] is not None, "lens and tokens")
+    _check(lib().psc_append_tokens(at[0], cap, at[1], B, at[2], at[3], _stream_ptr(stream)))
+
+
+def sample(logits, k, bitmask=None, temperature=None, top_k=None, top_p=None, min_p=None, noise=None, stream=None):
+    """(tokens int32 [B], logprobs float32 [B], ids int32 [B, k], id_logprobs
+    float32 [B, k]) of logits [B, V] under the bitmask: the k best tokens and
+    one drawn from them (psc_sample).  temperature, top_p, min_p: float32 [B];
+    top_k: int32 [B]; noise: float32 [B, k] of unit exponentials (None: the
+    best token)."""
+    code, stride = _rows(logits, "logits")
+    (B, V), dev = logits.shape, logits.get_device()
+    k = int(k)
+    _require(1 <= k <= SAMPLE_MAX_K, f"k in [1, {SAMPLE_MAX_K}]")
+    _require(V > 0, "logits of at least one token")
+    rows = (B,)
+    p = _Sampling(_vector(temperature, "temperature", "f32", dev, rows), _vector(top_k, "top_k", "i32", dev, rows),
+                  _vector(top_p, "top_p", "f32", dev, rows), _vector(min_p, "min_p", "f32", dev, rows),
+                  _vector(noise, "noise", "f32", dev, (B, k)))
+    words = _vector(bitmask, "bitmask", "i32", dev, (B, (V + 31) // 32))
+    L, device = lib(), logits.device
+    n = L.psc_sample_workspace(B, V, code)
+    ws = _new(n, "u8", device, stream)
+    tokens, ids = _new(B, "i32", device, stream), _new((B, k), "i32", device, stream)
+    logprobs, id_logprobs = _new(B, "f32", device, stream), _new((B, k), "f32", device, stream)
+    _check(L.psc_sample(logits.data_ptr(), code, stride, B, V, words, C.byref(p), k, tokens.data_ptr(),
+                        logprobs.data_ptr(), ids.data_ptr(), id_logprobs.data_ptr(), ws.data_ptr(), n,
+                        _stream_ptr(stream)))
+    return tokens, logprobs, ids, id_logprobs

@@ -1,0 +1,488 @@
+"""The operators around the logits against plain implementations in 64 bits.
+
+Tolerances: u = 2^-24 is the relative error of a rounding to float32.  A head's
+logit takes four of them (the sum, two scales, the bias), a penalised one at
+most six; they are held to eight of the sum of the terms' absolute values.
+Rounding to bfloat16 keeps the order of numbers, so a bfloat16 result lies
+between the roundings of the two ends of what float32 may be off.
+"""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2608_03065_amd import psc  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def host(t):
+    return t.detach().cpu().double().numpy() if t.is_floating_point() else t.cpu().numpy()
+
+
+def rows_apart(t, gap):
+    """A copy of the matrix t whose rows lie `gap` elements further apart."""
+    if not gap:
+        return t.clone()
+    wide = torch.full((t.shape[0], t.shape[1] + gap), 7, dtype=t.dtype, device=t.device)
+    view = wide[:, gap // 2:gap // 2 + t.shape[1]]
+    view.copy_(t)
+    return view
+
+
+def around(view, gap):
+    """What lies between the rows of rows_apart's result."""
+    if not gap:
+        return True
+    wide, cols, at = view._base, view.shape[1], gap // 2
+    return bool((wide[:, :at] == 7).all() and (wide[:, at + cols:] == 7).all())
+
+
+def mask(B, V, seed, shares):
+    """int32 words and booleans; row b allows each token with probability shares[b % len(shares)]."""
+    r = np.random.default_rng(seed)
+    keep = np.zeros((B, (V + 31) // 32 * 32), bool)
+    for b in range(B):
+        keep[b, :V] = r.random(V) < shares[b % len(shares)]
+    words = np.packbits(keep, axis=1, bitorder="little").view(np.int32)
+    return torch.from_numpy(words.copy()).to(DEV), keep[:, :V]
+
+
+def close(got, want, bound):
+    """Equal where `want` is not finite, else float32 within bound, or bfloat16 between the roundings of its ends."""
+    fine, dtype = np.isfinite(want), got.dtype
+    got = host(got)
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    assert np.array_equal(got[~fine & ~np.isnan(want)], want[~fine & ~np.isnan(want)])
+    got, want, bound = got[fine], want[fine], np.broadcast_to(bound, want.shape)[fine]
+    low, high = want - bound, want + bound
+    if dtype == torch.bfloat16:
+        low, high = (torch.from_numpy(a).to(dtype).double().numpy() for a in (low, high))
+    bad = (got < low) | (got > high)
+    assert not bad.any(), (bad.sum(), np.abs(got - want).max())
+
+
+# ---------------------------------------------------------------- rows in 8 bits
+
+def quantized(x):
+    x = x.float().cpu().numpy()
+    most = np.abs(x).max(1, keepdims=True) if x.shape[1] else np.zeros((x.shape[0], 1), np.float32)
+    fine = np.isfinite(most)
+    scale = np.where(fine, most / np.float32(127), np.float32("nan"))
+    with np.errstate(invalid="ignore", divide="ignore"):
+        q = np.where(scale > 0, np.clip(np.rint(x / scale), -127, 127), 0)
+    return q.astype(np.int64), scale[:, 0]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,D,gap", [(1, 1, 0), (3, 7, 0), (5, 16, 3), (2, 100, 0), (7, 2047, 1), (4, 2049, 0), (3, 8192, 8),
+                                     (2, 20000, 0)])
+def test_quantize_rows(dtype, n, D, gap):
+    g = torch.Generator().manual_seed(D)
+    x = torch.randn(n, D, generator=g).to(TYPES[dtype])
+    x[0, D // 2] = x[0].abs().max() * 2          # halves of the largest one are ties
+    x[0, D // 3] = x[0, D // 2] / 2
+    if n > 2:
+        x[2] = 0
+    q, s = psc.quantize_rows(rows_apart(x.to(DEV), gap))
+    want, scale = quantized(x)
+    assert q.shape == (n, D) and q.stride(0) % 16 == 0 and q.data_ptr() % 16 == 0
+    assert np.array_equal(host(q), want)
+    assert np.array_equal(s.cpu().numpy(), scale)
+    if q.stride(0) > D:                          # the bytes up to the next row are zeros
+        wide = torch.as_strided(q, (n, q.stride(0)), q.stride())
+        assert not bool(wide[:, D:].any())
+
+
+def test_quantize_rows_that_are_not_numbers():
+    x = torch.ones(5, 40, device=DEV)
+    x[0, 3], x[1, 39], x[2, 0], x[3] = math.nan, math.inf, -math.inf, 1e-44
+    q, s = psc.quantize_rows(x)
+    assert bool(torch.isnan(s[:3]).all()) and not bool(q[:3].any())
+    want, scale = quantized(x[3:])
+    assert np.array_equal(host(q[3:]), want) and np.array_equal(s[3:].cpu().numpy(), scale)
+
+
+# ---------------------------------------------------------------- head
+
+def head_case(B, D, V, dtype, seed, x_dtype=torch.bfloat16):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(B, D, generator=g).to(x_dtype)
+    wide = torch.randint(-128, 128, (V, (D + 15) // 16 * 16), generator=g, dtype=torch.int8)
+    w = wide[:, :D]
+    scales, bias = torch.rand(V, generator=g) / D, torch.randn(V, generator=g)
+    q, s = quantized(x)
+    y = (q @ w.long().numpy().T).astype(np.float64) * s[:, None].astype(np.float64) * scales.double().numpy()
+    return x.to(DEV), wide.to(DEV)[:, :D], scales.to(DEV), bias.to(DEV), y, bias.double().numpy()
+
+
+def head_bound(y, bias):
+    return 8 * U * (np.abs(y) + np.abs(bias))
+
+
+HEADS = [(1, 64, 1), (1, 1, 33), (2, 17, 64), (3, 128, 65), (8, 200, 513), (15, 1024, 1000), (16, 130, 700), (17, 256, 513),
+         (33, 96, 1537), (48, 640, 300), (64, 512, 2049), (65, 300, 777), (100, 1000, 4097), (128, 384, 515),
+         (200, 129, 1025), (256, 256, 600), (257, 320, 1100), (300, 128, 5000), (520, 144, 257), (1, 8192, 513), (4, 5000, 100),
+         (60, 4096, 130), (300, 4096, 300)]
+
+
+@pytest.mark.parametrize("B,D,V", HEADS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_head_logits(B, D, V, dtype):
+    x, w, scales, _, y, _ = head_case(B, D, V, dtype, B + D + V)
+    got = psc.head_logits(x, w, scales, dtype=TYPES[dtype])
+    assert got.dtype == TYPES[dtype]
+    close(got, y, head_bound(y, 0))
+
+
+@pytest.mark.parametrize("B,D,V", HEADS)
+@pytest.mark.parametrize("shares", [(0.0,), (0.9, 0.001, 0.0, 0.05), (0.002,)])
+def test_head_logits_masked_with_bias(B, D, V, shares):
+    dtype = ("bf16", "f32")[(B + V) % 2]
+    gap = (0, 1, 8)[D % 3]
+    x, w, scales, bias, y, b = head_case(B, D, V, dtype, B + D + V + 1)
+    words, keep = mask(B, V, D, shares)
+    out = rows_apart(torch.zeros(B, V, dtype=TYPES[dtype], device=DEV), gap)
+    assert psc.head_logits(x, w, scales, bias=bias, bitmask=words, out=out) is out
+    close(out, np.where(keep, y + b, -np.inf), head_bound(y, b))
+    assert around(out, gap)
+
+
+def test_head_logits_of_strided_and_fp32_states():
+    x, w, scales, _, y, _ = head_case(20, 200, 600, "f32", 5, torch.float32)
+    got = psc.head_logits(rows_apart(x, 5), w, scales)
+    assert got.dtype == torch.float32
+    close(got, y, head_bound(y, 0))
+
+
+@pytest.mark.parametrize("B", [1, 16, 40, 130, 300])
+def test_head_logits_of_rows_that_are_not_numbers_or_zero(B):
+    x, w, scales, _, y, _ = head_case(B, 256, 600, "f32", 6)
+    x[0, 5] = math.nan
+    y[0] = np.nan
+    if B > 2:
+        x[1], x[2, 0] = 0, math.inf
+        y[1], y[2] = 0, np.nan
+    close(psc.head_logits(x, w, scales, dtype=torch.float32), y, head_bound(y, 0))
+
+
+def test_head_logits_largest_sum():
+    """Every product 127 * -128 at the largest D: the sum is the one that fits 32 bits."""
+    D = 131072
+    w = torch.full((3, D), -128, dtype=torch.int8, device=DEV)
+    got = psc.head_logits(torch.ones(2, D, device=DEV), w, torch.ones(3, device=DEV))
+    want = np.full((2, 3), -127.0 * 128 * D * float(np.float32(1) / np.float32(127)))
+    close(got, want, 8 * U * np.abs(want))
+
+
+@pytest.mark.parametrize("B,D", [(5, 100), (80, 260), (300, 260)])
+def test_head_logits_ignores_what_lies_between_weights(B, D):
+    x, w, scales, _, y, _ = head_case(B, D, 300, "f32", 8)
+    wide = torch.full((300, (D + 15) // 16 * 16 + 32), 99, dtype=torch.int8, device=DEV)
+    wide[:, :D] = w
+    close(psc.head_logits(x, wide[:, :D], scales, dtype=torch.float32), y, head_bound(y, 0))
+
+
+def test_quantized_weights_go_into_the_head():
+    g = torch.Generator().manual_seed(9)
+    x, w = torch.randn(6, 150, generator=g).to(torch.bfloat16), torch.randn(400, 150, generator=g)
+    q, s = psc.quantize_rows(w.to(DEV))
+    (xq, xs), (wq, ws) = quantized(x), quantized(w)
+    y = (xq @ wq.T) * xs[:, None].astype(np.float64) * ws.astype(np.float64)
+    close(psc.head_logits(x.to(DEV), q, s, dtype=torch.float32), y, head_bound(y, 0))
+    # 8 bits a side: the logits of the unquantised product, to the quantisation's own step
+    exact = x.double().numpy() @ w.double().numpy().T
+    assert np.abs(y - exact).std() < 0.02 * exact.std()
+
+
+# ---------------------------------------------------------------- penalties
+
+def penalized(x, history, lens, prompts, r, p, f, ids=None, values=None, keep=None):
+    """The operator in 64 bits, and the sum of the absolute values of the terms that it adds up."""
+    y, size = x.copy(), np.abs(x)
+    B, V = x.shape
+    for b in range(B):
+        n = min(max(int(lens[b]), 0), history.shape[1])
+        m = min(max(int(prompts[b]), 0), n)
+        said = history[b, :n]
+        for v in np.unique(said[(said >= 0) & (said < V)]):
+            y[b, v] = y[b, v] / r[b] if y[b, v] > 0 else y[b, v] * r[b]
+        size[b] = np.maximum(size[b], np.abs(y[b]))
+        after = said[m:]
+        for v, c in zip(*np.unique(after[(after >= 0) & (after < V)], return_counts=True)):
+            y[b, v] -= c * f[b] + p[b]
+            size[b, v] += c * abs(f[b]) + abs(p[b])
+        if ids is not None:
+            for v, a in {int(v): a for v, a in zip(ids[b], values[b])}.items():
+                if 0 <= v < V:
+                    y[b, v] += a
+                    size[b, v] += abs(a)
+    y[np.isneginf(x)] = -np.inf
+    if keep is not None:
+        y[~keep] = -np.inf
+    return y, size
+
+
+PENALTIES = [(1, 1, 1, 0), (1, 33, 5, 3), (3, 513, 40, 0), (4, 1000, 1, 7), (2, 32769, 300, 20), (5, 70001, 2000, 300),
+             (9, 513, 5000, 1024), (300, 2049, 64, 5), (2, 131073, 20001, 0), (1, 600, 33000, 2)]
+
+
+@pytest.mark.parametrize("B,V,cap,biases", PENALTIES)
+@pytest.mark.parametrize("dtype,masked,gap", [("bf16", True, 0), ("f32", False, 3), ("f32", True, 0), ("bf16", False, 1)])
+def test_penalize(B, V, cap, biases, dtype, masked, gap):
+    r = np.random.default_rng(V + cap)
+    x = torch.from_numpy(r.normal(0, 4, (B, V))).to(TYPES[dtype])
+    x[:, ::7] = -math.inf
+    x[:, 1::11] = 0
+    # few distinct tokens, so that counts are large, beside tokens that are none
+    history = np.where(r.random((B, cap)) < 0.5, r.integers(0, min(V, 20), (B, cap)), r.integers(-2, V + 2, (B, cap)))
+    history = history.astype(np.int32)
+    lens = r.integers(0, cap + 1, B).astype(np.int32)
+    lens[0] = cap
+    if B > 2:
+        lens[1], lens[2] = 0, cap + 5                   # clamped
+    prompts = (lens * r.random(B)).astype(np.int32)
+    rep, pres, freq = r.uniform(0.8, 1.6, B), r.uniform(-1, 1, B), r.uniform(0, 0.5, B)
+    ids = r.integers(-1, V + 1, (B, biases)).astype(np.int32)
+    if biases > 4:
+        ids[:, 3], ids[:, 1] = ids[:, 0], history[:, 0]  # a token twice, and one of the history
+    values = r.normal(0, 5, (B, biases))
+    words, keep = mask(B, V, cap, (0.5, 0.0, 0.97, 0.01)) if masked else (None, None)
+    t = lambda a: torch.from_numpy(a.astype(np.float32) if a.dtype == np.float64 else a).to(DEV)  # noqa: E731
+    back = lambda a: a.astype(np.float32).astype(np.float64)  # noqa: E731
+    got = rows_apart(x.to(DEV), gap)
+    assert psc.penalize(got, t(history), t(lens), prompt_lens=t(prompts), repetition=t(rep), presence=t(pres),
+                        frequency=t(freq), bias_ids=t(ids) if biases else None,
+                        bias_values=t(values) if biases else None, bitmask=words) is got
+    want, size = penalized(x.double().numpy(), history, lens, prompts, back(rep), back(pres), back(freq), ids,
+                           back(values), keep)
+    close(got, want, 8 * U * size)
+    assert around(got, gap)
+
+
+def test_penalize_parts_alone():
+    r = np.random.default_rng(3)
+    B, V, cap = 6, 900, 50
+    x = torch.from_numpy(r.normal(0, 4, (B, V))).float()
+    history = torch.from_numpy(r.integers(0, V, (B, cap)).astype(np.int32)).to(DEV)
+    lens = torch.full((B,), cap, dtype=torch.int32, device=DEV)
+    f = torch.full((B,), 0.25, device=DEV)
+    one, none = np.ones(B), np.zeros(B)
+    args = (x.double().numpy(), host(history), host(lens), none)
+    for kw, (rep, pres, freq) in ((dict(repetition=f + 1), (one * 1.25, none, none)), (dict(presence=f), (one, one / 4, none)),
+                                  (dict(frequency=f), (one, none, one / 4)), ({}, (one, none, none))):
+        got = psc.penalize(x.to(DEV), history, lens, **kw)
+        want, size = penalized(*args, rep, pres, freq)
+        close(got, want, 8 * U * size)
+    # no history: biases only, then the mask only, then nothing
+    ids = torch.tensor([[5, 7, 5]] * B, dtype=torch.int32, device=DEV)
+    values = torch.tensor([[1.0, 2.0, 4.0]] * B, device=DEV)
+    want = x.double().numpy()
+    want[:, 5] += 4
+    want[:, 7] += 2
+    close(psc.penalize(x.to(DEV), bias_ids=ids, bias_values=values), want, 2 * U * np.abs(want))
+    words, keep = mask(B, V, 1, (0.4,))
+    close(psc.penalize(x.to(DEV), bitmask=words), np.where(keep, x.double().numpy(), -np.inf), 0)
+    assert torch.equal(psc.penalize(x.to(DEV)).cpu(), x)
+
+
+def test_penalize_leaves_other_logits_bits_alone():
+    """NaNs with a payload and -0 outlive a call that does not concern them."""
+    x = torch.full((2, 700), -0.0, device=DEV)
+    x.view(torch.int32)[:, 5] = 0x7FC12345
+    before = x.view(torch.int32).clone()
+    history = torch.tensor([[3, 3, 9]] * 2, dtype=torch.int32, device=DEV)
+    lens = torch.full((2,), 3, dtype=torch.int32, device=DEV)
+    psc.penalize(x, history, lens, presence=torch.ones(2, device=DEV))
+    changed = (x.view(torch.int32) != before).nonzero().cpu().tolist()
+    assert changed == [[0, 3], [0, 9], [1, 3], [1, 9]]
+
+
+def test_append_tokens():
+    history = torch.full((6, 4), -7, dtype=torch.int32, device=DEV)
+    lens = torch.tensor([0, 3, 4, 1, -1, 9], dtype=torch.int32, device=DEV)
+    status = torch.full((6,), 99, dtype=torch.int32, device=DEV)
+    psc.append_tokens(history, lens, torch.tensor([10, 11, 12, -1, 14, 15], dtype=torch.int32, device=DEV), status)
+    assert status.tolist() == [psc.ADV_OK, psc.ADV_OK, psc.ADV_OVERFLOW, psc.ADV_SKIPPED, psc.ADV_BAD_INPUT, psc.ADV_OVERFLOW]
+    assert lens.tolist() == [1, 4, 4, 1, -1, 9]
+    want = torch.full((6, 4), -7)
+    want[0, 0], want[1, 3] = 10, 11
+    assert torch.equal(history.cpu().long(), want)
+    psc.append_tokens(history, lens, torch.tensor([1] * 6, dtype=torch.int32, device=DEV))
+    assert lens.tolist() == [2, 4, 4, 2, -1, 9]
+
+
+# ---------------------------------------------------------------- sampling
+
+def sampled(x, k, keep=None, temperature=None, top_k=None, top_p=None, min_p=None, noise=None):
+    """The operator in 64 bits: (token or None where the draw hangs on less than 1e-4, logprob, ids, logprobs, spread)."""
+    B, V = x.shape
+    ids, logprobs = np.full((B, k), -1, np.int32), np.full((B, k), -np.inf)
+    tokens, spread = [], np.zeros((B, k))
+    for b in range(B):
+        row = np.where(keep[b], x[b], -np.inf) if keep is not None else x[b]
+        order = np.argsort(np.where(np.isnan(row), -np.inf, -row), kind="stable")[:k]
+        order = order[~np.isneginf(row[order])]
+        n = order.size
+        if not n:
+            tokens.append(-1)
+            continue
+        t = 1.0 if temperature is None else temperature[b]
+        greedy = noise is None or not t > 0
+        t = t if t > 0 else 1.0
+        ids[b, :n] = order
+        if not row[order[0]] < np.inf:
+            logprobs[b, :n] = np.nan
+            tokens.append(int(order[0]))
+            continue
+        z = (row - row[order[0]]) / t
+        logprobs[b, :n] = z[order] - np.log(np.exp(z).sum())
+        spread[b, :n] = -z[order]
+        if greedy:
+            tokens.append(int(order[0]))
+            continue
+        top = n if top_k is None or top_k[b] <= 0 else min(n, top_k[b])
+        w = np.exp(z[order[:top]])
+        before = (np.cumsum(w) - w) / w.sum()
+        cut = 1.0 if top_p is None else top_p[b]
+        least = 0.0 if min_p is None else min_p[b]
+        first = np.arange(top) == 0
+        kept = ((cut >= 1) | (before < cut) | first) & ((w >= least) | first)
+        near = ((cut < 1) & (np.abs(before - cut) < 1e-4) | (np.abs(w - least) < 1e-4 * w)) & ~first
+        score = np.where(kept, w / noise[b, :top], -1)
+        best = np.argsort(-score, kind="stable")
+        margin = near.any() or (top > 1 and score[best[1]] > score[best[0]] * (1 - 1e-4))
+        tokens.append(None if margin else int(order[best[0]]))
+    return tokens, ids, logprobs, spread
+
+
+def check_sample(x, k, words=None, keep=None, **kw):
+    """The sum of V exponentials is off by at most 2^-17 of itself (its arguments, up to 20 where they matter, are off by
+    2^-22 of themselves, and partial sums of up to 64 terms are rounded); z by 2^-21 of itself."""
+    t = {n: a if isinstance(a, torch.Tensor) or a is None else torch.from_numpy(a).to(DEV) for n, a in kw.items()}
+    tokens, logprob, ids, logprobs = psc.sample(x, k, bitmask=words, **t)
+    plain = {n: None if a is None else a.astype(np.float64) if a.dtype == np.float32 else a for n, a in kw.items()}
+    want = sampled(host(x), k, keep, **plain)
+    assert np.array_equal(host(ids), want[1])
+    close(logprobs, want[2], 2.0 ** -17 + 2.0 ** -21 * want[3])
+    got, lp = host(tokens), host(logprobs)
+    sure = [b for b, v in enumerate(want[0]) if v is not None]
+    assert len(sure) >= 0.9 * len(got) - 1
+    assert [int(got[b]) for b in sure] == [want[0][b] for b in sure]
+    for b in range(len(got)):
+        at = np.nonzero(want[1][b] == got[b])[0][0]
+        assert np.array_equal(host(logprob)[b], lp[b, at], equal_nan=True)
+
+
+SAMPLES = [(1, 1, 1), (1, 1, 64), (2, 33, 5), (3, 64, 64), (5, 513, 20), (2, 2048, 64), (7, 2049, 1), (3, 32000, 50),
+           (2, 32001, 64), (4, 70001, 33), (2, 262145, 64), (70, 1000, 17), (600, 129, 8)]
+
+
+@pytest.mark.parametrize("B,V,k", SAMPLES)
+@pytest.mark.parametrize("dtype,shares,gap", [("bf16", None, 0), ("f32", (0.9, 0.0, 0.001, 0.3), 0), ("bf16", (0.01,), 3),
+                                              ("f32", None, 1), ("bf16", (0.97, 0.0), 0)])
+def test_sample(B, V, k, dtype, shares, gap):
+    r = np.random.default_rng(B + V + k)
+    x = rows_apart(torch.from_numpy(r.normal(0, 3, (B, V))).to(TYPES[dtype]).to(DEV), gap)
+    words, keep = mask(B, V, k, shares) if shares else (None, None)
+    f = lambda a: a.astype(np.float32)  # noqa: E731
+    temperature = f(r.uniform(0.4, 2, B))
+    temperature[::5] = 0
+    check_sample(x, k, words, keep, temperature=temperature, top_k=r.integers(-1, k + 3, B).astype(np.int32),
+                 top_p=f(r.uniform(0.5, 1.1, B)), min_p=f(r.uniform(0, 0.1, B)), noise=f(r.exponential(1, (B, k)) + 1e-9))
+    check_sample(x, k, words, keep)
+    assert around(x, gap)
+
+
+@pytest.mark.parametrize("V,k", [(64, 64), (5000, 64), (5000, 3), (151665, 40), (262145, 64)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_sample_ties_go_to_the_lowest_id(V, k, dtype):
+    r = np.random.default_rng(V)
+    x = np.zeros((6, V))
+    x[1] = r.integers(0, 3, V)              # three values
+    x[2] = np.where(r.random(V) < 0.5, 0.0, -0.0)
+    x[3] = -5
+    x[3, V // 2:V // 2 + 70] = 1            # more ties than k, across lines
+    x[4] = np.linspace(-1, 1, V)
+    x[5, -1] = 1
+    check_sample(torch.from_numpy(x).to(TYPES[dtype]).to(DEV), k, temperature=np.full(6, 0.7, np.float32))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_sample_of_rows_that_are_not_numbers_or_empty(dtype):
+    r = np.random.default_rng(1)
+    x = r.normal(0, 3, (9, 5000))
+    x[0, [7, 4000]] = np.nan
+    x[1, [9, 11]] = np.inf
+    x[2] = -np.inf
+    x[3] = -np.inf
+    x[3, 1234] = -3.0e38
+    x[4, 100:] = -np.inf
+    x[5] = np.nan
+    x[6, 5] = np.finfo(np.float32).max / 2
+    x[7] = r.normal(0, 1e-38, 5000)
+    x[8] *= 1e30
+    check_sample(torch.from_numpy(x).to(TYPES[dtype]).to(DEV), 20, noise=(r.exponential(1, (9, 20)) + 1e-9).astype(np.float32),
+                 temperature=np.full(9, 1.5, np.float32))
+
+
+def test_sample_does_not_see_forbidden_values():
+    r = np.random.default_rng(2)
+    x = torch.from_numpy(r.normal(0, 3, (4, 3001))).float().to(DEV)
+    words, keep = mask(4, 3001, 5, (0.3, 0.01, 0.0, 0.9))
+    want = psc.sample(x, 30, bitmask=words)
+    for bad in (math.nan, math.inf, -math.inf, 3e38):
+        y = torch.where(torch.from_numpy(keep).to(DEV), x, torch.tensor(bad, device=DEV))
+        assert all(torch.equal(a, b) for a, b in zip(psc.sample(y, 30, bitmask=words), want))
+
+
+def test_sample_draws_in_proportion():
+    """100,000 draws from five tokens: each share within five standard deviations."""
+    n, p = 50000, np.array([0.4, 0.3, 0.2, 0.07, 0.03])
+    x = torch.full((n, 40), -math.inf, device=DEV)
+    x[:, 10:15] = torch.from_numpy(np.log(p)).float().to(DEV)
+    noise = torch.empty(n, 8, device=DEV).exponential_(generator=torch.Generator(DEV).manual_seed(4))
+    tokens = psc.sample(x, 8, noise=noise)[0].cpu().numpy()
+    share = np.array([(tokens == 10 + i).mean() for i in range(5)])
+    assert share.sum() == 1 and (np.abs(share - p) < 5 * np.sqrt(p * (1 - p) / n)).all()
+
+
+# ---------------------------------------------------------------- streams and graphs
+
+def test_operators_on_another_stream_and_in_a_graph():
+    x, w, scales, bias, _, _ = head_case(24, 512, 5000, "bf16", 11)
+    words, _ = mask(24, 5000, 1, (0.9, 0.02, 0.0))
+    r = np.random.default_rng(5)
+    history = torch.from_numpy(r.integers(0, 5000, (24, 90)).astype(np.int32)).to(DEV)
+    lens, f = torch.full((24,), 80, dtype=torch.int32, device=DEV), torch.full((24,), 1.3, device=DEV)
+    noise = torch.from_numpy(r.exponential(1, (24, 16)).astype(np.float32)).to(DEV)
+
+    def step(stream=None):
+        y = psc.head_logits(x, w, scales, bias=bias, bitmask=words, stream=stream)
+        psc.penalize(y, history, lens, repetition=f, presence=f, stream=stream)
+        return (y, *psc.sample(y, 16, bitmask=words, temperature=f, noise=noise, stream=stream))
+
+    want = [t.clone() for t in step()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = step(side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for k in range(4):
+        x.copy_(torch.randn(24, 512, generator=torch.Generator().manual_seed(k)))
+        graph.replay()
+        torch.cuda.synchronize()
+        again = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, again)), k
