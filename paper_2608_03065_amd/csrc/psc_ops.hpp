@@ -22,6 +22,44 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p, uint3
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int32_t)bytes, 0x00020000);
 }
 
+// The value of another lane, moved by a DPP control into the rows of kRowMask;
+// `none` where there is no such lane.
+template <int kCtrl, int kRowMask, class T>
+__device__ __forceinline__ T dpp_from(T v, T none) {
+    static_assert(sizeof(T) == 4, "one register");
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, v), kCtrl,
+                                                             kRowMask, 0xF, false));
+}
+
+// op over the lanes up to this one, in a fixed order; `none` is op's neutral
+// element.  Shifts by 1, 2, 4 and 8 within rows of 16 lanes, then lane 15 into
+// the rows after its own pair's first (row_bcast:15) and lane 31 into the
+// upper half.  Every lane of the wavefront takes part.
+template <class T, class Op>
+__device__ __forceinline__ T wave_scan(T v, T none, const Op &op) {
+    v = op(v, dpp_from<0x111, 0xF>(v, none));
+    v = op(v, dpp_from<0x112, 0xF>(v, none));
+    v = op(v, dpp_from<0x114, 0xF>(v, none));
+    v = op(v, dpp_from<0x118, 0xF>(v, none));
+    v = op(v, dpp_from<0x142, 0xA>(v, none));
+    return op(v, dpp_from<0x143, 0xC>(v, none));
+}
+
+template <class T>
+__device__ __forceinline__ T lane_value(T v, int lane) {      // `lane` is uniform
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+}
+
+// op over the wavefront's lanes, uniform.
+template <class T, class Op>
+__device__ __forceinline__ T wave_all(T v, T none, const Op &op) {
+    return lane_value(wave_scan(v, none, op), kWave - 1);
+}
+
+constexpr auto kAdd = [](auto a, auto b) { return a + b; };
+constexpr auto kMax = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
+constexpr auto kMin = [](uint32_t a, uint32_t b) { return a < b ? a : b; };
+
 // Logits are float32 or bfloat16; the arithmetic on them is float32.
 template <bool kBf16>
 struct Logit {

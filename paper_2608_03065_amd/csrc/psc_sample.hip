@@ -3,12 +3,12 @@
 // one token drawn from these under temperature, top-k, top-p and min-p.
 //
 // Two kernels.  The scan reads every allowed logit once and leaves, per 4 KB of
-// a row, its maximum and the sum of exponentials below it, and per 128-byte
-// line the line's maximum.  The k best tokens lie in the k lines with the
-// largest maxima (ties to the lower line): any token outside them is preceded
-// by those lines' k maxima, which are larger, or equal and of lower id.  So the
-// second kernel, a workgroup per row, selects k lines, reads them again,
-// selects k of their tokens, orders them and draws.
+// a row, its maximum and the sum of exponentials below it, and per group of 64
+// tokens the group's maximum.  The k best tokens lie in the k groups with the
+// largest maxima (ties to the lower group): any token outside them is preceded
+// by those groups' k maxima, which are larger, or equal and of lower id.  So
+// the second kernel, a workgroup per row, selects groups that hold these k,
+// reads them again, orders their best tokens and draws.
 #include "psc_ops.hpp"
 
 #include <algorithm>
@@ -21,7 +21,7 @@ namespace {
 constexpr int kScanBlock = 256;
 constexpr int kTileBytes = 4096;
 constexpr int kLineBytes = 128;
-constexpr int kTileLines = kTileBytes / kLineBytes;
+constexpr int kGroup = 64;                          // tokens per group
 constexpr int kVecs = kTileBytes / 16 / kWave;      // 16-byte vectors per lane
 constexpr uint32_t kOffSkip = 0x80000000u;
 constexpr int kMostK = kWave;
@@ -33,7 +33,7 @@ struct SampleArgs {
     int32_t V, W, k, tiles;
     const float *temperature, *top_p, *min_p, *noise;
     const int32_t *top_k;
-    uint32_t *line_keys;         // [B][tiles * kTileLines]
+    uint32_t *group_keys;        // [B][tiles * Row::kTileGroups]
     float2 *parts;               // [B][tiles] (maximum, sum)
     int32_t *tokens, *ids;
     float *logprobs, *id_logprobs;
@@ -67,16 +67,14 @@ __device__ __forceinline__ float exp_scaled(float x, float c) { return __builtin
 // The larger of two floats; a NaN wins.
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
-template <int kCtrl>
-__device__ __forceinline__ float dpp(float v) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kCtrl, 0xF, 0xF, false));
-}
+constexpr auto kLarger = [](float a, float b) { return larger(a, b); };
 
 // Row b: `line` is the 128-byte line that holds its first element, the delta
 // elements before it there are not the row's.
 template <bool kBf16>
 struct Row {
     static constexpr int kElem = kBf16 ? 2 : 4, kPerVec = 16 / kElem;
+    static constexpr int kTileGroups = kTileBytes / (kGroup * kElem), kGroupLanes = kGroup / kPerVec;
     const char *line;
     int32_t delta;
     __device__ __forceinline__ Row(const SampleArgs &a, int64_t b) {
@@ -87,16 +85,16 @@ struct Row {
 };
 
 // Bits of the `count` tokens from v on (v may be negative): 1 where a token
-// is in the vocabulary and allowed.
+// is in the vocabulary and allowed.  Without branches, so that the words' loads
+// overlap what else is loaded.
 __device__ __forceinline__ uint32_t allowed_bits(const uint32_t *__restrict__ words, int64_t v, int count, int32_t V, int32_t W) {
     uint32_t in = (1u << count) - 1;
     if (v < 0) in = v > -count ? in & ~0u << -v : 0;
     if (v + count > V) in = v < V ? in & ((1u << (V - v)) - 1) : 0;
-    if (!words || !in) return in;
-    const int64_t w = v >> 5;
-    const int shift = (int)(v & 31);
-    const uint32_t lo = w >= 0 && w < W ? words[w] : 0, hi = shift + count > 32 && w + 1 >= 0 && w + 1 < W ? words[w + 1] : 0;
-    return __builtin_amdgcn_alignbit(hi, lo, shift) & in;
+    if (!words) return in;
+    const int32_t w = (int32_t)(v >> 5), last = W - 1;
+    const uint32_t lo = words[min(max(w, 0), last)], hi = words[min(max(w + 1, 0), last)];
+    return __builtin_amdgcn_alignbit(hi, lo, (uint32_t)v & 31) & in;
 }
 
 template <bool kBf16>
@@ -145,21 +143,21 @@ scan_kernel(const SampleArgs a) {
         return (keep[j] >> e) & 1 ? __builtin_bit_cast(float, u) : kMinusInf;
     };
     float most = kMinusInf;
-    uint32_t *keys = a.line_keys + (b * a.tiles + t) * kTileLines;
+    uint32_t *keys = a.group_keys + (b * a.tiles + t) * R::kTileGroups;
 #pragma unroll
     for (int j = 0; j < kVecs; j++) {
         float m = kMinusInf;
 #pragma unroll
         for (int e = 0; e < R::kPerVec; e++) m = larger(m, value(j, e));
-        // over the 8 lanes that hold a line
-        m = larger(m, dpp<0xB1>(m));     // quad_perm [1,0,3,2]
-        m = larger(m, dpp<0x4E>(m));     // quad_perm [2,3,0,1]
-        m = larger(m, dpp<0x141>(m));    // row_half_mirror
-        if (lane % 8 == 0) keys[j * 8 + lane / 8] = key_of(m);
+        // over the 8 or 16 lanes that hold a group
+        m = larger(m, dpp_from<0xB1, 0xF>(m, m));     // quad_perm [1,0,3,2]
+        m = larger(m, dpp_from<0x4E, 0xF>(m, m));     // quad_perm [2,3,0,1]
+        m = larger(m, dpp_from<0x141, 0xF>(m, m));    // row_half_mirror
+        if (!kBf16) m = larger(m, dpp_from<0x140, 0xF>(m, m));    // row_mirror
+        if (lane % R::kGroupLanes == 0) keys[(j * kWave + lane) / R::kGroupLanes] = key_of(m);
         most = larger(most, m);
     }
-#pragma unroll
-    for (int o = 8; o < kWave; o *= 2) most = larger(most, __shfl_xor(most, o, kWave));
+    most = wave_all(most, kMinusInf, kLarger);
     float sum = 0;
     if (most > kMinusInf || most != most) {
 #pragma unroll
@@ -167,116 +165,185 @@ scan_kernel(const SampleArgs a) {
 #pragma unroll
             for (int e = 0; e < R::kPerVec; e++) sum += exp_scaled(value(j, e) - most, c);
     }
-#pragma unroll
-    for (int o = 1; o < kWave; o *= 2) sum += __shfl_xor(sum, o, kWave);
+    sum = wave_all(sum, 0.0f, kAdd);
     if (lane == 0) a.parts[b * a.tiles + t] = make_float2(most, sum);
 }
 
 // ---------------------------------------------------------------- selection
 
-constexpr int kPickBlock = 1024;
+constexpr int kPickBlock = 256;
 constexpr int kPickWaves = kPickBlock / kWave;
-constexpr int kBins = kPickBlock;
+constexpr int kBinsEach = 4, kBins = kPickBlock * kBinsEach;
+constexpr int kMostGroups = 128;
+constexpr int kMostFound = kPickBlock;                    // a multiple of 16
 
 struct PickShared {
-    uint32_t bins[kBins];
+    __align__(16) uint32_t bins[kBins];
     uint32_t waves[kPickWaves];
-    uint32_t least, most, bin, above, in_bin;
-    int32_t lines[kMostK];
-    uint32_t keys[kMostK];
-    int32_t ids[kMostK];
-    float2 part;
+    float2 parts[kPickWaves];
+    uint32_t least[kPickWaves], most[kPickWaves];
+    uint32_t lo, hi, count, bin, above, in_bin, n_groups, n_found;
+    int32_t groups[kMostGroups];
+    __align__(16) uint64_t found[kMostFound];
+    uint64_t best[kMostK];
 };
 
-__device__ __forceinline__ uint32_t wave_inclusive(uint32_t v, int lane) {
-#pragma unroll
-    for (int o = 1; o < kWave; o *= 2) {
-        const uint32_t u = __shfl_up(v, o, kWave);
-        if (lane >= o) v += u;
-    }
-    return v;
-}
+// Larger for a larger key, and of equal keys for the lower token.
+__device__ __forceinline__ uint64_t ranked(uint32_t key, int32_t id) { return (uint64_t)key << 32 | ~(uint32_t)id; }
 
 // The sum of v over the threads before this one.  Every thread calls it.
 __device__ __forceinline__ uint32_t block_before(uint32_t v, PickShared &s) {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const uint32_t upto = wave_inclusive(v, lane);
-    __syncthreads();
+    const uint32_t upto = wave_scan(v, 0u, kAdd);
     if (lane == kWave - 1) s.waves[wave] = upto;
     __syncthreads();
     uint32_t before = upto - v;
-    for (int i = 0; i < wave; i++) before += s.waves[i];
+#pragma unroll
+    for (int i = 0; i < kPickWaves; i++) before += i < wave ? s.waves[i] : 0;
     return before;
 }
 
-// Of the workgroup's non-zero keys (n of them per thread): a threshold t and
-// the number `above` of keys > t such that the k largest are those above t and
-// k - above of those equal to t (or all of them, if there are fewer than k:
-// t = 0).  Histograms of the keys between two bounds, which close in on the
-// k-th largest key by a factor of kBins a round.
+// One round of the search for the k-th largest of the workgroup's keys, of
+// which more than k lie in [lo, hi] or above: a histogram of the keys in [lo,
+// hi] over equal bins.  [lo, hi] becomes the bin in which the number of keys
+// from the top reaches k; `above` keys are larger, in_bin lie in it.
+// bins are zero before and after.
 template <int kPer>
-__device__ __forceinline__ uint32_t kth_key(const uint32_t (&key)[kPer], uint32_t k, PickShared &s, uint32_t &above) {
-    uint32_t lo = 1, hi = 0;
-    uint32_t count = 0;
-    {
-        uint32_t most = 0, least = ~0u;
+__device__ __forceinline__ void narrow(const uint32_t (&key)[kPer], uint32_t k, PickShared &s, uint32_t &lo, uint32_t &hi,
+                                       uint32_t &above, uint32_t &in_bin) {
+    const uint32_t range = hi - lo;
+    const int shift = range < kBins ? 0 : 32 - __builtin_clz(range) - 10;
+    static_assert(kBins == 1 << 10, "range >> shift < kBins");
 #pragma unroll
-        for (int i = 0; i < kPer; i++) {
-            most = max(most, key[i]);
-            if (key[i]) least = min(least, key[i]), count++;
-        }
-        if (threadIdx.x == 0) s.most = 0, s.least = ~0u, s.in_bin = 0;
-        __syncthreads();
+    for (int i = 0; i < kPer; i++)
+        if (key[i] >= lo && key[i] <= hi) atomicAdd(&s.bins[(hi - key[i]) >> shift], 1u);
+    __syncthreads();
+    static_assert(kBinsEach == 4, "a vector of a thread's bins");
+    u32x4 &bins = reinterpret_cast<u32x4 *>(s.bins)[threadIdx.x];
+    const u32x4 mine = bins;
+    bins = u32x4{};
+    uint32_t before = above + block_before(mine.x + mine.y + mine.z + mine.w, s);
 #pragma unroll
-        for (int o = 1; o < kWave; o *= 2) {
-            most = max(most, (uint32_t)__shfl_xor((int)most, o, kWave));
-            least = min(least, (uint32_t)__shfl_xor((int)least, o, kWave));
-            count += __shfl_xor(count, o, kWave);
+    for (int i = 0; i < kBinsEach; i++) {
+        if (before < k && before + mine[i] >= k) {
+            s.bin = threadIdx.x * kBinsEach + i;
+            s.above = before;
+            s.in_bin = mine[i];
         }
-        if (threadIdx.x % kWave == 0 && count) {
-            atomicMax(&s.most, most);
-            atomicMin(&s.least, least);
-            atomicAdd(&s.in_bin, count);
-        }
-        __syncthreads();
-        lo = s.least;
-        hi = s.most;
-        count = s.in_bin;
+        before += mine[i];
     }
-    above = 0;
-    if (count <= k) return 0;
-    // the k - above largest keys in [lo, hi] are wanted, of more than there are
-    for (;;) {
-        if (lo == hi) return lo;
-        const uint32_t range = hi - lo;
-        int shift = 0;
-        while ((range >> shift) >= kBins) shift++;
-        __syncthreads();
-        s.bins[threadIdx.x] = 0;
-        __syncthreads();
+    __syncthreads();
+    above = s.above;
+    in_bin = s.in_bin;
+    hi -= s.bin << shift;
+    const uint32_t span = (1u << shift) - 1;
+    lo = hi - lo > span ? hi - span : lo;
+    __syncthreads();
+}
+
+// Of the workgroup's non-zero keys: a threshold t and the number `above` of
+// keys > t such that the k largest are those and k - above of the keys equal to
+// t.  t = 0 if there are no more than k.
+template <int kPer>
+__device__ uint32_t kth_key(const uint32_t (&key)[kPer], uint32_t k, PickShared &s, uint32_t &above) {
+    uint32_t most = 0, least = ~0u, count = 0;
 #pragma unroll
-        for (int i = 0; i < kPer; i++)
-            if (key[i] >= lo && key[i] <= hi) atomicAdd(&s.bins[(hi - key[i]) >> shift], 1u);
-        __syncthreads();
-        const uint32_t mine = s.bins[threadIdx.x];
-        const uint32_t before = block_before(mine, s);
-        if (above + before < k && above + before + mine >= k) {
-            s.bin = threadIdx.x;
-            s.above = above + before;
-            s.in_bin = mine;
-        }
-        __syncthreads();
-        above = s.above;
-        const uint32_t in_bin = s.in_bin, bin = s.bin;
-        const uint32_t top = hi - (bin << shift);
-        const uint32_t span = (1u << shift) - 1;
-        lo = max(lo, top - min(span, top));
-        hi = top;
-        if (above + in_bin == k) {      // the whole bin is wanted
+    for (int i = 0; i < kPer; i++) {
+        most = max(most, key[i]);
+        if (key[i]) least = min(least, key[i]), count++;
+    }
+    __syncthreads();
+    reinterpret_cast<u32x4 *>(s.bins)[threadIdx.x] = u32x4{};
+    if (threadIdx.x == 0) s.hi = 0, s.lo = ~0u, s.count = 0;
+    __syncthreads();
+    atomicMax(&s.hi, most);
+    atomicMin(&s.lo, least);
+    atomicAdd(&s.count, count);
+    __syncthreads();
+    uint32_t lo = s.lo, hi = s.hi, in_bin = 0;
+    above = 0;
+    if (s.count <= k) return 0;
+    while (lo != hi) {
+        narrow<kPer>(key, k, s, lo, hi, above, in_bin);
+        if (above + in_bin == k) {
             above = k;
             return lo - 1;
         }
     }
+    return lo;
+}
+
+// Exactly the k best tokens into s.found, whatever the row: the k groups, then
+// k of their tokens, ties to the lower ones.  Groups and tokens are dealt to
+// the threads in ascending order, so that a sum over the threads before this
+// one is a place in that order.
+template <bool kBf16, int kPer>
+__device__ __attribute__((noinline)) void pick_exactly(const SampleArgs &a, int64_t b, PickShared &s) {
+    using R = Row<kBf16>;
+    const int tid = threadIdx.x;
+    const uint32_t k = (uint32_t)a.k;
+    const int32_t groups = a.tiles * R::kTileGroups;
+    uint32_t key[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; i++) {
+        const int32_t l = tid * kPer + i;
+        key[i] = l < groups ? a.group_keys[b * groups + l] : 0;
+    }
+    s.found[tid] = 0;
+    uint32_t above;
+    uint32_t t = kth_key<kPer>(key, k, s, above);
+    uint32_t n = 0;      // those above t, and, << 16, those equal to it
+#pragma unroll
+    for (int i = 0; i < kPer; i++) n += key[i] > t ? 1u : key[i] == t && t ? 1u << 16 : 0u;
+    __syncthreads();
+    uint32_t before = block_before(n, s);
+    uint32_t gt = before & 0xFFFF, eq = before >> 16, quota = k - above;
+#pragma unroll
+    for (int i = 0; i < kPer; i++) {
+        const bool more = key[i] > t, same = key[i] == t && t;
+        if (more || (same && eq < quota)) s.groups[gt + min(eq, quota)] = tid * kPer + i;
+        gt += more;
+        eq += same;
+    }
+    if (tid == kPickBlock - 1) s.n_groups = gt + min(eq, quota);
+    __syncthreads();
+    constexpr int kMine = kMostK * kGroup / kPickBlock;
+    uint32_t mine[kMine] = {};
+    int64_t v = 0;
+    const uint32_t g = (uint32_t)tid / (kGroup / kMine);
+    if (g < s.n_groups) {
+        const R row(a, b);
+        const int64_t at = (int64_t)s.groups[g] * kGroup + (tid % (kGroup / kMine)) * kMine;
+        v = at - row.delta;
+        const uint32_t keep = allowed_bits(a.bitmask ? a.bitmask + b * a.W : nullptr, v, kMine, a.V, a.W);
+#pragma unroll
+        for (int e = 0; e < kMine; e++)
+            if ((keep >> e) & 1) mine[e] = key_of(load_logit<kBf16>(row.line, at + e));
+    }
+    t = kth_key<kMine>(mine, k, s, above);
+    n = 0;
+#pragma unroll
+    for (int e = 0; e < kMine; e++) n += mine[e] > t ? 1u : mine[e] == t && t ? 1u << 16 : 0u;
+    __syncthreads();
+    before = block_before(n, s);
+    gt = before & 0xFFFF, eq = before >> 16, quota = k - above;
+#pragma unroll
+    for (int e = 0; e < kMine; e++) {
+        const bool more = mine[e] > t, same = mine[e] == t && t;
+        if (more || (same && eq < quota)) s.found[gt + min(eq, quota)] = ranked(mine[e], (int32_t)(v + e));
+        gt += more;
+        eq += same;
+    }
+    if (tid == kPickBlock - 1) s.n_found = gt + min(eq, quota);
+    __syncthreads();
+}
+
+// Places for each lane's n entries in a list of *count so far: the first of them.
+__device__ __forceinline__ uint32_t reserve(uint32_t *count, uint32_t n, int lane) {
+    const uint32_t upto = wave_scan(n, 0u, kAdd), all = lane_value(upto, kWave - 1);
+    uint32_t at = 0;
+    if (all && lane == 0) at = atomicAdd(count, all);
+    return lane_value(at, 0) + upto - n;
 }
 
 template <bool kBf16, int kPer>
@@ -286,140 +353,174 @@ pick_kernel(const SampleArgs a) {
     __shared__ PickShared s;
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     const int64_t b = blockIdx.x;
-    const float c = inverse_temperature(a.temperature, b);
-    const int32_t lines = a.tiles * kTileLines;
-    // the row's maximum and sum
-    float most = kMinusInf, sum = 0;
-    for (int32_t t = tid; t < a.tiles; t += kPickBlock) {
-        const float2 p = a.parts[b * a.tiles + t];
-        const float m = larger(most, p.x);
-        if (m > kMinusInf || m != m) sum = sum * (most > kMinusInf ? exp_scaled(most - m, c) : 0.0f) + (p.x > kMinusInf || p.x != p.x ? p.y * exp_scaled(p.x - m, c) : 0.0f);
-        most = m;
-    }
-    // in a fixed order, so that the same row gives the same sum
-    __shared__ float2 s_parts[kPickWaves];
-#pragma unroll
-    for (int o = 1; o < kWave; o *= 2) {
-        const float m2 = __shfl_xor(most, o, kWave), s2 = __shfl_xor(sum, o, kWave);
-        const float m = larger(most, m2);
-        const float f = most > kMinusInf || most != most ? exp_scaled(most - m, c) * sum : 0.0f;
-        const float g = m2 > kMinusInf || m2 != m2 ? exp_scaled(m2 - m, c) * s2 : 0.0f;
-        sum = f + g;
-        most = m;
-    }
-    if (lane == 0) s_parts[wave] = make_float2(most, sum);
-    __syncthreads();
-    most = kMinusInf;
-    for (int i = 0; i < kPickWaves; i++) most = larger(most, s_parts[i].x);
-    sum = 0;
-    for (int i = 0; i < kPickWaves; i++)
-        if (s_parts[i].x > kMinusInf || s_parts[i].x != s_parts[i].x) sum += s_parts[i].y * exp_scaled(s_parts[i].x - most, c);
-
-    // the k lines, in ascending order
-    const uint32_t *line_keys = a.line_keys + b * lines;
+    const uint32_t k = (uint32_t)a.k;
+    const int32_t groups = a.tiles * R::kTileGroups;
     uint32_t key[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; i++) {
-        const int32_t l = tid * kPer + i;
-        key[i] = l < lines ? line_keys[l] : 0;
+        const int32_t l = i * kPickBlock + tid;
+        key[i] = l < groups ? a.group_keys[b * groups + l] : 0;
     }
-    const uint32_t k = (uint32_t)a.k;
-    uint32_t above;
-    uint32_t t = kth_key<kPer>(key, k, s, above);
-    uint32_t n = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; i++) n += key[i] > t ? 1u : key[i] == t && t ? 1u << 16 : 0u;
-    uint32_t before = block_before(n, s);
-    uint32_t n_lines;
-    {
-        uint32_t gt = before & 0xFFFF, eq = before >> 16;
-        const uint32_t quota = k - above;
-#pragma unroll
-        for (int i = 0; i < kPer; i++) {
-            const bool more = key[i] > t, same = key[i] == t && t;
-            if (more || (same && eq < quota)) s.lines[gt + min(eq, quota)] = tid * kPer + i;
-            gt += more;
-            eq += same;
-        }
-        if (tid == kPickBlock - 1) s.in_bin = gt + min(eq, quota);
-        __syncthreads();
-        n_lines = s.in_bin;
-    }
-    // their tokens: 8 bytes a thread, 16 threads a line
-    constexpr int kMine = 8 / R::kElem;
-    uint32_t mine[kMine] = {};
-    int64_t v = 0;
-    if ((uint32_t)tid / 16 < n_lines) {
-        const R row(a, b);
-        const int64_t at = (int64_t)s.lines[tid / 16] * (kLineBytes / R::kElem) + (tid % 16) * kMine;
-        v = at - row.delta;
-        const uint32_t keep = allowed_bits(a.bitmask ? a.bitmask + b * a.W : nullptr, v, kMine, a.V, a.W);
-        const char *from = row.line + at * R::kElem;
-#pragma unroll
-        for (int e = 0; e < kMine; e++)
-            if ((keep >> e) & 1) mine[e] = key_of(load_logit<kBf16>(from, e));
-    }
-    t = kth_key<kMine>(mine, k, s, above);
-    n = 0;
-#pragma unroll
-    for (int e = 0; e < kMine; e++) n += mine[e] > t ? 1u : mine[e] == t && t ? 1u << 16 : 0u;
-    before = block_before(n, s);
-    {
-        uint32_t gt = before & 0xFFFF, eq = before >> 16;
-        const uint32_t quota = k - above;
-#pragma unroll
-        for (int e = 0; e < kMine; e++) {
-            const bool more = mine[e] > t, same = mine[e] == t && t;
-            if (more || (same && eq < quota)) {
-                s.keys[gt + min(eq, quota)] = mine[e];
-                s.ids[gt + min(eq, quota)] = (int32_t)(v + e);
-            }
-            gt += more;
-            eq += same;
-        }
-        if (tid == kPickBlock - 1) s.in_bin = gt + min(eq, quota);
-        __syncthreads();
-    }
-    if (wave) return;
-    // one wavefront: lane j takes the j-th best
-    const uint32_t live = s.in_bin;
-    const uint32_t my_key = (uint32_t)lane < live ? s.keys[lane] : 0;
-    const int32_t my_id = (uint32_t)lane < live ? s.ids[lane] : -1;
-    int rank = 0;
-    for (int j = 0; j < (int)live; j++) {
-        const uint32_t other = (uint32_t)__builtin_amdgcn_readlane((int)my_key, j);
-        rank += other > my_key || (other == my_key && j < lane);
-    }
-    // the lanes past the live ones keep their places behind them
-    if ((uint32_t)lane >= live) rank = lane;
-    const uint32_t best_key = (uint32_t)__builtin_amdgcn_ds_permute(rank * 4, (int)my_key);
-    const int32_t id = __builtin_amdgcn_ds_permute(rank * 4, my_id);
-    const bool is = (uint32_t)lane < live;
-    const float x = of_key(best_key), x0 = __shfl(x, 0, kWave);
-    const float z = is ? (x - x0) * c : kMinusInf;
-    const float logprob = is ? z - __builtin_logf(sum) : kMinusInf;
+    // what the first wavefront needs at the end is on its way from the start
+    const float c = inverse_temperature(a.temperature, b);
+    const bool cold = a.temperature && !(a.temperature[b] > 0);
     const int32_t top_k = a.top_k ? a.top_k[b] : 0;
+    const float top_p = a.top_p ? a.top_p[b] : 1.0f, min_p = a.min_p ? a.min_p[b] : 0.0f;
+    const float noise = wave == 0 && lane < a.k && a.noise ? a.noise[b * a.k + lane] : 1.0f;
+    // the row's maximum and sum: tile t by thread t, and on
+    float2 part = make_float2(kMinusInf, 0.0f);
+    for (int32_t t = tid; t < a.tiles; t += kPickBlock) {
+        const float2 p = a.parts[b * a.tiles + t];
+        const float m = larger(part.x, p.x);
+        if (m != kMinusInf)
+            part.y = (part.x == kMinusInf ? 0.0f : part.y * exp_scaled(part.x - m, c)) +
+                     (p.x == kMinusInf ? 0.0f : p.y * exp_scaled(p.x - m, c));
+        part.x = m;
+    }
+    reinterpret_cast<u32x4 *>(s.bins)[tid] = u32x4{};
+    s.found[tid] = 0;
+    if (tid == 0) s.n_groups = s.n_found = 0, s.bin = kBins - 1, s.above = 0, s.in_bin = 0;
+    // Every lane of a wavefront has a key that is at least the wavefront's
+    // least lane maximum: kMostK keys lie at or above it.
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; i++) most = max(most, key[i]);
+    const uint32_t least = wave_all(most, ~0u, kMin);
+    most = wave_all(most, 0u, kMax);
+    const float top = wave_all(part.x, kMinusInf, kLarger);
+    const float sum_here = wave_all(part.x == kMinusInf ? 0.0f : part.y * exp_scaled(part.x - top, c), 0.0f, kAdd);
+    if (lane == 0) {
+        s.parts[wave] = make_float2(top, sum_here);
+        s.most[wave] = most;
+        s.least[wave] = least;
+    }
+    __syncthreads();
+    uint32_t lo = 1, hi = 0;
+#pragma unroll
+    for (int i = 0; i < kPickWaves; i++) {
+        hi = max(hi, s.most[i]);
+        lo = max(lo, s.least[i]);
+    }
+    const bool some = hi != 0;
+    uint32_t above = 0, in_bin = 0;
+    // One round leaves little more than k groups, unless many maxima are equal
+    // or nearly so.  Where a row has fewer than k, all of them are taken.
+    if (some) {
+        narrow<kPer>(key, k, s, lo, hi, above, in_bin);
+        if (!in_bin) lo = 1;
+    }
+    {
+        uint64_t hits = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; i++) hits |= (uint64_t)(some && key[i] >= lo) << i;
+        uint32_t to = reserve(&s.n_groups, __popcll(hits), lane);
+        for (; hits; hits &= hits - 1, to++)
+            if (to < kMostGroups) s.groups[to] = (__ffsll((long long)hits) - 1) * kPickBlock + tid;
+    }
+    __syncthreads();
+    const uint32_t n_groups = s.n_groups;
+    // their tokens, kMine at a time; every load is under way before the first is used
+    constexpr int kMine = 8, kParts = kGroup / kMine, kTurns = kMostGroups * kParts / kPickBlock;
+    if (n_groups <= kMostGroups) {
+        const R row(a, b);
+        const uint32_t *words = a.bitmask ? a.bitmask + b * a.W : nullptr;
+        constexpr int kVecsMine = kMine / R::kPerVec;
+        const __amdgpu_buffer_rsrc_t rsrc = buffer_of(row.line, (uint32_t)a.tiles * kTileBytes);
+        u32x4 x[kTurns][kVecsMine];
+        uint32_t keep[kTurns];
+        int32_t first[kTurns];       // of the tokens, in the row
+        bool ends = false;
+#pragma unroll
+        for (int i = 0; i < kTurns; i++) {
+            const int n = i * kPickBlock + tid;
+            const bool mine = (uint32_t)n / kParts < n_groups;
+            const int32_t at = mine ? s.groups[n / kParts] * kGroup + n % kParts * kMine : 0;
+            first[i] = mine ? at - row.delta : a.V;
+            const bool whole = first[i] >= 0 && first[i] <= a.V - kMine;
+            ends |= !whole && first[i] < a.V;
+#pragma unroll
+            for (int j = 0; j < kVecsMine; j++)
+                x[i][j] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, whole ? (uint32_t)at * R::kElem + 16 * j : kOffSkip, 0, 0);
+            keep[i] = allowed_bits(words, first[i], kMine, a.V, a.W);
+        }
+        if (__ballot(ends)) {        // what reaches out of the row is read by element
+#pragma unroll
+            for (int i = 0; i < kTurns; i++) {
+                if (first[i] >= a.V || (first[i] >= 0 && first[i] <= a.V - kMine)) continue;
+                const char *from = row.line + ((int64_t)first[i] + row.delta) * R::kElem;
+#pragma unroll
+                for (int e = 0; e < kMine; e++) {
+                    if (!((keep[i] >> e) & 1)) continue;
+                    if constexpr (kBf16) x[i][0][e / 2] |= (uint32_t) reinterpret_cast<const uint16_t *>(from)[e] << (e % 2 * 16);
+                    else x[i][e / 4][e % 4] = reinterpret_cast<const uint32_t *>(from)[e];
+                }
+            }
+        }
+        // a bit per token that is not below the threshold (a NaN is not)
+        const float least_value = lo < 0x00800000u ? -FLT_MAX : of_key(lo);
+        uint32_t hits = 0;
+        static_assert(kTurns * kMine <= 32, "a bit per token of a thread");
+#pragma unroll
+        for (int i = 0; i < kTurns; i++) {
+#pragma unroll
+            for (int e = 0; e < kMine; e++) {
+                const uint32_t u = kBf16 ? (e % 2 ? x[i][0][e / 2] & 0xFFFF0000u : x[i][0][e / 2] << 16) : x[i][e / 4 % kVecsMine][e % 4];
+                hits |= (uint32_t)!(__builtin_bit_cast(float, u) < least_value) << (i * kMine + e);
+            }
+            hits &= ~(((1u << kMine) - 1) << (i * kMine)) | keep[i] << (i * kMine);
+        }
+        // few are: those are read again rather than picked out of registers,
+        // for the code's length is time where a launch runs it once
+        uint32_t to = reserve(&s.n_found, __popc(hits), lane);
+        for (; hits; hits &= hits - 1, to++) {
+            const int bit = __ffs((int)hits) - 1, i = bit / kMine;
+            const int32_t v = (i < 2 ? i < 1 ? first[0] : first[1] : i < 3 ? first[2] : first[3]) + bit % kMine;
+            static_assert(kTurns == 4, "the turns named here");
+            if (to < kMostFound) s.found[to] = ranked(key_of(load_logit<kBf16>(row.line, (int64_t)v + row.delta)), v);
+        }
+    }
+    __syncthreads();
+    if (n_groups > kMostGroups || s.n_found > kMostFound) pick_exactly<kBf16, kPer>(a, b, s);
+    // the place of every token found, by counting those before it
+    const uint32_t n_found = s.n_found;
+    if ((uint32_t)tid < n_found) {
+        const uint64_t mine = s.found[tid];
+        uint32_t rank = 0;
+        constexpr int kAtOnce = 16;      // what lies behind the last one is 0
+        for (uint32_t j = 0; j < n_found; j += kAtOnce) {
+            uint64_t other[kAtOnce];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; i++) other[i] = s.found[j + i];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; i++) rank += other[i] > mine;
+        }
+        if (rank < k) s.best[rank] = mine;
+    }
+    __syncthreads();
+    if (wave) return;
+    // one wavefront: lane j has the j-th best
+    const uint32_t live = min(n_found, k);
+    const bool is = (uint32_t)lane < live;
+    const uint64_t mine = is ? s.best[lane] : 0;
+    const int32_t id = is ? (int32_t)~(uint32_t)mine : -1;
+    const float x = of_key((uint32_t)(mine >> 32)), x0 = lane_value(x, 0);
+    float sum = 0;
+#pragma unroll
+    for (int i = 0; i < kPickWaves; i++)
+        if (s.parts[i].x != kMinusInf) sum += s.parts[i].y * exp_scaled(s.parts[i].x - x0, c);
+    const float z = (x - x0) * c;
+    const float logprob = is ? z - __builtin_logf(sum) : kMinusInf;
     const bool in_top = is && (top_k <= 0 || lane < top_k);
     const float weight = in_top ? exp_scaled(x - x0, c) : 0.0f;
-    float upto = weight;
-#pragma unroll
-    for (int o = 1; o < kWave; o *= 2) {
-        const float u = __shfl_up(upto, o, kWave);
-        if (lane >= o) upto += u;
-    }
-    const float all = __shfl(upto, kWave - 1, kWave);
-    const float top_p = a.top_p ? a.top_p[b] : 1.0f, min_p = a.min_p ? a.min_p[b] : 0.0f;
+    const float upto = wave_scan(weight, 0.0f, kAdd), all = lane_value(upto, kWave - 1);
     const bool kept = weight > 0 && (top_p >= 1 || upto - weight < top_p * all || lane == 0) && (weight >= min_p || lane == 0);
-    const bool greedy = !a.noise || (a.temperature && !(a.temperature[b] > 0)) || !(sum < INFINITY);
-    float score = kept && !greedy ? weight / a.noise[b * a.k + lane] : -1.0f;
-    int at = lane;
-#pragma unroll
-    for (int o = 1; o < kWave; o *= 2) {
-        const float other = __shfl_xor(score, o, kWave);
-        const int other_at = __shfl_xor(at, o, kWave);
-        if (other > score || (other == score && other_at < at)) score = other, at = other_at;
+    int at = 0;
+    if (a.noise && !cold && sum < INFINITY) {
+        const float score = kept ? weight / noise : -1.0f;
+        const float largest = wave_all(score, -1.0f, [](float p, float q) { return fmaxf(p, q); });
+        const uint64_t where = __ballot(score == largest);
+        if (largest >= 0 && where) at = __ffsll((long long)where) - 1;
     }
-    if (greedy || !(score >= 0)) at = 0;
     if (lane == at) {
         a.tokens[b] = id;
         if (a.logprobs) a.logprobs[b] = logprob;
@@ -438,19 +539,21 @@ template <bool kBf16>
 void launch_sample(const SampleArgs &a, int32_t B, hipStream_t s) {
     constexpr int kWaves = kScanBlock / kWave;
     hipLaunchKernelGGL(scan_kernel<kBf16>, dim3((a.tiles + kWaves - 1) / kWaves, B), dim3(kScanBlock), 0, s, a);
-    const int32_t lines = a.tiles * kTileLines;
-    if (lines <= kPickBlock * 2) hipLaunchKernelGGL((pick_kernel<kBf16, 2>), dim3(B), dim3(kPickBlock), 0, s, a);
-    else if (lines <= kPickBlock * 5) hipLaunchKernelGGL((pick_kernel<kBf16, 5>), dim3(B), dim3(kPickBlock), 0, s, a);
-    else hipLaunchKernelGGL((pick_kernel<kBf16, 16>), dim3(B), dim3(kPickBlock), 0, s, a);
+    const int32_t groups = a.tiles * Row<kBf16>::kTileGroups;
+    const dim3 rows(B), block(kPickBlock);
+    if (groups <= kPickBlock * 4) hipLaunchKernelGGL((pick_kernel<kBf16, 4>), rows, block, 0, s, a);
+    else if (groups <= kPickBlock * 10) hipLaunchKernelGGL((pick_kernel<kBf16, 10>), rows, block, 0, s, a);
+    else if (groups <= kPickBlock * 20) hipLaunchKernelGGL((pick_kernel<kBf16, 20>), rows, block, 0, s, a);
+    else hipLaunchKernelGGL((pick_kernel<kBf16, 64>), rows, block, 0, s, a);
 }
 
-constexpr int32_t kMostTiles = kPickBlock * 16 / kTileLines;       // 2 MiB of logits a row
+constexpr int32_t kMostTiles = kPickBlock * 64 / Row<true>::kTileGroups;       // 2 MiB of logits a row
 
 }  // namespace
 
 extern "C" size_t psc_sample_workspace(int32_t B, int32_t V, psc_dtype dtype) {
     if (B <= 0 || V <= 0 || !is_dtype(dtype)) return 0;
-    return (size_t)B * (size_t)tiles_of(V, dtype) * (sizeof(float2) + kTileLines * sizeof(uint32_t));
+    return (size_t)B * (size_t)tiles_of(V, dtype) * (sizeof(float2) + Row<true>::kTileGroups * sizeof(uint32_t));
 }
 
 extern "C" psc_status psc_sample(const void *logits, psc_dtype dtype, int64_t stride, int32_t B, int32_t V,
@@ -483,7 +586,7 @@ extern "C" psc_status psc_sample(const void *logits, psc_dtype dtype, int64_t st
         a.noise = sampling->noise;
     }
     a.parts = static_cast<float2 *>(workspace);
-    a.line_keys = reinterpret_cast<uint32_t *>(a.parts + (size_t)B * a.tiles);
+    a.group_keys = reinterpret_cast<uint32_t *>(a.parts + (size_t)B * a.tiles);
     a.tokens = tokens;
     a.logprobs = logprobs;
     a.ids = ids;
