@@ -2,6 +2,13 @@
 // rows of int8 with one scale each on both sides, products summed exactly in
 // 32-bit integers by the matrix cores, and one epilogue that scales, adds the
 // bias, applies the grammar mask and rounds once.
+//
+// A call launches prepare_kernel (the states to 8 bits and, under a mask, the
+// list of tokens that any row allows), then the product: small_kernel for up to
+// 128 rows, wide_kernel above.  Where the mask leaves few tokens, the product
+// is taken of the listed tokens' weights only (small_kernel, `gather`).  Where there are
+// too few tiles for the GPU, D is split over workgroups; the last one of a tile
+// to end adds their sums, which are integers: any order gives the same.
 #include "psc_ops.hpp"
 
 #include <algorithm>
@@ -34,22 +41,32 @@ __device__ __forceinline__ void load_vec(const void *row, int64_t d, int32_t D, 
     }
 }
 
-// One workgroup per row; q[D .. padded) become zeros.
+// The row by one workgroup; q[D .. padded) become zeros.
 template <bool kBf16>
-__global__ void __launch_bounds__(kQuantBlock)
-quantize_kernel(const void *__restrict__ x, int64_t x_stride, int32_t D, int32_t padded, int8_t *__restrict__ q,
-                int64_t q_stride, float *__restrict__ scales) {
-    __shared__ uint32_t s_most[kQuantBlock / kWave];
-    const int64_t r = blockIdx.x;
+__device__ __forceinline__ void quantize_row(const void *__restrict__ x, int64_t x_stride, int64_t r, int32_t D, int32_t padded,
+                                             int8_t *__restrict__ q, int64_t q_stride, float *__restrict__ scales,
+                                             uint32_t *s_most) {
     const char *row = static_cast<const char *>(x) + r * x_stride * (kBf16 ? 2 : 4);
     uint32_t most = 0;            // of the absolute values' bits: a NaN's are above an infinity's
-    float v[kQuantVec];
-    for (int32_t d = threadIdx.x * kQuantVec; d < D; d += kQuantBlock * kQuantVec) {
-        load_vec<kBf16>(row, d, D, v);
+    // a row of up to kHeld elements is read once
+    constexpr int kTurns = 4, kHeld = kTurns * kQuantBlock * kQuantVec;
+    float held[kTurns][kQuantVec], v[kQuantVec];
+    const bool once = D <= kHeld;
+    if (once) {
 #pragma unroll
-        for (int k = 0; k < kQuantVec; k++) most = max(most, __builtin_bit_cast(uint32_t, v[k]) & 0x7FFFFFFFu);
+        for (int i = 0; i < kTurns; i++) load_vec<kBf16>(row, (i * kQuantBlock + (int)threadIdx.x) * kQuantVec, D, held[i]);
+#pragma unroll
+        for (int i = 0; i < kTurns; i++)
+#pragma unroll
+            for (int k = 0; k < kQuantVec; k++) most = max(most, __builtin_bit_cast(uint32_t, held[i][k]) & 0x7FFFFFFFu);
+    } else {
+        for (int32_t d = threadIdx.x * kQuantVec; d < D; d += kQuantBlock * kQuantVec) {
+            load_vec<kBf16>(row, d, D, v);
+#pragma unroll
+            for (int k = 0; k < kQuantVec; k++) most = max(most, __builtin_bit_cast(uint32_t, v[k]) & 0x7FFFFFFFu);
+        }
     }
-    for (int o = kWave / 2; o > 0; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o, kWave));
+    most = wave_all(most, 0u, kMax);
     if (threadIdx.x % kWave == 0) s_most[threadIdx.x / kWave] = most;
     __syncthreads();
 #pragma unroll
@@ -58,24 +75,50 @@ quantize_kernel(const void *__restrict__ x, int64_t x_stride, int32_t D, int32_t
     const float scale = finite ? __builtin_bit_cast(float, most) / 127.0f : __builtin_nanf("");
     if (threadIdx.x == 0) scales[r] = scale;
     int8_t *to = q + r * q_stride;
-    for (int32_t d = threadIdx.x * kQuantVec; d < padded; d += kQuantBlock * kQuantVec) {
-        load_vec<kBf16>(row, d, D, v);
+    const auto put = [&](int32_t d, const float(&f8)[kQuantVec]) {
         uint64_t out = 0;
 #pragma unroll
         for (int k = 0; k < kQuantVec; k++) {
             // past D the element is 0; a scale too small for its row's maximum (a subnormal one) is clamped
-            const float f = scale > 0 ? __builtin_rintf(v[k] / scale) : 0.0f;
+            const float f = scale > 0 ? __builtin_rintf(f8[k] / scale) : 0.0f;
             out |= (uint64_t)(uint8_t)(int8_t)(int)fminf(fmaxf(f, -127.0f), 127.0f) << (8 * k);
         }
         __builtin_memcpy(to + d, &out, sizeof out);
+    };
+    if (once) {
+#pragma unroll
+        for (int i = 0; i < kTurns; i++) {
+            const int32_t d = (i * kQuantBlock + (int)threadIdx.x) * kQuantVec;
+            if (d < padded) put(d, held[i]);
+        }
+    } else {
+        for (int32_t d = threadIdx.x * kQuantVec; d < padded; d += kQuantBlock * kQuantVec) {
+            load_vec<kBf16>(row, d, D, v);
+            put(d, v);
+        }
     }
 }
 
-// ---------------------------------------------------------------- the product
+template <bool kBf16>
+__global__ void __launch_bounds__(kQuantBlock)
+quantize_kernel(const void *__restrict__ x, int64_t x_stride, int32_t D, int32_t padded, int8_t *__restrict__ q,
+                int64_t q_stride, float *__restrict__ scales) {
+    __shared__ uint32_t s_most[kQuantBlock / kWave];
+    quantize_row<kBf16>(x, x_stride, blockIdx.x, D, padded, q, q_stride, scales, s_most);
+}
+
+// ---------------------------------------------------------------- the product's arguments
 
 constexpr int kStep = 128;        // bytes of a row per step along D: one line
 constexpr int kChunk = 16;        // bytes per lane of a load and of a matrix instruction's operand
 constexpr int kChunks = kStep / kChunk;
+constexpr uint32_t kNowhere = 0xFFFF8000u;        // an offset past any resource: the hardware drops the access
+constexpr uint32_t kMostBytes = 0xFFFF0000u;      // of a resource
+
+// The tokens that any row allows, in blocks of kBlockWords mask words: each
+// block's number of them, and their ids in ascending order.
+constexpr int kBlockWords = 64, kBlockTokens = kBlockWords * 32;
+constexpr int kMostBlocks = 512;                  // V up to 1,048,576
 
 struct HeadArgs {
     const int8_t *x;              // quantised states, rows x_stride apart, zeros from D up to whole steps
@@ -89,60 +132,320 @@ struct HeadArgs {
     int64_t y_stride;
     int32_t B, D, V, W;
     int32_t steps, m_tiles;
+    int32_t splits;               // parts of D, where all tokens are taken
+    const int32_t *counts, *ids;  // needed tokens: [blocks], [blocks][kBlockTokens]; null without a mask
+    int32_t blocks;
+    int32_t gather_most;          // most needed tokens at which only they are taken
+    int32_t units;                // workgroups there are for tiles times parts
+    int32_t *partials;            // [tiles][parts][kM * kN] sums, where D is split
+    int64_t partials_most;        // their room
+    uint32_t *arrivals;           // [tiles] parts that have ended: prepare_kernel clears them
+    int32_t arrivals_most;
 };
+
+// How a call is carried out: which columns (all tokens, or the needed ones),
+// and in how many parts of D each.  Every workgroup works it out alike.
+struct Plan {
+    bool gather;
+    int32_t columns, tiles, splits;
+};
+
+// What is read is the wavefront's; `total` as needed_total gives it.
+template <int kM, int kN>
+__device__ __forceinline__ Plan plan_of(const HeadArgs &a, int32_t total) {
+    Plan p{false, a.V, (a.V + kN - 1) / kN, a.splits};
+    if (a.counts && total <= a.gather_most) {
+        p.gather = true;
+        p.columns = total;
+        p.tiles = (total + kN - 1) / kN;
+        const int32_t tiles = max(p.tiles * a.m_tiles, 1);
+        const int64_t room = tiles > a.arrivals_most ? 1 : a.partials_most / ((int64_t)tiles * kM * kN);
+        p.splits = max(1, (int32_t)min((int64_t)min(a.units / tiles, min(a.steps / 2, 16)), room));
+    }
+    return p;
+}
+
+// Sum of the blocks' counts up to and with the lane's share of them, kShare
+// consecutive blocks a lane.
+constexpr int kShare = kMostBlocks / kWave;
+__device__ __forceinline__ int32_t needed_upto(const HeadArgs &a, int lane, int32_t (&count)[kShare]) {
+    int32_t sum = 0;
+#pragma unroll
+    for (int i = 0; i < kShare; i++) {
+        const int32_t at = lane * kShare + i;
+        count[i] = at < a.blocks ? a.counts[at] : 0;
+        sum += count[i];
+    }
+    return wave_scan(sum, 0, kAdd);
+}
+
+// ---------------------------------------------------------------- prepare
+
+// Block `block` of the needed tokens: the OR of the rows' words, by one
+// workgroup, its wavefronts over every fourth row.  Most masks allow almost all
+// tokens; as soon as a block has all of its bits, the other rows are not read.
+__device__ __forceinline__ void needed_block(const HeadArgs &a, int32_t block, int32_t *__restrict__ counts,
+                                             int32_t *__restrict__ ids, uint32_t (*s_words)[kBlockWords]) {
+    constexpr int kWaves = kQuantBlock / kWave, kAhead = 8;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int32_t w = block * kBlockWords + lane;
+    const int32_t left = a.V - w * 32;        // tokens from the word's first on
+    const uint32_t inside = left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1;
+    uint32_t any = 0;
+    for (int32_t b = wave; b < a.B; b += kWaves * kAhead) {
+        uint32_t word[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; i++) {
+            const int32_t row = b + i * kWaves;
+            word[i] = inside && row < a.B ? a.bitmask[(int64_t)row * a.W + w] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; i++) any |= word[i];
+        if (!__ballot((any & inside) != inside)) break;
+    }
+    s_words[wave][lane] = any & inside;
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int i = 1; i < kWaves; i++) any |= s_words[i][lane];
+    any &= inside;
+    const int32_t n = __popc(any), upto = wave_scan(n, 0, kAdd);
+    if (lane == kWave - 1) counts[block] = upto;
+    int32_t *to = ids + (int64_t)block * kBlockTokens + upto - n;
+    for (; any; any &= any - 1) *to++ = w * 32 + __ffs((int)any) - 1;
+}
+
+// Workgroups 0 .. B - 1: a row of states each; the others a block of needed
+// tokens each; all of them clear the arrival counters.
+template <bool kBf16>
+__global__ void __launch_bounds__(kQuantBlock)
+prepare_kernel(const HeadArgs a, const void *__restrict__ x, int64_t x_stride, int8_t *__restrict__ q,
+               float *__restrict__ scales, int32_t *__restrict__ counts, int32_t *__restrict__ ids) {
+    __shared__ uint32_t shared[kQuantBlock / kWave][kBlockWords];
+    for (int64_t i = (int64_t)blockIdx.x * kQuantBlock + threadIdx.x; i < a.arrivals_most; i += (int64_t)gridDim.x * kQuantBlock)
+        a.arrivals[i] = 0;
+    if ((int64_t)blockIdx.x < a.B) quantize_row<kBf16>(x, x_stride, blockIdx.x, a.D, (int32_t)a.x_stride, q, a.x_stride, scales, shared[0]);
+    else needed_block(a, (int32_t)(blockIdx.x - a.B), counts, ids, shared);
+}
+
+// ---------------------------------------------------------------- results
+
+// sum * xs * ws + bias, in this order, each operation rounded to float32
+__device__ __forceinline__ float scaled(int32_t sum, float xs, float ws, float bias) { return (float)sum * xs * ws + bias; }
+
+// Four consecutive logits of a row from token v on, a multiple of 4; bit e of
+// `allowed` is token v + e's.
+template <bool kBf16>
+__device__ __forceinline__ void put_four(const HeadArgs &a, int32_t b, int32_t v, const i32x4 &sum, float xs, const float (&ws)[4],
+                                         const float (&bias)[4], uint32_t allowed) {
+    using T = typename Logit<kBf16>::type;
+    T out[4];
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        const float y = (allowed >> e) & 1 ? scaled(sum[e], xs, ws[e], bias[e]) : kMinusInf;
+        if constexpr (kBf16) out[e] = to_bf16(y);
+        else out[e] = y;
+    }
+    T *to = static_cast<T *>(a.y) + (int64_t)b * a.y_stride + v;
+    if (v + 4 <= a.V) __builtin_memcpy(to, out, sizeof out);
+    else
+        for (int e = 0; e < 4; e++)
+            if (v + e < a.V) to[e] = out[e];
+}
+
+// What kTn by kTm blocks of 16 tokens by 16 states need besides their sums: all
+// of it is loaded at once, and for small_kernel before the product.  The lane's
+// tokens of block i are v + 16 i .. + 3, its state of block j is b + 16 j;
+// places past the last row or token stand for the last one.
+template <int kTn, int kTm>
+struct Factors {
+    float ws[kTn][4], bias[kTn][4], xs[kTm];
+    uint32_t allowed[kTn][kTm];
+
+    __device__ __forceinline__ void load(const HeadArgs &a, int32_t v, int32_t b) {
+#pragma unroll
+        for (int j = 0; j < kTm; j++) xs[j] = a.x_scales[min(b + j * 16, a.B - 1)];
+#pragma unroll
+        for (int i = 0; i < kTn; i++) {
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const int32_t at = min(v + i * 16 + e, a.V - 1);
+                ws[i][e] = a.w_scales[at];
+                bias[i][e] = a.bias ? a.bias[at] : 0.0f;
+            }
+            const int32_t at = min(v + i * 16, a.V - 1);
+#pragma unroll
+            for (int j = 0; j < kTm; j++)
+                allowed[i][j] = a.bitmask ? a.bitmask[(int64_t)min(b + j * 16, a.B - 1) * a.W + (at >> 5)] >> (at & 31) : 15u;
+        }
+    }
+
+    template <bool kBf16>
+    __device__ __forceinline__ void put(const HeadArgs &a, int32_t v, int32_t b, const i32x4 (&sum)[kTn][kTm]) const {
+#pragma unroll
+        for (int i = 0; i < kTn; i++)
+#pragma unroll
+            for (int j = 0; j < kTm; j++)
+                if (v + i * 16 < a.V && b + j * 16 < a.B)
+                    put_four<kBf16>(a, b + j * 16, v + i * 16, sum[i][j], xs[j], ws[i], bias[i], allowed[i][j]);
+    }
+};
+
+// One logit, if its row allows it.
+template <bool kBf16>
+__device__ __forceinline__ void put_if_allowed(const HeadArgs &a, int32_t b, int32_t v, int32_t sum, float xs, float ws, float bias) {
+    if (!((a.bitmask[(int64_t)b * a.W + (v >> 5)] >> (v & 31)) & 1)) return;
+    using T = typename Logit<kBf16>::type;
+    store_logit<kBf16>(static_cast<T *>(a.y) + (int64_t)b * a.y_stride, v, scaled(sum, xs, ws, bias));
+}
+
+// -inf in the forbidden logits and nothing else (the allowed ones are written
+// by other workgroups): piece by piece of 2,048 tokens of a row, eight of them
+// at once where they are all forbidden.
+template <bool kBf16>
+__device__ __forceinline__ void fill_forbidden(const HeadArgs &a, int64_t part, int64_t parts) {
+    using T = typename Logit<kBf16>::type;
+    const int32_t pieces = (a.V + kBlockTokens - 1) / kBlockTokens;
+    T inf[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        if constexpr (kBf16) inf[e] = 0xFF80u;
+        else inf[e] = kMinusInf;
+    }
+    for (int64_t u = part; u < (int64_t)a.B * pieces; u += parts) {
+        const int64_t b = u / pieces;
+        const int32_t v0 = (int32_t)(u - b * pieces) * kBlockTokens;
+        T *row = static_cast<T *>(a.y) + b * a.y_stride;
+        const uint32_t *words = a.bitmask + b * a.W;
+        for (int32_t v = v0 + (int32_t)threadIdx.x * 8; v < min(a.V, v0 + kBlockTokens); v += (int32_t)blockDim.x * 8) {
+            const uint32_t allowed = words[v >> 5] >> (v & 31) & 255;
+            if (allowed == 0 && v + 8 <= a.V) {
+                __builtin_memcpy(row + v, inf, sizeof inf);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    if (!((allowed >> e) & 1) && v + e < a.V) row[v + e] = inf[0];
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- up to 128 rows
 
 // Wait until at most n of the wavefront's loads are outstanding and its reads
 // of LDS are done, then for the other wavefronts of the workgroup.
 template <int n>
 __device__ __forceinline__ void wait_and_meet() {
+    static_assert(n < 64, "the counter's range");
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(n) : "memory");
 }
 
-// One workgroup computes kM states by kN tokens.  Steps of 128 bytes of all
-// its rows go straight from memory into one of kStages buffers in LDS, kStages
-// - 1 steps ahead.  A row's 16-byte chunk c lies at place c ^ (row & 7) of its
-// 128 bytes, so that the 16 rows that a matrix instruction reads at one chunk
-// fall into different banks; since a load puts lane l's chunk at place l, the
-// lane fetches the chunk that belongs there.
+// 16 bytes per lane from the resource straight to LDS: lane l's to place l from `to` on.
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t from, uint32_t offset, int8_t *to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)to, kChunk, offset, 0, 0, 0);
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const int8_t *p, int64_t bytes) {
+    return buffer_of(p, (uint32_t)min(max(bytes, (int64_t)0), (int64_t)kMostBytes));
+}
+// The weights from row `row` on; what lies behind the last row's D elements
+// (up to 16 bytes) is not touched.
+__device__ __forceinline__ int64_t weight_bytes(const HeadArgs &a, int32_t row) {
+    return (int64_t)(a.V - row - 1) * a.w_stride + (a.D + kChunk - 1) / kChunk * kChunk;
+}
+
+// One workgroup computes kM states by kN tokens over a part of D.  Steps of
+// 128 bytes of all its rows go straight from memory into one of kStages buffers
+// in LDS, kStages - 1 steps ahead.  A row's 16-byte chunk c lies at place c ^
+// (row & 7) of its 128 bytes, so that the 16 rows that a matrix instruction
+// reads at one chunk fall into different banks; since a load puts lane l's
+// chunk at place l, the lane fetches the chunk that belongs there.  What is
+// read past a row's D elements is multiplied by the states' zeros.
 template <int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kBf16>
-__global__ void __launch_bounds__(kWave * kWavesM * kWavesN)
-head_kernel(const HeadArgs a) {
+__device__ __forceinline__ void small_body(const HeadArgs &a, bool gather_only) {
     constexpr int kWaves = kWavesM * kWavesN, kRows = kM + kN;
     constexpr int kLoads = kRows * kChunks / (kWaves * kWave);
     static_assert(kLoads * kWaves * kWave == kRows * kChunks && kN % 8 == 0, "every wavefront loads as much");
     constexpr int kTm = kM / kWavesM / 16, kTn = kN / kWavesN / 16;   // 16 x 16 blocks of a wavefront
+    static_assert(kTm * kWavesM * 16 == kM && kTn * kWavesN * 16 == kN, "whole blocks");
     __shared__ __align__(1024) int8_t lds[kStages][kRows * kStep];
+    __shared__ int32_t s_ids[kN], s_before[kMostBlocks + 1];
+    __shared__ uint32_t s_arrived;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int wm = wave % kWavesM, wn = wave / kWavesM;
-    const int32_t m0 = (int32_t)(blockIdx.x % a.m_tiles) * kM, n0 = (int32_t)(blockIdx.x / a.m_tiles) * kN;
 
-    const int64_t w_bytes = (int64_t)(a.V - n0 - 1) * a.w_stride + (a.D + kChunk - 1) / kChunk * kChunk;
-    const __amdgpu_buffer_rsrc_t rw = buffer_of(a.w + (int64_t)n0 * a.w_stride, (uint32_t)min(w_bytes, (int64_t)INT32_MAX));
-    const int64_t x_bytes = (int64_t)(a.B - m0) * a.x_stride;
-    const __amdgpu_buffer_rsrc_t rx = buffer_of(a.x + (int64_t)m0 * a.x_stride, (uint32_t)min(x_bytes, (int64_t)INT32_MAX));
+    int32_t total = 0, count[kShare];
+    if (a.counts) {
+        const int32_t upto = needed_upto(a, lane, count);
+        total = lane_value(upto, kWave - 1);
+        if (total <= a.gather_most && wave == 0) {
+            int32_t before = upto;
+#pragma unroll
+            for (int i = kShare - 1; i >= 0; i--) {
+                s_before[lane * kShare + i + 1] = before;
+                before -= count[i];
+            }
+            if (lane == 0) s_before[0] = 0;
+        }
+    }
+    const Plan plan = plan_of<kM, kN>(a, total);
+    if (plan.gather) fill_forbidden<kBf16>(a, blockIdx.x, gridDim.x);
+    else if (gather_only) return;
+    const int32_t tiles = plan.tiles * a.m_tiles;
+    if ((int32_t)blockIdx.x >= tiles * plan.splits) return;
+    const int32_t split = (int32_t)blockIdx.x / tiles, tile = (int32_t)blockIdx.x - split * tiles;
+    const int32_t m0 = tile % a.m_tiles * kM, n0 = tile / a.m_tiles * kN;
+    const int32_t first = (int32_t)((int64_t)a.steps * split / plan.splits), steps = (int32_t)((int64_t)a.steps * (split + 1) / plan.splits);
+
+    if (plan.gather) {
+        // token n0 + i of the needed ones: its block by bisection of the sums before each
+        __syncthreads();
+        for (int i = threadIdx.x; i < kN; i += kWaves * kWave) {
+            int32_t id = -1;
+            if (n0 + i < plan.columns) {
+                int32_t lo = 0, hi = a.blocks;
+                while (hi - lo > 1) {
+                    const int32_t mid = (lo + hi) / 2;
+                    if (s_before[mid] <= n0 + i) lo = mid;
+                    else hi = mid;
+                }
+                id = a.ids[(int64_t)lo * kBlockTokens + n0 + i - s_before[lo]];
+            }
+            s_ids[i] = id;
+        }
+        __syncthreads();
+    }
+    const int32_t w_row = plan.gather ? 0 : n0;
+    const __amdgpu_buffer_rsrc_t rw = rows_from(a.w + (int64_t)w_row * a.w_stride, weight_bytes(a, w_row));
+    const __amdgpu_buffer_rsrc_t rx = rows_from(a.x + (int64_t)m0 * a.x_stride, (int64_t)(a.B - m0) * a.x_stride);
     uint32_t from[kLoads];
 #pragma unroll
     for (int i = 0; i < kLoads; i++) {
         const int row = (i * kWaves + wave) * 8 + lane / 8, chunk = (lane & 7) ^ (row & 7);
-        from[i] = (row < kN ? (uint32_t)row * (uint32_t)a.w_stride : (uint32_t)(row - kN) * (uint32_t)a.x_stride) + chunk * kChunk;
+        uint32_t at;
+        if (row >= kN) at = (uint32_t)(row - kN) * (uint32_t)a.x_stride;
+        else if (!plan.gather) at = (uint32_t)row * (uint32_t)a.w_stride;
+        else at = s_ids[row] >= 0 ? (uint32_t)s_ids[row] * (uint32_t)a.w_stride : kNowhere;
+        from[i] = at == kNowhere ? at : at + chunk * kChunk;
     }
-    auto fetch = [&](int32_t step) {
+    const auto fetch = [&](int32_t step) {
         int8_t *to = lds[step % kStages];
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
-            const int first = (i * kWaves + wave) * 8;
+            const int row = (i * kWaves + wave) * 8;
             // past the last step nothing is read, and the number of accesses stays the same
-            const uint32_t off = step < a.steps ? from[i] + (uint32_t)step * kStep : 0x80000000u;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(first < kN ? rw : rx,
-                                                     (__attribute__((address_space(3))) void *)(to + first * kStep),
-                                                     kChunk, off, 0, 0, 0);
+            const uint32_t off = step < steps && from[i] != kNowhere ? from[i] + (uint32_t)step * kStep : kNowhere;
+            load_to_lds(row < kN ? rw : rx, off, to + row * kStep);
         }
     };
     i32x4 acc[kTn][kTm] = {};
-#pragma unroll
-    for (int s = 0; s < kStages - 1; s++) fetch(s);
     const int r16 = lane % 16, quad = lane / 16;
-    for (int32_t step = 0; step < a.steps; step++) {
+    const int32_t v0 = n0 + wn * kTn * 16 + quad * 4, b0 = m0 + wm * kTm * 16 + r16;    // the lane's first token and state
+    Factors<kTn, kTm> factors;
+    if (!plan.gather && plan.splits == 1) factors.load(a, v0, b0);
+#pragma unroll
+    for (int s = 0; s < kStages - 1; s++) fetch(first + s);
+    for (int32_t step = first; step < steps; step++) {
         wait_and_meet<(kStages - 2) * kLoads>();   // the step has landed, and its predecessor's buffer is free
         fetch(step + kStages - 1);
         const int8_t *from_lds = lds[step % kStages];
@@ -166,65 +469,329 @@ head_kernel(const HeadArgs a) {
                     acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[i], fx[j], acc[i][j], 0, 0, 0);
         }
     }
-    // lane: state r16 of a block, tokens 4 quad .. 4 quad + 3
+    if (plan.splits > 1) {
+        // The sums go to memory at device scope, which every XCD sees alike, and
+        // only when they are there does the workgroup count itself in; the
+        // last one of the tile reads them all.
+        int32_t *const sums = a.partials + (int64_t)tile * plan.splits * (kM * kN);
+        const auto place = [&](int32_t part, int i, int j, int e) {
+            return sums + (int64_t)part * (kM * kN) + ((i * kTm + j) * 4 + e) * (kWaves * kWave) + threadIdx.x;
+        };
 #pragma unroll
-    for (int i = 0; i < kTn; i++) {
-        const int32_t v0 = n0 + (wn * kTn + i) * 16 + quad * 4;
-        if (v0 >= a.V) continue;
-        float ws[4], bias[4] = {};
+        for (int i = 0; i < kTn; i++)
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-            const int32_t v = min(v0 + e, a.V - 1);
-            ws[e] = a.w_scales[v];
-            if (a.bias) bias[e] = a.bias[v];
-        }
+            for (int j = 0; j < kTm; j++)
 #pragma unroll
-        for (int j = 0; j < kTm; j++) {
-            const int32_t b = m0 + (wm * kTm + j) * 16 + r16;
-            if (b >= a.B) continue;
-            const float xs = a.x_scales[b];
-            uint32_t bits = 15;
-            if (a.bitmask) bits = a.bitmask[(int64_t)b * a.W + (v0 >> 5)] >> (v0 & 31);
-            float y[4];
-#pragma unroll
-            for (int e = 0; e < 4; e++) y[e] = (bits >> e) & 1 ? (float)acc[i][j][e] * xs * ws[e] + bias[e] : kMinusInf;
-            using T = typename Logit<kBf16>::type;
-            T *to = static_cast<T *>(a.y) + (int64_t)b * a.y_stride + v0;
-            T out[4];
-#pragma unroll
-            for (int e = 0; e < 4; e++) {
-                if constexpr (kBf16) out[e] = to_bf16(y[e]);
-                else out[e] = y[e];
-            }
-            if (v0 + 4 <= a.V) __builtin_memcpy(to, out, sizeof out);
-            else
                 for (int e = 0; e < 4; e++)
-                    if (v0 + e < a.V) to[e] = out[e];
+                    __hip_atomic_store(place(split, i, j, e), acc[i][j][e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (threadIdx.x == 0) s_arrived = __hip_atomic_fetch_add(a.arrivals + tile, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        if (s_arrived != (uint32_t)plan.splits - 1) return;
+        if (!plan.gather) factors.load(a, v0, b0);
+        for (int32_t part = 0; part < plan.splits; part++) {
+            if (part == split) continue;
+#pragma unroll
+            for (int i = 0; i < kTn; i++)
+#pragma unroll
+                for (int j = 0; j < kTm; j++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        acc[i][j][e] += __hip_atomic_load(place(part, i, j, e), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
     }
+    if (!plan.gather) {
+        factors.template put<kBf16>(a, v0, b0, acc);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < kTn; i++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const int32_t v = s_ids[(wn * kTn + i) * 16 + quad * 4 + e];
+            if (v < 0) continue;
+            const float ws = a.w_scales[v], bias = a.bias ? a.bias[v] : 0.0f;
+#pragma unroll
+            for (int j = 0; j < kTm; j++)
+                if (b0 + j * 16 < a.B) put_if_allowed<kBf16>(a, b0 + j * 16, v, acc[i][j][e], a.x_scales[b0 + j * 16], ws, bias);
+        }
+}
+
+template <int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kBf16>
+__global__ void __launch_bounds__(kWave * kWavesM * kWavesN)
+small_kernel(const HeadArgs a, bool gather_only) {
+    small_body<kM, kN, kWavesM, kWavesN, kStages, kBf16>(a, gather_only);
+}
+
+// ---------------------------------------------------------------- more than 128 rows
+
+// 256 states by kN tokens a tile, 8 wavefronts of 64 states by kN / 2 tokens, a
+// workgroup per compute unit that goes through tiles until none are left, its
+// loads running ahead into the next tile.
+//
+// The matrix cores are fed by two groups of four wavefronts, one of each per
+// SIMD, half a turn apart: while one group multiplies (64 bytes of D, 32 or 40
+// matrix instructions a wavefront), the other reads its next operands from LDS
+// and issues loads, and a barrier ends each turn.
+//
+// LDS holds kRing steps of weights, which come from HBM, and two of states,
+// which come from L2.  A load covers whole 128-byte lines: with 64-byte pieces
+// the loads alone took 507 us of 2,048 x 128,256 x 4,096, with lines 322.
+//
+// XCDs take workgroups in turn; ids are dealt so that the tiles of one block of
+// tokens (all blocks of states) run on one XCD and share its L2.
+template <int kN, int kRing, bool kBf16, bool kPlain>
+__device__ __forceinline__ void wide_body(const HeadArgs &a) {
+    constexpr int kM = 256, kWavesM = 4, kWavesN = 2, kWaves = 8;
+    constexpr int kLoadsW = kN * kChunks / (kWaves * kWave), kLoadsX = kM * kChunks / (kWaves * kWave);
+    static_assert(kLoadsW * kWaves * kWave == kN * kChunks && kN % 64 == 0, "every wavefront loads as much");
+    static_assert(kRing == 2 || kRing == 3, "only the newest weights may be outstanding");
+    constexpr int kTm = kM / kWavesM / 16, kTn = kN / kWavesN / 16, kPairs = kTn / 2;
+    __shared__ __align__(1024) int8_t lds_w[kRing * kN * kStep], lds_x[2 * kM * kStep];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int wm = wave % kWavesM, wn = wave / kWavesM;
+    if (a.counts) {
+        int32_t count[kShare];
+        if (lane_value(needed_upto(a, lane, count), kWave - 1) <= a.gather_most) return;      // small_kernel's
+    }
+    const int32_t n_tiles = (a.V + kN - 1) / kN, tiles = n_tiles * a.m_tiles, whole = n_tiles / 8 * 8 * a.m_tiles;
+    const auto corner = [&](int32_t id, int32_t &m0, int32_t &n0) {
+        n0 = (id < whole ? id / 8 / a.m_tiles * 8 + id % 8 : id / a.m_tiles) * kN;
+        m0 = (id < whole ? id / 8 % a.m_tiles : id % a.m_tiles) * kM;
+    };
+    const int row8 = wave * 8 + lane / 8;
+    const uint32_t chunk = ((lane & 7) ^ (row8 & 7)) * kChunk;
+    const uint32_t base_w = (uint32_t)row8 * (uint32_t)a.w_stride + chunk, base_x = (uint32_t)row8 * (uint32_t)a.x_stride + chunk;
+    const uint32_t turn_w = kWaves * 8 * (uint32_t)a.w_stride, turn_x = kWaves * 8 * (uint32_t)a.x_stride;
+    // the loads' own tile and step; past the last tile they read nothing, and their number stays the same
+    int32_t id_w = blockIdx.x, id_x = blockIdx.x, step_w = 0, step_x = 0, to_w = 0, to_x = 0;
+    __amdgpu_buffer_rsrc_t rw, rx;
+    const auto point_w = [&]() {
+        int32_t m0, n0;
+        corner(id_w, m0, n0);
+        rw = id_w < tiles ? rows_from(a.w + (int64_t)n0 * a.w_stride, weight_bytes(a, n0)) : rows_from(a.w, 0);
+    };
+    const auto point_x = [&]() {
+        int32_t m0, n0;
+        corner(id_x, m0, n0);
+        rx = id_x < tiles ? rows_from(a.x + (int64_t)m0 * a.x_stride, (int64_t)(a.B - m0) * a.x_stride) : rows_from(a.x, 0);
+    };
+    const auto fetch_w = [&]() {
+#pragma unroll
+        for (int i = 0; i < kLoadsW; i++)
+            load_to_lds(rw, base_w + i * turn_w + (uint32_t)step_w * kStep, lds_w + (to_w * kN + (i * kWaves + wave) * 8) * kStep);
+        to_w = to_w == kRing - 1 ? 0 : to_w + 1;
+        if (++step_w == a.steps) {
+            step_w = 0;
+            id_w += (int32_t)gridDim.x;
+            point_w();
+        }
+    };
+    const auto fetch_x = [&]() {
+#pragma unroll
+        for (int i = 0; i < kLoadsX; i++)
+            load_to_lds(rx, base_x + i * turn_x + (uint32_t)step_x * kStep, lds_x + (to_x * kM + (i * kWaves + wave) * 8) * kStep);
+        to_x ^= 1;
+        if (++step_x == a.steps) {
+            step_x = 0;
+            id_x += (int32_t)gridDim.x;
+            point_x();
+        }
+    };
+    point_w();
+    point_x();
+    fetch_x();
+    for (int i = 0; i < kRing - 1; i++) fetch_w();
+    const int r16 = lane % 16, quad = lane / 16;
+    // the newest step of weights, fetched after the states of its turn, need not have landed where there are three
+    constexpr int kLeft = kRing == 3 ? kLoadsW : 0;
+    wait_and_meet<kLeft>();
+    if (wave >= kWaves / 2) asm volatile("s_barrier" ::: "memory");      // the second group, one turn later
+    int32_t at_w = 0, at_x = 0;
+    for (int32_t id = blockIdx.x; id < tiles; id += (int32_t)gridDim.x) {
+        i32x4 acc[kTn][kTm] = {};
+        for (int32_t s = 0; s < a.steps; s++) {
+            const int8_t *const pw = lds_w + (at_w * kN + wn * kTn * 16 + r16) * kStep;
+            const int8_t *const px = lds_x + (at_x * kM + wm * kTm * 16 + r16) * kStep;
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+                const int place = ((k * 4 + quad) ^ (r16 & 7)) * kChunk;
+                i32x4 fw[kTn], fx[kTm];
+#pragma unroll
+                for (int i = 0; i < kTn; i++) fw[i] = *reinterpret_cast<const i32x4 *>(pw + i * 16 * kStep + place);
+#pragma unroll
+                for (int j = 0; j < kTm; j++) fx[j] = *reinterpret_cast<const i32x4 *>(px + j * 16 * kStep + place);
+                // Into the buffers of the step before, which the second group left two turns ago.
+                if (k == 0) {
+                    fetch_x();
+                    fetch_w();
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (k == 0) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                else wait_and_meet<kLeft>();       // this wavefront's part of the next step has landed
+                __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+                for (int i = 0; i < kTn; i++)
+#pragma unroll
+                    for (int j = 0; j < kTm; j++)
+                        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[i], fx[j], acc[i][j], 0, 0, 0);
+                __builtin_amdgcn_s_setprio(0);
+                __builtin_amdgcn_sched_barrier(0);
+                asm volatile("s_barrier" ::: "memory");
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            at_w = at_w == kRing - 1 ? 0 : at_w + 1;
+            at_x ^= 1;
+        }
+        int32_t m0, n0;
+        corner(id, m0, n0);
+        const int32_t v0 = n0 + wn * kTn * 16;       // the wavefront's first token
+        if (kBf16 && m0 + kM <= a.B && n0 + kN <= a.V) {
+            // Whole tiles of bfloat16: of two blocks of 16 tokens, lanes 16
+            // apart swap halves, so that each has eight consecutive tokens
+            // and a store writes 64 bytes of every state's row.
+            using T = typename Logit<kBf16>::type;
+            const int32_t mine = (quad & 1) * 16 + (quad >> 1) * 8;
+            float xs[kTm];
+            T *to[kTm];
+            const uint32_t *words[kTm];
+#pragma unroll
+            for (int j = 0; j < kTm; j++) {
+                const int32_t b = m0 + (wm * kTm + j) * 16 + r16;
+                xs[j] = a.x_scales[b];
+                to[j] = static_cast<T *>(a.y) + (int64_t)b * a.y_stride + v0 + mine;
+                if (!kPlain && a.bitmask) words[j] = a.bitmask + (int64_t)b * a.W + (v0 >> 5);
+            }
+#pragma unroll
+            for (int p = 0; p < kPairs; p++) {
+                float ws[2][4], bias[2][4] = {};
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    const int32_t v = v0 + (2 * p + h) * 16 + quad * 4;
+                    __builtin_memcpy(ws[h], a.w_scales + v, sizeof ws[h]);
+                    if (!kPlain && a.bias) __builtin_memcpy(bias[h], a.bias + v, sizeof bias[h]);
+                }
+#pragma unroll
+                for (int j = 0; j < kTm; j++) {
+                    uint32_t o[2][2];
+#pragma unroll
+                    for (int h = 0; h < 2; h++)
+#pragma unroll
+                        for (int e = 0; e < 2; e++)
+                            o[h][e] = (uint32_t)to_bf16(scaled(acc[2 * p + h][j][2 * e], xs[j], ws[h][2 * e], bias[h][2 * e])) |
+                                      (uint32_t)to_bf16(scaled(acc[2 * p + h][j][2 * e + 1], xs[j], ws[h][2 * e + 1], bias[h][2 * e + 1])) << 16;
+                    const auto s0 = __builtin_amdgcn_permlane16_swap(o[0][0], o[1][0], false, false);
+                    const auto s1 = __builtin_amdgcn_permlane16_swap(o[0][1], o[1][1], false, false);
+                    u32x4 t = {(uint32_t)s0[0], (uint32_t)s1[0], (uint32_t)s0[1], (uint32_t)s1[1]};
+                    if (!kPlain && a.bitmask) {
+                        const uint32_t allowed = words[j][p] >> mine;
+#pragma unroll
+                        for (int e = 0; e < 4; e++) {
+                            const uint32_t keep = ((allowed >> (2 * e)) & 1 ? 0xFFFFu : 0u) | ((allowed >> (2 * e + 1)) & 1 ? 0xFFFF0000u : 0u);
+                            t[e] = (t[e] & keep) | (0xFF80FF80u & ~keep);
+                        }
+                    }
+                    __builtin_memcpy(to[j] + p * 32, &t, sizeof t);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kTn; i++) {
+                const int32_t v = v0 + i * 16 + quad * 4, b = m0 + wm * kTm * 16 + r16;
+                Factors<1, kTm> factors;
+                factors.load(a, v, b);
+                factors.template put<kBf16>(a, v, b, reinterpret_cast<const i32x4 (&)[1][kTm]>(acc[i]));
+            }
+        }
+    }
+    if (wave < kWaves / 2) asm volatile("s_barrier" ::: "memory");
+}
+
+// kPlain: neither a mask nor a bias.
+template <int kN, int kRing, bool kBf16, bool kPlain>
+__global__ void __launch_bounds__(kWave * 8, 2)
+wide_kernel(const HeadArgs a) {
+    wide_body<kN, kRing, kBf16, kPlain>(a);
+}
+
+// ---------------------------------------------------------------- host side
+
+constexpr int32_t kComputeUnits = 256;
+constexpr int32_t kWideRows = 128;       // from here on, wide_kernel
+
+int32_t up(int64_t n, int64_t d) { return (int32_t)((n + d - 1) / d); }
+
+// How small_kernel is launched: its tiles of kM by kN, the parts of D, and the
+// workgroups, of which there are enough to split D further when few tokens are needed.
+template <int kM, int kN>
+void shape_small(HeadArgs &a, bool gather_only) {
+    a.m_tiles = up(a.B, kM);
+    const int64_t tiles = (int64_t)a.m_tiles * up(a.V, kN);
+    // Parts of D where the tiles alone would leave compute units idle, of at
+    // least four steps each.
+    const int64_t room = tiles > a.arrivals_most ? 1 : a.partials_most / (tiles * kM * kN);
+    a.splits = gather_only ? 1 : (int32_t)std::max<int64_t>(1, std::min<int64_t>({2 * kComputeUnits / tiles, a.steps / 4, 16, room}));
+    a.units = (int32_t)std::max<int64_t>(tiles * a.splits, 2 * kComputeUnits);
 }
 
 template <int kM, int kN, int kWavesM, int kWavesN, int kStages>
-void launch_head(HeadArgs a, bool bf16, hipStream_t s) {
-    a.m_tiles = (a.B + kM - 1) / kM;
-    const dim3 grid((uint32_t)a.m_tiles * (uint32_t)((a.V + kN - 1) / kN)), block(kWave * kWavesM * kWavesN);
-    if (bf16) hipLaunchKernelGGL((head_kernel<kM, kN, kWavesM, kWavesN, kStages, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((head_kernel<kM, kN, kWavesM, kWavesN, kStages, false>), grid, block, 0, s, a);
+void launch_small(HeadArgs a, bool bf16, bool gather_only, hipStream_t s) {
+    shape_small<kM, kN>(a, gather_only);
+    const dim3 grid((uint32_t)a.units), block(kWave * kWavesM * kWavesN);
+    if (bf16) hipLaunchKernelGGL((small_kernel<kM, kN, kWavesM, kWavesN, kStages, true>), grid, block, 0, s, a, gather_only);
+    else hipLaunchKernelGGL((small_kernel<kM, kN, kWavesM, kWavesN, kStages, false>), grid, block, 0, s, a, gather_only);
 }
 
-void launch_quantize(const void *x, psc_dtype dtype, int64_t x_stride, int64_t n_rows, int32_t D, int32_t padded,
-                     int8_t *q, int64_t q_stride, float *scales, hipStream_t s) {
-    const dim3 grid((uint32_t)n_rows);
-    if (dtype == PSC_BF16)
-        hipLaunchKernelGGL(quantize_kernel<true>, grid, dim3(kQuantBlock), 0, s, x, x_stride, D, padded, q, q_stride, scales);
-    else
-        hipLaunchKernelGGL(quantize_kernel<false>, grid, dim3(kQuantBlock), 0, s, x, x_stride, D, padded, q, q_stride, scales);
+template <int kN, int kRing>
+void launch_wide(HeadArgs a, bool bf16, hipStream_t s) {
+    a.m_tiles = up(a.B, 256);
+    const dim3 grid((uint32_t)std::min<int64_t>(kComputeUnits, (int64_t)a.m_tiles * up(a.V, kN))), block(kWave * 8);
+    if (!bf16) hipLaunchKernelGGL((wide_kernel<kN, kRing, false, false>), grid, block, 0, s, a);
+    else if (a.bitmask || a.bias) hipLaunchKernelGGL((wide_kernel<kN, kRing, true, false>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((wide_kernel<kN, kRing, true, true>), grid, block, 0, s, a);
+}
+
+// Of the two widths of wide_kernel the one that ends first: rounds of tiles
+// over the compute units times a tile's width.  256 states x 151,936 tokens x
+// 4,096: 3 rounds of 256 take 221 us, 2 of 320 201; 2,048 x 128,256: 16 of 256
+// 922, 13 of 320 936.
+void launch_product(const HeadArgs &a, bool bf16, hipStream_t s) {
+    if (a.B <= 16) return launch_small<16, 16, 1, 1, 4>(a, bf16, false, s);
+    if (a.B <= 32) return launch_small<32, 64, 1, 4, 4>(a, bf16, false, s);
+    if (a.B <= 64) return launch_small<64, 128, 1, 4, 3>(a, bf16, false, s);
+    if (a.B <= kWideRows) return launch_small<128, 128, 2, 4, 3>(a, bf16, false, s);
+    if (a.counts) launch_small<64, 128, 1, 4, 3>(a, bf16, true, s);
+    const int64_t rounds256 = up((int64_t)up(a.B, 256) * up(a.V, 256), kComputeUnits),
+                  rounds320 = up((int64_t)up(a.B, 256) * up(a.V, 320), kComputeUnits);
+    if (rounds320 * 320 < rounds256 * 256) launch_wide<320, 2>(a, bf16, s);
+    else launch_wide<256, 3>(a, bf16, s);
 }
 
 constexpr int32_t kMostD = 131072;       // |sum| <= 127 * 128 * D stays below 2^31
-int32_t whole_steps(int32_t D) { return (D + kStep - 1) / kStep * kStep; }
-// The workspace: quantised states [B][whole_steps(D)], then their scales.
-size_t states_bytes(int32_t B, int32_t D) { return (size_t)B * (size_t)whole_steps(D); }
+int32_t whole_steps(int32_t D) { return up(D, kStep) * kStep; }
+
+// The workspace: quantised states [B][whole_steps(D)], their scales, the needed
+// tokens, the arrival counters, the partial sums; each from a multiple of 16
+// bytes on.
+constexpr int32_t kMostArrivals = 2 * kComputeUnits;
+struct Workspace {
+    size_t scales, counts, ids, arrivals, partials, total;
+    int64_t partials_most;
+    Workspace(int32_t B, int32_t D, int32_t V) {
+        const auto whole = [](size_t n) { return (n + 15) / 16 * 16; };
+        const int64_t blocks = up(V, kBlockTokens);
+        scales = (size_t)B * (size_t)whole_steps(D);
+        counts = scales + whole((size_t)B * sizeof(float));
+        ids = counts + whole(blocks <= kMostBlocks ? blocks * sizeof(int32_t) : 0);
+        arrivals = ids + (blocks <= kMostBlocks ? blocks * kBlockTokens * sizeof(int32_t) : 0);
+        partials = arrivals + kMostArrivals * sizeof(uint32_t);
+        // twice the compute units' number of the largest tiles
+        partials_most = std::min<int64_t>((int64_t)kMostArrivals * 128 * 128, (int64_t)16 * up(B, 16) * 16 * (up(V, 128) * 128));
+        total = partials + (size_t)partials_most * sizeof(int32_t);
+    }
+};
 
 }  // namespace
 
@@ -237,16 +804,19 @@ extern "C" psc_status psc_quantize_rows(const void *x, psc_dtype dtype, int64_t 
     const int64_t padded = ((int64_t)D + kChunk - 1) / kChunk * kChunk;
     if ((D > 0 && (!x || !q)) || !scales) return refuse(what, "null pointer");
     if (n_rows > INT32_MAX) return refuse(what, "more than 2^31 - 1 rows");
+    if (D > INT32_MAX - 8 * kQuantBlock * kQuantVec) return refuse(what, "D too large");
     if (x_stride < 0 || !aligned_to(x, size_of(dtype))) return refuse(what, "negative stride, or x off its elements' alignment");
     if (q_stride % kChunk || q_stride < padded || !aligned_to(q, kChunk))
         return refuse(what, "rows of q start at 16 bytes and hold D elements");
-    launch_quantize(x, dtype, x_stride, n_rows, D, (int32_t)padded, q, q_stride, scales, reinterpret_cast<hipStream_t>(stream));
+    const dim3 grid((uint32_t)n_rows), block(kQuantBlock);
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    if (dtype == PSC_BF16) hipLaunchKernelGGL(quantize_kernel<true>, grid, block, 0, s, x, x_stride, D, (int32_t)padded, q, q_stride, scales);
+    else hipLaunchKernelGGL(quantize_kernel<false>, grid, block, 0, s, x, x_stride, D, (int32_t)padded, q, q_stride, scales);
     return launched_op(what);
 }
 
 extern "C" size_t psc_head_workspace(int32_t B, int32_t D, int32_t V) {
-    (void)V;
-    return B <= 0 || D < 0 ? 0 : states_bytes(B, D) + (size_t)B * sizeof(float);
+    return B <= 0 || D <= 0 || D > kMostD || V <= 0 ? 0 : Workspace(B, D, V).total;
 }
 
 extern "C" psc_status psc_head_logits(const void *x, psc_dtype x_dtype, int64_t x_stride, int32_t B, int32_t D,
@@ -265,14 +835,12 @@ extern "C" psc_status psc_head_logits(const void *x, psc_dtype x_dtype, int64_t 
     if (workspace_bytes < psc_head_workspace(B, D, V) || !aligned_to(workspace, kChunk))
         return refuse(what, "the workspace is too small or not 16-byte aligned");
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    const Workspace ws(B, D, V);
+    char *at = static_cast<char *>(workspace);
     HeadArgs a{};
-    int8_t *q = static_cast<int8_t *>(workspace);
-    float *scales = reinterpret_cast<float *>(q + states_bytes(B, D));
-    launch_quantize(x, x_dtype, x_stride, B, D, whole_steps(D), q, whole_steps(D), scales, s);
-    if (psc_status st = launched_op(what)) return st;
-    a.x = q;
+    a.x = reinterpret_cast<int8_t *>(at);
     a.x_stride = whole_steps(D);
-    a.x_scales = scales;
+    a.x_scales = reinterpret_cast<float *>(at + ws.scales);
     a.w = w;
     a.w_stride = w_stride;
     a.w_scales = w_scales;
@@ -283,11 +851,25 @@ extern "C" psc_status psc_head_logits(const void *x, psc_dtype x_dtype, int64_t 
     a.B = B;
     a.D = D;
     a.V = V;
-    a.W = (int32_t)(((int64_t)V + 31) / 32);
+    a.W = up(V, 32);
     a.steps = whole_steps(D) / kStep;
-    const bool bf16 = dtype == PSC_BF16;
-    if (B <= 16) launch_head<16, 64, 1, 2, 4>(a, bf16, s);
-    else if (B <= 64) launch_head<64, 128, 2, 2, 3>(a, bf16, s);
-    else launch_head<256, 256, 2, 4, 2>(a, bf16, s);
+    a.partials = reinterpret_cast<int32_t *>(at + ws.partials);
+    a.partials_most = ws.partials_most;
+    a.arrivals = reinterpret_cast<uint32_t *>(at + ws.arrivals);
+    a.arrivals_most = kMostArrivals;
+    // The needed tokens are listed where offsets of all weights fit 32 bits.
+    int32_t *counts = nullptr, *ids = nullptr;
+    if (bitmask && up(V, kBlockTokens) <= kMostBlocks && (int64_t)V * w_stride < kMostBytes) {
+        a.blocks = up(V, kBlockTokens);
+        a.counts = counts = reinterpret_cast<int32_t *>(at + ws.counts);
+        a.ids = ids = reinterpret_cast<int32_t *>(at + ws.ids);
+        a.gather_most = V / 2;
+    }
+    const dim3 grid((uint32_t)((int64_t)B + a.blocks)), block(kQuantBlock);
+    int8_t *q = reinterpret_cast<int8_t *>(at);
+    float *scales = reinterpret_cast<float *>(at + ws.scales);
+    if (x_dtype == PSC_BF16) hipLaunchKernelGGL(prepare_kernel<true>, grid, block, 0, s, a, x, x_stride, q, scales, counts, ids);
+    else hipLaunchKernelGGL(prepare_kernel<false>, grid, block, 0, s, a, x, x_stride, q, scales, counts, ids);
+    launch_product(a, dtype == PSC_BF16, s);
     return launched_op(what);
 }

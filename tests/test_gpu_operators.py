@@ -486,3 +486,64 @@ def test_operators_on_another_stream_and_in_a_graph():
         again = step()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(held, again)), k
+
+
+# ---------------------------------------------------------------- head: many tiles, split sums, few needed tokens
+
+def head_exact(x, w, scales, bias=None):
+    """The logits in 64 bits, the sums by float64 products of whole numbers (exact)."""
+    q, s = quantized(x)
+    y = (torch.from_numpy(q).double() @ w.cpu().double().T).numpy()
+    y = y * s[:, None].astype(np.float64) * scales.cpu().double().numpy()
+    return y if bias is None else y + bias.cpu().double().numpy()
+
+
+def head_inputs(B, D, V, seed):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(B, D, generator=g).to(torch.bfloat16)
+    w = torch.randint(-128, 128, (V, (D + 15) // 16 * 16), generator=g, dtype=torch.int8).to(DEV)[:, :D]
+    return x.to(DEV), w, (torch.rand(V, generator=g) / D).to(DEV), torch.randn(V, generator=g).to(DEV)
+
+
+@pytest.mark.parametrize("B,D,V", [(256, 64, 70000), (300, 192, 66051), (256, 130, 151937), (1000, 40, 40000),
+                                   (129, 256, 82000), (2048, 16, 9000)])
+def test_head_logits_of_more_tiles_than_compute_units(B, D, V):
+    x, w, scales, bias = head_inputs(B, D, V, V)
+    words, keep = mask(B, V, 3, (0.97, 0.9, 0.0, 0.001))
+    for dtype in TYPES.values():
+        y = head_exact(x, w, scales)
+        close(psc.head_logits(x, w, scales, dtype=dtype), y, head_bound(y, 0))
+        close(psc.head_logits(x, w, scales, dtype=dtype, bias=bias, bitmask=words),
+              np.where(keep, y + host(bias), -np.inf), head_bound(y, host(bias)))
+
+
+@pytest.mark.parametrize("B", [1, 9, 16, 25, 32, 50, 64, 100, 128, 140])
+@pytest.mark.parametrize("D,V", [(2048, 100), (4096, 1500), (8192, 33), (1000, 9000), (640, 70001)])
+def test_head_logits_by_parts_of_d_and_of_few_tokens(B, D, V):
+    """Splits of D, and masks whose union is nothing, one token, some, about half of the tokens, and all but a few."""
+    x, w, scales, bias = head_inputs(B, D, V, B + D)
+    y = head_exact(x, w, scales)
+    close(psc.head_logits(x, w, scales, dtype=torch.float32), y, head_bound(y, 0))
+    r = np.random.default_rng(D)
+    union = r.random(V) < 0.5
+    for n, within in enumerate((np.zeros(V, bool), np.arange(V) == V - 1, r.random(V) < 30 / V, union,
+                                np.arange(V) < V // 2, np.arange(V) % 64 == 63, r.random(V) < 0.98)):
+        keep = within & (r.random((B, V)) < (1.0 if n % 2 else 0.6))
+        words = np.zeros((B, (V + 31) // 32 * 32), bool)
+        words[:, :V] = keep
+        words = torch.from_numpy(np.packbits(words, axis=1, bitorder="little").view(np.int32).copy()).to(DEV)
+        dtype = (torch.float32, torch.bfloat16)[n % 2]
+        out = rows_apart(torch.zeros(B, V, dtype=dtype, device=DEV), (0, 3)[n % 2])
+        psc.head_logits(x, w, scales, bias=bias, bitmask=words, out=out)
+        close(out, np.where(keep, y + host(bias), -np.inf), head_bound(y, host(bias)))
+        assert around(out, (0, 3)[n % 2])
+
+
+def test_head_logits_of_states_and_weights_that_lie_apart():
+    """States with a row stride, weights with room between the rows, D beyond what a row's quantisation holds at once."""
+    g = torch.Generator().manual_seed(12)
+    x = torch.randn(20, 9000, generator=g)
+    wide = torch.randint(-128, 128, (700, 9200), generator=g, dtype=torch.int8).to(DEV)
+    scales = (torch.rand(700, generator=g) / 9000).to(DEV)
+    y = head_exact(x, wide[:, :9000], scales)
+    close(psc.head_logits(rows_apart(x.to(DEV), 7), wide[:, :9000], scales), y, head_bound(y, 0))
