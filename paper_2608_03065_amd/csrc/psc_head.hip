@@ -114,6 +114,7 @@ constexpr int kChunk = 16;        // bytes per lane of a load and of a matrix in
 constexpr int kChunks = kStep / kChunk;
 constexpr uint32_t kNowhere = 0xFFFF8000u;        // an offset past any resource: the hardware drops the access
 constexpr uint32_t kMostBytes = 0xFFFF0000u;      // of a resource
+constexpr int32_t kMostRows = 256;                // of a tile
 
 // The tokens that any row allows, in blocks of kBlockWords mask words: each
 // block's number of them, and their ids in ascending order.
@@ -138,7 +139,7 @@ struct HeadArgs {
     int32_t gather_most;          // most needed tokens at which only they are taken
     int32_t units;                // workgroups there are for tiles times parts
     int32_t *partials;            // [tiles][parts][kM * kN] sums, where D is split
-    int64_t partials_most;        // their room
+    int32_t partials_most;        // their room
     uint32_t *arrivals;           // [tiles] parts that have ended: prepare_kernel clears them
     int32_t arrivals_most;
 };
@@ -159,8 +160,8 @@ __device__ __forceinline__ Plan plan_of(const HeadArgs &a, int32_t total) {
         p.columns = total;
         p.tiles = (total + kN - 1) / kN;
         const int32_t tiles = max(p.tiles * a.m_tiles, 1);
-        const int64_t room = tiles > a.arrivals_most ? 1 : a.partials_most / ((int64_t)tiles * kM * kN);
-        p.splits = max(1, (int32_t)min((int64_t)min(a.units / tiles, min(a.steps / 2, 16)), room));
+        const int32_t room = tiles > a.arrivals_most ? 1 : a.partials_most / (tiles * kM * kN);
+        p.splits = max(1, min(min(a.units / tiles, room), min(a.steps / 2, 16)));
     }
     return p;
 }
@@ -253,41 +254,51 @@ __device__ __forceinline__ void put_four(const HeadArgs &a, int32_t b, int32_t v
             if (v + e < a.V) to[e] = out[e];
 }
 
-// What kTn by kTm blocks of 16 tokens by 16 states need besides their sums: all
-// of it is loaded at once, and for small_kernel before the product.  The lane's
-// tokens of block i are v + 16 i .. + 3, its state of block j is b + 16 j;
-// places past the last row or token stand for the last one.
-template <int kTn, int kTm>
+__device__ __forceinline__ uint32_t load_word(__amdgpu_buffer_rsrc_t from, int32_t at) {
+    return __builtin_amdgcn_raw_buffer_load_b32(from, (uint32_t)at * 4u, 0, 0);
+}
+
+// What kTn by kTm blocks of 16 tokens by 16 states need besides their sums.
+// The lane's tokens of block i are v + 16 i .. + 3, its state of block j is
+// m0 + b + 16 j.  All of it is loaded at once, by small_kernel before the
+// product, without a branch: places outside, a bias or a mask that there is not
+// give zeros.  kPlain: neither a bias nor a mask.
+template <int kTn, int kTm, bool kPlain>
 struct Factors {
     float ws[kTn][4], bias[kTn][4], xs[kTm];
-    uint32_t allowed[kTn][kTm];
+    uint32_t words[kTn][kTm];
 
-    __device__ __forceinline__ void load(const HeadArgs &a, int32_t v, int32_t b) {
+    __device__ __forceinline__ void load(const HeadArgs &a, int32_t v, int32_t m0, int32_t b) {
+        const uint32_t tokens = (uint32_t)a.V * 4u;
+        const __amdgpu_buffer_rsrc_t from_ws = buffer_of(a.w_scales, tokens), from_bias = buffer_of(a.bias, a.bias ? tokens : 0);
+        const __amdgpu_buffer_rsrc_t from_xs = buffer_of(a.x_scales + m0, (uint32_t)min(a.B - m0, kMostRows) * 4u);
+        const __amdgpu_buffer_rsrc_t from_mask =
+            buffer_of(a.bitmask + (a.bitmask ? (int64_t)m0 * a.W : 0), a.bitmask ? (uint32_t)min((int64_t)min(a.B - m0, kMostRows) * a.W * 4, (int64_t)kMostBytes) : 0);
 #pragma unroll
-        for (int j = 0; j < kTm; j++) xs[j] = a.x_scales[min(b + j * 16, a.B - 1)];
+        for (int j = 0; j < kTm; j++) xs[j] = __builtin_bit_cast(float, load_word(from_xs, b + j * 16));
 #pragma unroll
         for (int i = 0; i < kTn; i++) {
 #pragma unroll
             for (int e = 0; e < 4; e++) {
-                const int32_t at = min(v + i * 16 + e, a.V - 1);
-                ws[i][e] = a.w_scales[at];
-                bias[i][e] = a.bias ? a.bias[at] : 0.0f;
+                ws[i][e] = __builtin_bit_cast(float, load_word(from_ws, v + i * 16 + e));
+                bias[i][e] = kPlain ? 0.0f : __builtin_bit_cast(float, load_word(from_bias, v + i * 16 + e));
             }
-            const int32_t at = min(v + i * 16, a.V - 1);
+            if (!kPlain)
 #pragma unroll
-            for (int j = 0; j < kTm; j++)
-                allowed[i][j] = a.bitmask ? a.bitmask[(int64_t)min(b + j * 16, a.B - 1) * a.W + (at >> 5)] >> (at & 31) : 15u;
+                for (int j = 0; j < kTm; j++) words[i][j] = load_word(from_mask, (b + j * 16) * a.W + ((v + i * 16) >> 5));
         }
     }
 
     template <bool kBf16>
     __device__ __forceinline__ void put(const HeadArgs &a, int32_t v, int32_t b, const i32x4 (&sum)[kTn][kTm]) const {
+        const uint32_t all = kPlain || !a.bitmask ? 15u : 0u;
 #pragma unroll
         for (int i = 0; i < kTn; i++)
 #pragma unroll
             for (int j = 0; j < kTm; j++)
                 if (v + i * 16 < a.V && b + j * 16 < a.B)
-                    put_four<kBf16>(a, b + j * 16, v + i * 16, sum[i][j], xs[j], ws[i], bias[i], allowed[i][j]);
+                    put_four<kBf16>(a, b + j * 16, v + i * 16, sum[i][j], xs[j], ws[i], bias[i],
+                                    kPlain ? 15u : words[i][j] >> ((v + i * 16) & 31) | all);
     }
 };
 
@@ -313,7 +324,7 @@ __device__ __forceinline__ void fill_forbidden(const HeadArgs &a, int64_t part, 
         else inf[e] = kMinusInf;
     }
     for (int64_t u = part; u < (int64_t)a.B * pieces; u += parts) {
-        const int64_t b = u / pieces;
+        const int64_t b = u >> 32 ? u / pieces : (int64_t)((uint32_t)u / (uint32_t)pieces);
         const int32_t v0 = (int32_t)(u - b * pieces) * kBlockTokens;
         T *row = static_cast<T *>(a.y) + b * a.y_stride;
         const uint32_t *words = a.bitmask + b * a.W;
@@ -340,13 +351,24 @@ __device__ __forceinline__ void wait_and_meet() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(n) : "memory");
 }
 
-// 16 bytes per lane from the resource straight to LDS: lane l's to place l from `to` on.
-__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t from, uint32_t offset, int8_t *to) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)to, kChunk, offset, 0, 0, 0);
+// 16 bytes per lane from the resource straight to LDS: lane l's to place l from
+// byte `to` of LDS on (M0; the hardware wants an instruction between its write
+// and the load).  In assembly, because the compiler would wait for all such
+// loads before any read of LDS; wait_and_meet waits for the ones that are due.
+__device__ __forceinline__ void load_to_lds(u32x4 from, uint32_t offset, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(from)
+                 : "memory", "m0");
 }
 
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const int8_t *p, int64_t bytes) {
-    return buffer_of(p, (uint32_t)min(max(bytes, (int64_t)0), (int64_t)kMostBytes));
+// The byte of LDS that a pointer into it names.
+__device__ __forceinline__ uint32_t lds_byte(const void *p) {
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p;
+}
+
+// The words of buffer_of's resource.
+__device__ __forceinline__ u32x4 rows_from(const int8_t *p, int64_t bytes) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    return u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, (uint32_t)min(max(bytes, (int64_t)0), (int64_t)kMostBytes), 0x00020000u};
 }
 // The weights from row `row` on; what lies behind the last row's D elements
 // (up to 16 bytes) is not touched.
@@ -361,7 +383,7 @@ __device__ __forceinline__ int64_t weight_bytes(const HeadArgs &a, int32_t row) 
 // reads at one chunk fall into different banks; since a load puts lane l's
 // chunk at place l, the lane fetches the chunk that belongs there.  What is
 // read past a row's D elements is multiplied by the states' zeros.
-template <int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kBf16>
+template <int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kBf16, bool kPlain>
 __device__ __forceinline__ void small_body(const HeadArgs &a, bool gather_only) {
     constexpr int kWaves = kWavesM * kWavesN, kRows = kM + kN;
     constexpr int kLoads = kRows * kChunks / (kWaves * kWave);
@@ -369,13 +391,16 @@ __device__ __forceinline__ void small_body(const HeadArgs &a, bool gather_only) 
     constexpr int kTm = kM / kWavesM / 16, kTn = kN / kWavesN / 16;   // 16 x 16 blocks of a wavefront
     static_assert(kTm * kWavesM * 16 == kM && kTn * kWavesN * 16 == kN, "whole blocks");
     __shared__ __align__(1024) int8_t lds[kStages][kRows * kStep];
-    __shared__ int32_t s_ids[kN], s_before[kMostBlocks + 1];
+    __shared__ int32_t s_ids[kN];
     __shared__ uint32_t s_arrived;
+    // until the first loads into lds: the needed tokens before each block
+    int32_t *const s_before = reinterpret_cast<int32_t *>(&lds[0][0]);
+    static_assert(sizeof lds >= (kMostBlocks + 1) * sizeof(int32_t), "room for the blocks");
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int wm = wave % kWavesM, wn = wave / kWavesM;
 
     int32_t total = 0, count[kShare];
-    if (a.counts) {
+    if (!kPlain && a.counts) {
         const int32_t upto = needed_upto(a, lane, count);
         total = lane_value(upto, kWave - 1);
         if (total <= a.gather_most && wave == 0) {
@@ -388,14 +413,15 @@ __device__ __forceinline__ void small_body(const HeadArgs &a, bool gather_only) 
             if (lane == 0) s_before[0] = 0;
         }
     }
-    const Plan plan = plan_of<kM, kN>(a, total);
+    Plan plan = plan_of<kM, kN>(a, total);
+    if (kPlain) plan.gather = false;
     if (plan.gather) fill_forbidden<kBf16>(a, blockIdx.x, gridDim.x);
     else if (gather_only) return;
     const int32_t tiles = plan.tiles * a.m_tiles;
     if ((int32_t)blockIdx.x >= tiles * plan.splits) return;
     const int32_t split = (int32_t)blockIdx.x / tiles, tile = (int32_t)blockIdx.x - split * tiles;
     const int32_t m0 = tile % a.m_tiles * kM, n0 = tile / a.m_tiles * kN;
-    const int32_t first = (int32_t)((int64_t)a.steps * split / plan.splits), steps = (int32_t)((int64_t)a.steps * (split + 1) / plan.splits);
+    const int32_t first = a.steps * split / plan.splits, steps = a.steps * (split + 1) / plan.splits;
 
     if (plan.gather) {
         // token n0 + i of the needed ones: its block by bisection of the sums before each
@@ -416,8 +442,8 @@ __device__ __forceinline__ void small_body(const HeadArgs &a, bool gather_only) 
         __syncthreads();
     }
     const int32_t w_row = plan.gather ? 0 : n0;
-    const __amdgpu_buffer_rsrc_t rw = rows_from(a.w + (int64_t)w_row * a.w_stride, weight_bytes(a, w_row));
-    const __amdgpu_buffer_rsrc_t rx = rows_from(a.x + (int64_t)m0 * a.x_stride, (int64_t)(a.B - m0) * a.x_stride);
+    const u32x4 rw = rows_from(a.w + (int64_t)w_row * a.w_stride, weight_bytes(a, w_row));
+    const u32x4 rx = rows_from(a.x + (int64_t)m0 * a.x_stride, (int64_t)(a.B - m0) * a.x_stride);
     uint32_t from[kLoads];
 #pragma unroll
     for (int i = 0; i < kLoads; i++) {
@@ -429,20 +455,20 @@ __device__ __forceinline__ void small_body(const HeadArgs &a, bool gather_only) 
         from[i] = at == kNowhere ? at : at + chunk * kChunk;
     }
     const auto fetch = [&](int32_t step) {
-        int8_t *to = lds[step % kStages];
+        const uint32_t to = lds_byte(lds) + (uint32_t)(step % kStages) * (kRows * kStep);
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
             const int row = (i * kWaves + wave) * 8;
             // past the last step nothing is read, and the number of accesses stays the same
             const uint32_t off = step < steps && from[i] != kNowhere ? from[i] + (uint32_t)step * kStep : kNowhere;
-            load_to_lds(row < kN ? rw : rx, off, to + row * kStep);
+            load_to_lds(row < kN ? rw : rx, off, to + (uint32_t)row * kStep);
         }
     };
     i32x4 acc[kTn][kTm] = {};
     const int r16 = lane % 16, quad = lane / 16;
     const int32_t v0 = n0 + wn * kTn * 16 + quad * 4, b0 = m0 + wm * kTm * 16 + r16;    // the lane's first token and state
-    Factors<kTn, kTm> factors;
-    if (!plan.gather && plan.splits == 1) factors.load(a, v0, b0);
+    Factors<kTn, kTm, kPlain> factors;
+    if (!plan.gather && plan.splits == 1) factors.load(a, v0, m0, b0 - m0);
 #pragma unroll
     for (int s = 0; s < kStages - 1; s++) fetch(first + s);
     for (int32_t step = first; step < steps; step++) {
@@ -489,7 +515,7 @@ __device__ __forceinline__ void small_body(const HeadArgs &a, bool gather_only) 
         if (threadIdx.x == 0) s_arrived = __hip_atomic_fetch_add(a.arrivals + tile, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
         if (s_arrived != (uint32_t)plan.splits - 1) return;
-        if (!plan.gather) factors.load(a, v0, b0);
+        if (!plan.gather) factors.load(a, v0, m0, b0 - m0);
         for (int32_t part = 0; part < plan.splits; part++) {
             if (part == split) continue;
 #pragma unroll
@@ -518,10 +544,10 @@ __device__ __forceinline__ void small_body(const HeadArgs &a, bool gather_only) 
         }
 }
 
-template <int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kBf16>
-__global__ void __launch_bounds__(kWave * kWavesM * kWavesN)
+template <int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kBf16, bool kPlain>
+__global__ void __launch_bounds__(kWave * kWavesM * kWavesN, 2)
 small_kernel(const HeadArgs a, bool gather_only) {
-    small_body<kM, kN, kWavesM, kWavesN, kStages, kBf16>(a, gather_only);
+    small_body<kM, kN, kWavesM, kWavesN, kStages, kBf16, kPlain>(a, gather_only);
 }
 
 // ---------------------------------------------------------------- more than 128 rows
@@ -566,7 +592,7 @@ __device__ __forceinline__ void wide_body(const HeadArgs &a) {
     const uint32_t turn_w = kWaves * 8 * (uint32_t)a.w_stride, turn_x = kWaves * 8 * (uint32_t)a.x_stride;
     // the loads' own tile and step; past the last tile they read nothing, and their number stays the same
     int32_t id_w = blockIdx.x, id_x = blockIdx.x, step_w = 0, step_x = 0, to_w = 0, to_x = 0;
-    __amdgpu_buffer_rsrc_t rw, rx;
+    u32x4 rw, rx;
     const auto point_w = [&]() {
         int32_t m0, n0;
         corner(id_w, m0, n0);
@@ -580,7 +606,7 @@ __device__ __forceinline__ void wide_body(const HeadArgs &a) {
     const auto fetch_w = [&]() {
 #pragma unroll
         for (int i = 0; i < kLoadsW; i++)
-            load_to_lds(rw, base_w + i * turn_w + (uint32_t)step_w * kStep, lds_w + (to_w * kN + (i * kWaves + wave) * 8) * kStep);
+            load_to_lds(rw, base_w + i * turn_w + (uint32_t)step_w * kStep, lds_byte(lds_w) + (uint32_t)(to_w * kN + (i * kWaves + wave) * 8) * kStep);
         to_w = to_w == kRing - 1 ? 0 : to_w + 1;
         if (++step_w == a.steps) {
             step_w = 0;
@@ -591,7 +617,7 @@ __device__ __forceinline__ void wide_body(const HeadArgs &a) {
     const auto fetch_x = [&]() {
 #pragma unroll
         for (int i = 0; i < kLoadsX; i++)
-            load_to_lds(rx, base_x + i * turn_x + (uint32_t)step_x * kStep, lds_x + (to_x * kM + (i * kWaves + wave) * 8) * kStep);
+            load_to_lds(rx, base_x + i * turn_x + (uint32_t)step_x * kStep, lds_byte(lds_x) + (uint32_t)(to_x * kM + (i * kWaves + wave) * 8) * kStep);
         to_x ^= 1;
         if (++step_x == a.steps) {
             step_x = 0;
@@ -700,10 +726,12 @@ __device__ __forceinline__ void wide_body(const HeadArgs &a) {
 #pragma unroll
             for (int i = 0; i < kTn; i++) {
                 const int32_t v = v0 + i * 16 + quad * 4, b = m0 + wm * kTm * 16 + r16;
-                Factors<1, kTm> factors;
-                factors.load(a, v, b);
+                Factors<1, kTm, kPlain> factors;
+                factors.load(a, v, m0, b - m0);
                 factors.template put<kBf16>(a, v, b, reinterpret_cast<const i32x4 (&)[1][kTm]>(acc[i]));
             }
+            // no load of this branch is left for the compiler to wait for after the other, where a wait is one for all stores
+            __builtin_amdgcn_s_waitcnt(0x0F70);     // vmcnt(0)
         }
     }
     if (wave < kWaves / 2) asm volatile("s_barrier" ::: "memory");
@@ -740,17 +768,28 @@ template <int kM, int kN, int kWavesM, int kWavesN, int kStages>
 void launch_small(HeadArgs a, bool bf16, bool gather_only, hipStream_t s) {
     shape_small<kM, kN>(a, gather_only);
     const dim3 grid((uint32_t)a.units), block(kWave * kWavesM * kWavesN);
-    if (bf16) hipLaunchKernelGGL((small_kernel<kM, kN, kWavesM, kWavesN, kStages, true>), grid, block, 0, s, a, gather_only);
-    else hipLaunchKernelGGL((small_kernel<kM, kN, kWavesM, kWavesN, kStages, false>), grid, block, 0, s, a, gather_only);
+    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a, gather_only); };
+    if (a.bitmask || a.bias) {
+        if (bf16) go(small_kernel<kM, kN, kWavesM, kWavesN, kStages, true, false>);
+        else go(small_kernel<kM, kN, kWavesM, kWavesN, kStages, false, false>);
+    } else {
+        if (bf16) go(small_kernel<kM, kN, kWavesM, kWavesN, kStages, true, true>);
+        else go(small_kernel<kM, kN, kWavesM, kWavesN, kStages, false, true>);
+    }
 }
 
 template <int kN, int kRing>
 void launch_wide(HeadArgs a, bool bf16, hipStream_t s) {
     a.m_tiles = up(a.B, 256);
     const dim3 grid((uint32_t)std::min<int64_t>(kComputeUnits, (int64_t)a.m_tiles * up(a.V, kN))), block(kWave * 8);
-    if (!bf16) hipLaunchKernelGGL((wide_kernel<kN, kRing, false, false>), grid, block, 0, s, a);
-    else if (a.bitmask || a.bias) hipLaunchKernelGGL((wide_kernel<kN, kRing, true, false>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((wide_kernel<kN, kRing, true, true>), grid, block, 0, s, a);
+    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
+    if (a.bitmask || a.bias) {
+        if (bf16) go(wide_kernel<kN, kRing, true, false>);
+        else go(wide_kernel<kN, kRing, false, false>);
+    } else {
+        if (bf16) go(wide_kernel<kN, kRing, true, true>);
+        else go(wide_kernel<kN, kRing, false, true>);
+    }
 }
 
 // Of the two widths of wide_kernel the one that ends first: rounds of tiles
@@ -758,7 +797,6 @@ void launch_wide(HeadArgs a, bool bf16, hipStream_t s) {
 // 4,096: 3 rounds of 256 take 221 us, 2 of 320 201; 2,048 x 128,256: 16 of 256
 // 922, 13 of 320 936.
 void launch_product(const HeadArgs &a, bool bf16, hipStream_t s) {
-    if (a.B <= 16) return launch_small<16, 16, 1, 1, 4>(a, bf16, false, s);
     if (a.B <= 32) return launch_small<32, 64, 1, 4, 4>(a, bf16, false, s);
     if (a.B <= 64) return launch_small<64, 128, 1, 4, 3>(a, bf16, false, s);
     if (a.B <= kWideRows) return launch_small<128, 128, 2, 4, 3>(a, bf16, false, s);
@@ -778,7 +816,7 @@ int32_t whole_steps(int32_t D) { return up(D, kStep) * kStep; }
 constexpr int32_t kMostArrivals = 2 * kComputeUnits;
 struct Workspace {
     size_t scales, counts, ids, arrivals, partials, total;
-    int64_t partials_most;
+    int32_t partials_most;
     Workspace(int32_t B, int32_t D, int32_t V) {
         const auto whole = [](size_t n) { return (n + 15) / 16 * 16; };
         const int64_t blocks = up(V, kBlockTokens);
@@ -788,7 +826,7 @@ struct Workspace {
         arrivals = ids + (blocks <= kMostBlocks ? blocks * kBlockTokens * sizeof(int32_t) : 0);
         partials = arrivals + kMostArrivals * sizeof(uint32_t);
         // twice the compute units' number of the largest tiles
-        partials_most = std::min<int64_t>((int64_t)kMostArrivals * 128 * 128, (int64_t)16 * up(B, 16) * 16 * (up(V, 128) * 128));
+        partials_most = (int32_t)std::min<int64_t>((int64_t)kMostArrivals * 128 * 128, (int64_t)16 * up(B, 16) * 16 * (up(V, 128) * 128));
         total = partials + (size_t)partials_most * sizeof(int32_t);
     }
 };
