@@ -608,8 +608,8 @@ typedef struct {
  *   v among the biases:                 x = x + value
  *   forbidden by `bitmask`:             x = -inf
  * in float32, rounded once to `dtype`.  A logit that is -inf stays so; logits
- * of which none of this is true are neither read nor written.  `penalties`
- * may be NULL.  B == 0 or V == 0 is a no-op.  Errors: PSC_E_INVALID_ARG,
+ * of which none of this is true keep their bits.  V * sizeof(logit) < 2^31.
+ * `penalties` may be NULL.  B == 0 or V == 0 is a no-op.  Errors: PSC_E_INVALID_ARG,
  * PSC_E_DEVICE.
  */
 psc_status psc_penalize(void *logits, psc_dtype dtype, int64_t stride, int32_t B, int32_t V,

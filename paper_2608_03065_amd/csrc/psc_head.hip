@@ -144,6 +144,8 @@ struct HeadArgs {
     int32_t arrivals_most;
 };
 
+constexpr int32_t kMostSplits = 8;
+
 // How a call is carried out: which columns (all tokens, or the needed ones),
 // and in how many parts of D each.  Every workgroup works it out alike.
 struct Plan {
@@ -161,7 +163,7 @@ __device__ __forceinline__ Plan plan_of(const HeadArgs &a, int32_t total) {
         p.tiles = (total + kN - 1) / kN;
         const int32_t tiles = max(p.tiles * a.m_tiles, 1);
         const int32_t room = tiles > a.arrivals_most ? 1 : a.partials_most / (tiles * kM * kN);
-        p.splits = max(1, min(min(a.units / tiles, room), min(a.steps / 2, 16)));
+        p.splits = max(1, min(min(a.units / tiles, room), min(a.steps / 2, kMostSplits)));
     }
     return p;
 }
@@ -187,7 +189,7 @@ __device__ __forceinline__ int32_t needed_upto(const HeadArgs &a, int lane, int3
 // tokens; as soon as a block has all of its bits, the other rows are not read.
 __device__ __forceinline__ void needed_block(const HeadArgs &a, int32_t block, int32_t *__restrict__ counts,
                                              int32_t *__restrict__ ids, uint32_t (*s_words)[kBlockWords]) {
-    constexpr int kWaves = kQuantBlock / kWave, kAhead = 8;
+    constexpr int kWaves = kQuantBlock / kWave, kAhead = 16;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int32_t w = block * kBlockWords + lane;
     const int32_t left = a.V - w * 32;        // tokens from the word's first on
@@ -258,6 +260,12 @@ __device__ __forceinline__ uint32_t load_word(__amdgpu_buffer_rsrc_t from, int32
     return __builtin_amdgcn_raw_buffer_load_b32(from, (uint32_t)at * 4u, 0, 0);
 }
 
+// The mask's words from row m0 on; nothing without a mask.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t mask_from(const HeadArgs &a, int32_t m0) {
+    const int64_t rows = a.bitmask ? min(a.B - m0, kMostRows) : 0;
+    return buffer_of(a.bitmask + (a.bitmask ? (int64_t)m0 * a.W : 0), (uint32_t)min(rows * a.W * 4, (int64_t)kMostBytes));
+}
+
 // What kTn by kTm blocks of 16 tokens by 16 states need besides their sums.
 // The lane's tokens of block i are v + 16 i .. + 3, its state of block j is
 // m0 + b + 16 j.  All of it is loaded at once, by small_kernel before the
@@ -272,8 +280,7 @@ struct Factors {
         const uint32_t tokens = (uint32_t)a.V * 4u;
         const __amdgpu_buffer_rsrc_t from_ws = buffer_of(a.w_scales, tokens), from_bias = buffer_of(a.bias, a.bias ? tokens : 0);
         const __amdgpu_buffer_rsrc_t from_xs = buffer_of(a.x_scales + m0, (uint32_t)min(a.B - m0, kMostRows) * 4u);
-        const __amdgpu_buffer_rsrc_t from_mask =
-            buffer_of(a.bitmask + (a.bitmask ? (int64_t)m0 * a.W : 0), a.bitmask ? (uint32_t)min((int64_t)min(a.B - m0, kMostRows) * a.W * 4, (int64_t)kMostBytes) : 0);
+        const __amdgpu_buffer_rsrc_t from_mask = mask_from(a, m0);
 #pragma unroll
         for (int j = 0; j < kTm; j++) xs[j] = __builtin_bit_cast(float, load_word(from_xs, b + j * 16));
 #pragma unroll
@@ -302,42 +309,19 @@ struct Factors {
     }
 };
 
-// One logit, if its row allows it.
-template <bool kBf16>
-__device__ __forceinline__ void put_if_allowed(const HeadArgs &a, int32_t b, int32_t v, int32_t sum, float xs, float ws, float bias) {
-    if (!((a.bitmask[(int64_t)b * a.W + (v >> 5)] >> (v & 31)) & 1)) return;
-    using T = typename Logit<kBf16>::type;
-    store_logit<kBf16>(static_cast<T *>(a.y) + (int64_t)b * a.y_stride, v, scaled(sum, xs, ws, bias));
-}
-
-// -inf in the forbidden logits and nothing else (the allowed ones are written
-// by other workgroups): piece by piece of 2,048 tokens of a row, eight of them
-// at once where they are all forbidden.
-template <bool kBf16>
-__device__ __forceinline__ void fill_forbidden(const HeadArgs &a, int64_t part, int64_t parts) {
-    using T = typename Logit<kBf16>::type;
-    const int32_t pieces = (a.V + kBlockTokens - 1) / kBlockTokens;
-    T inf[8];
-#pragma unroll
-    for (int e = 0; e < 8; e++) {
-        if constexpr (kBf16) inf[e] = 0xFF80u;
-        else inf[e] = kMinusInf;
-    }
-    for (int64_t u = part; u < (int64_t)a.B * pieces; u += parts) {
+// -inf in the forbidden logits and nothing else: the allowed ones are written
+// by other workgroups.  `part` of `parts` workgroups; each wavefront takes
+// kTiles tiles of a row at a time.
+template <bool kBf16, int kTiles>
+__device__ __forceinline__ void fill_forbidden(const HeadArgs &a, int32_t part, int32_t parts) {
+    constexpr int kElem = kBf16 ? 2 : 4;
+    const int32_t waves = (int32_t)blockDim.x / kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int32_t pieces = (tiles_of_row(a.V, kElem) + kTiles - 1) / kTiles;
+    const int64_t all = (int64_t)a.B * pieces;
+    for (int64_t u = (int64_t)part * waves + wave; u < all; u += (int64_t)parts * waves) {
         const int64_t b = u >> 32 ? u / pieces : (int64_t)((uint32_t)u / (uint32_t)pieces);
-        const int32_t v0 = (int32_t)(u - b * pieces) * kBlockTokens;
-        T *row = static_cast<T *>(a.y) + b * a.y_stride;
-        const uint32_t *words = a.bitmask + b * a.W;
-        for (int32_t v = v0 + (int32_t)threadIdx.x * 8; v < min(a.V, v0 + kBlockTokens); v += (int32_t)blockDim.x * 8) {
-            const uint32_t allowed = words[v >> 5] >> (v & 31) & 255;
-            if (allowed == 0 && v + 8 <= a.V) {
-                __builtin_memcpy(row + v, inf, sizeof inf);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; e++)
-                    if (!((allowed >> e) & 1) && v + e < a.V) row[v + e] = inf[0];
-            }
-        }
+        forbid_tiles<kBf16, kTiles>(static_cast<char *>(a.y) + b * a.y_stride * kElem, a.bitmask + b * a.W, a.V, a.W,
+                                    (int32_t)(u - b * pieces) * kTiles, threadIdx.x % kWave);
     }
 }
 
@@ -415,10 +399,13 @@ __device__ __forceinline__ void small_body(const HeadArgs &a, bool gather_only) 
     }
     Plan plan = plan_of<kM, kN>(a, total);
     if (kPlain) plan.gather = false;
-    if (plan.gather) fill_forbidden<kBf16>(a, blockIdx.x, gridDim.x);
-    else if (gather_only) return;
+    if (gather_only && !plan.gather) return;
+    const bool fill = plan.gather && !gather_only;        // else wide_kernel does it
     const int32_t tiles = plan.tiles * a.m_tiles;
-    if ((int32_t)blockIdx.x >= tiles * plan.splits) return;
+    if ((int32_t)blockIdx.x >= tiles * plan.splits) {
+        if (fill) fill_forbidden<kBf16, 1>(a, blockIdx.x, gridDim.x);
+        return;
+    }
     const int32_t split = (int32_t)blockIdx.x / tiles, tile = (int32_t)blockIdx.x - split * tiles;
     const int32_t m0 = tile % a.m_tiles * kM, n0 = tile / a.m_tiles * kN;
     const int32_t first = a.steps * split / plan.splits, steps = a.steps * (split + 1) / plan.splits;
@@ -471,6 +458,7 @@ __device__ __forceinline__ void small_body(const HeadArgs &a, bool gather_only) 
     if (!plan.gather && plan.splits == 1) factors.load(a, v0, m0, b0 - m0);
 #pragma unroll
     for (int s = 0; s < kStages - 1; s++) fetch(first + s);
+    if (fill) fill_forbidden<kBf16, 1>(a, blockIdx.x, gridDim.x);
     for (int32_t step = first; step < steps; step++) {
         wait_and_meet<(kStages - 2) * kLoads>();   // the step has landed, and its predecessor's buffer is free
         fetch(step + kStages - 1);
@@ -499,49 +487,81 @@ __device__ __forceinline__ void small_body(const HeadArgs &a, bool gather_only) 
         // The sums go to memory at device scope, which every XCD sees alike, and
         // only when they are there does the workgroup count itself in; the
         // last one of the tile reads them all.
-        int32_t *const sums = a.partials + (int64_t)tile * plan.splits * (kM * kN);
-        const auto place = [&](int32_t part, int i, int j, int e) {
-            return sums + (int64_t)part * (kM * kN) + ((i * kTm + j) * 4 + e) * (kWaves * kWave) + threadIdx.x;
-        };
+        constexpr uint32_t kPart = kM * kN * sizeof(int32_t);
+        constexpr int kDevice = 16;        // the accesses' scope (sc1)
+        const __amdgpu_buffer_rsrc_t sums = buffer_of(a.partials + (int64_t)tile * plan.splits * (kM * kN), (uint32_t)plan.splits * kPart);
+        const auto place = [&](int i, int j) { return (uint32_t)(((i * kTm + j) * kWaves * kWave + (int)threadIdx.x) * 16); };
 #pragma unroll
         for (int i = 0; i < kTn; i++)
 #pragma unroll
             for (int j = 0; j < kTm; j++)
-#pragma unroll
-                for (int e = 0; e < 4; e++)
-                    __hip_atomic_store(place(split, i, j, e), acc[i][j][e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[i][j]), sums, (uint32_t)split * kPart + place(i, j), 0, kDevice);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if (threadIdx.x == 0) s_arrived = __hip_atomic_fetch_add(a.arrivals + tile, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
         if (s_arrived != (uint32_t)plan.splits - 1) return;
         if (!plan.gather) factors.load(a, v0, m0, b0 - m0);
-        for (int32_t part = 0; part < plan.splits; part++) {
-            if (part == split) continue;
+        constexpr int kAtOnce = 4;
+        for (int32_t part = 0; part < plan.splits; part += kAtOnce) {
+            u32x4 t[kAtOnce][kTn][kTm];
 #pragma unroll
-            for (int i = 0; i < kTn; i++)
+            for (int n = 0; n < kAtOnce; n++)
 #pragma unroll
-                for (int j = 0; j < kTm; j++)
+                for (int i = 0; i < kTn; i++)
 #pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        acc[i][j][e] += __hip_atomic_load(place(part, i, j, e), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    for (int j = 0; j < kTm; j++) {
+                        // its own sum it has; parts that there are not give zeros
+                        const bool other = part + n < plan.splits && part + n != split;
+                        t[n][i][j] = __builtin_amdgcn_raw_buffer_load_b128(sums, other ? (uint32_t)(part + n) * kPart + place(i, j) : kNowhere, 0, kDevice);
+                    }
+#pragma unroll
+            for (int n = 0; n < kAtOnce; n++)
+#pragma unroll
+                for (int i = 0; i < kTn; i++)
+#pragma unroll
+                    for (int j = 0; j < kTm; j++) acc[i][j] += __builtin_bit_cast(i32x4, t[n][i][j]);
         }
     }
     if (!plan.gather) {
         factors.template put<kBf16>(a, v0, b0, acc);
         return;
     }
+    // few of a tile's logits are allowed: first all the bits, at once, then those
+    const __amdgpu_buffer_rsrc_t mask = mask_from(a, m0);
+    uint32_t allowed[kTm] = {};
 #pragma unroll
-    for (int i = 0; i < kTn; i++)
+    for (int i = 0; i < kTn; i++) {
+        uint32_t words[kTm][4];
+        int32_t v[4];
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-            const int32_t v = s_ids[(wn * kTn + i) * 16 + quad * 4 + e];
-            if (v < 0) continue;
-            const float ws = a.w_scales[v], bias = a.bias ? a.bias[v] : 0.0f;
+            v[e] = s_ids[(wn * kTn + i) * 16 + quad * 4 + e];
 #pragma unroll
             for (int j = 0; j < kTm; j++)
-                if (b0 + j * 16 < a.B) put_if_allowed<kBf16>(a, b0 + j * 16, v, acc[i][j][e], a.x_scales[b0 + j * 16], ws, bias);
+                words[j][e] = __builtin_amdgcn_raw_buffer_load_b32(mask, v[e] < 0 ? kNowhere : (uint32_t)((b0 - m0 + j * 16) * a.W + (v[e] >> 5)) * 4u, 0, 0);
         }
+#pragma unroll
+        for (int j = 0; j < kTm; j++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) allowed[j] |= (words[j][e] >> (v[e] & 31) & 1u) << (i * 4 + e);
+    }
+#pragma unroll
+    for (int j = 0; j < kTm; j++) {
+        const int32_t b = b0 + j * 16;
+        if (b >= a.B || !allowed[j]) continue;
+        const float xs = a.x_scales[b];
+        using T = typename Logit<kBf16>::type;
+        T *const row = static_cast<T *>(a.y) + (int64_t)b * a.y_stride;
+#pragma unroll
+        for (int i = 0; i < kTn; i++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                if (!((allowed[j] >> (i * 4 + e)) & 1)) continue;
+                const int32_t v = s_ids[(wn * kTn + i) * 16 + quad * 4 + e];
+                store_logit<kBf16>(row, v, scaled(acc[i][j][e], xs, a.w_scales[v], a.bias ? a.bias[v] : 0.0f));
+            }
+    }
 }
 
 template <int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kBf16, bool kPlain>
@@ -577,9 +597,12 @@ __device__ __forceinline__ void wide_body(const HeadArgs &a) {
     __shared__ __align__(1024) int8_t lds_w[kRing * kN * kStep], lds_x[2 * kM * kStep];
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int wm = wave % kWavesM, wn = wave / kWavesM;
-    if (a.counts) {
+    if (!kPlain && a.counts) {
         int32_t count[kShare];
-        if (lane_value(needed_upto(a, lane, count), kWave - 1) <= a.gather_most) return;      // small_kernel's
+        if (lane_value(needed_upto(a, lane, count), kWave - 1) <= a.gather_most) {
+            fill_forbidden<kBf16, 4>(a, blockIdx.x, gridDim.x);      // the product was small_kernel's
+            return;
+        }
     }
     const int32_t n_tiles = (a.V + kN - 1) / kN, tiles = n_tiles * a.m_tiles, whole = n_tiles / 8 * 8 * a.m_tiles;
     const auto corner = [&](int32_t id, int32_t &m0, int32_t &n0) {
@@ -674,12 +697,13 @@ __device__ __forceinline__ void wide_body(const HeadArgs &a) {
         int32_t m0, n0;
         corner(id, m0, n0);
         const int32_t v0 = n0 + wn * kTn * 16;       // the wavefront's first token
-        if (kBf16 && m0 + kM <= a.B && n0 + kN <= a.V) {
-            // Whole tiles of bfloat16: of two blocks of 16 tokens, lanes 16
-            // apart swap halves, so that each has eight consecutive tokens
-            // and a store writes 64 bytes of every state's row.
+        if (m0 + kM <= a.B && n0 + kN <= a.V) {
+            // Whole tiles.  A lane has four consecutive tokens of every block:
+            // 16 bytes of float32.  Of bfloat16 it gets eight: of two blocks
+            // of 16 tokens, lanes 16 apart swap halves.  Either way a store
+            // writes 64 bytes of every state's row.
             using T = typename Logit<kBf16>::type;
-            const int32_t mine = (quad & 1) * 16 + (quad >> 1) * 8;
+            const int32_t mine = kBf16 ? (quad & 1) * 16 + (quad >> 1) * 8 : quad * 4;
             float xs[kTm];
             T *to[kTm];
             const uint32_t *words[kTm];
@@ -693,6 +717,7 @@ __device__ __forceinline__ void wide_body(const HeadArgs &a) {
 #pragma unroll
             for (int p = 0; p < kPairs; p++) {
                 float ws[2][4], bias[2][4] = {};
+                uint32_t word[kTm];
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
                     const int32_t v = v0 + (2 * p + h) * 16 + quad * 4;
@@ -700,26 +725,42 @@ __device__ __forceinline__ void wide_body(const HeadArgs &a) {
                     if (!kPlain && a.bias) __builtin_memcpy(bias[h], a.bias + v, sizeof bias[h]);
                 }
 #pragma unroll
+                for (int j = 0; j < kTm; j++) word[j] = !kPlain && a.bitmask ? words[j][p] >> mine : ~0u;
+#pragma unroll
                 for (int j = 0; j < kTm; j++) {
-                    uint32_t o[2][2];
+                    float y[2][4];
 #pragma unroll
                     for (int h = 0; h < 2; h++)
 #pragma unroll
-                        for (int e = 0; e < 2; e++)
-                            o[h][e] = (uint32_t)to_bf16(scaled(acc[2 * p + h][j][2 * e], xs[j], ws[h][2 * e], bias[h][2 * e])) |
-                                      (uint32_t)to_bf16(scaled(acc[2 * p + h][j][2 * e + 1], xs[j], ws[h][2 * e + 1], bias[h][2 * e + 1])) << 16;
-                    const auto s0 = __builtin_amdgcn_permlane16_swap(o[0][0], o[1][0], false, false);
-                    const auto s1 = __builtin_amdgcn_permlane16_swap(o[0][1], o[1][1], false, false);
-                    u32x4 t = {(uint32_t)s0[0], (uint32_t)s1[0], (uint32_t)s0[1], (uint32_t)s1[1]};
-                    if (!kPlain && a.bitmask) {
-                        const uint32_t allowed = words[j][p] >> mine;
+                        for (int e = 0; e < 4; e++) y[h][e] = scaled(acc[2 * p + h][j][e], xs[j], ws[h][e], bias[h][e]);
+                    if constexpr (kBf16) {
+                        uint32_t o[2][2];
 #pragma unroll
-                        for (int e = 0; e < 4; e++) {
-                            const uint32_t keep = ((allowed >> (2 * e)) & 1 ? 0xFFFFu : 0u) | ((allowed >> (2 * e + 1)) & 1 ? 0xFFFF0000u : 0u);
-                            t[e] = (t[e] & keep) | (0xFF80FF80u & ~keep);
+                        for (int h = 0; h < 2; h++)
+#pragma unroll
+                            for (int e = 0; e < 2; e++)
+                                o[h][e] = (uint32_t)to_bf16(y[h][2 * e]) | (uint32_t)to_bf16(y[h][2 * e + 1]) << 16;
+                        const auto s0 = __builtin_amdgcn_permlane16_swap(o[0][0], o[1][0], false, false);
+                        const auto s1 = __builtin_amdgcn_permlane16_swap(o[0][1], o[1][1], false, false);
+                        u32x4 t = {(uint32_t)s0[0], (uint32_t)s1[0], (uint32_t)s0[1], (uint32_t)s1[1]};
+                        if (!kPlain)
+#pragma unroll
+                            for (int e = 0; e < 4; e++) {
+                                const uint32_t lo = (uint32_t)((int32_t)(word[j] << (31 - 2 * e)) >> 31);
+                                const uint32_t hi = (uint32_t)((int32_t)(word[j] << (30 - 2 * e)) >> 31);
+                                const uint32_t keep = (lo & 0xFFFFu) | (hi & 0xFFFF0000u);
+                                t[e] = (t[e] & keep) | (0xFF80FF80u & ~keep);
+                            }
+                        __builtin_memcpy(to[j] + p * 32, &t, sizeof t);
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < 2; h++) {
+                            if (!kPlain)
+#pragma unroll
+                                for (int e = 0; e < 4; e++) y[h][e] = (word[j] >> (h * 16 + e)) & 1 ? y[h][e] : kMinusInf;
+                            __builtin_memcpy(to[j] + p * 32 + h * 16, y[h], sizeof y[h]);
                         }
                     }
-                    __builtin_memcpy(to[j] + p * 32, &t, sizeof t);
                 }
             }
         } else {
@@ -747,7 +788,7 @@ wide_kernel(const HeadArgs a) {
 // ---------------------------------------------------------------- host side
 
 constexpr int32_t kComputeUnits = 256;
-constexpr int32_t kWideRows = 128;       // from here on, wide_kernel
+constexpr int32_t kWideRows = 128;
 
 int32_t up(int64_t n, int64_t d) { return (int32_t)((n + d - 1) / d); }
 
@@ -760,8 +801,8 @@ void shape_small(HeadArgs &a, bool gather_only) {
     // Parts of D where the tiles alone would leave compute units idle, of at
     // least four steps each.
     const int64_t room = tiles > a.arrivals_most ? 1 : a.partials_most / (tiles * kM * kN);
-    a.splits = gather_only ? 1 : (int32_t)std::max<int64_t>(1, std::min<int64_t>({2 * kComputeUnits / tiles, a.steps / 4, 16, room}));
-    a.units = (int32_t)std::max<int64_t>(tiles * a.splits, 2 * kComputeUnits);
+    a.splits = gather_only ? 1 : (int32_t)std::max<int64_t>(1, std::min<int64_t>({2 * kComputeUnits / tiles, a.steps / 4, kMostSplits, room}));
+    a.units = (int32_t)std::max<int64_t>(gather_only ? (int64_t)a.m_tiles * up(a.gather_most, kN) : tiles * a.splits, 2 * kComputeUnits);
 }
 
 template <int kM, int kN, int kWavesM, int kWavesN, int kStages>
@@ -792,6 +833,12 @@ void launch_wide(HeadArgs a, bool bf16, hipStream_t s) {
     }
 }
 
+// wide_kernel's calls: above kWideRows rows, unless its tiles would leave most
+// compute units idle.
+bool takes_wide(const HeadArgs &a) {
+    return a.B > kWideRows && (int64_t)up(a.B, 256) * up(a.V, 256) >= kComputeUnits / 2;
+}
+
 // Of the two widths of wide_kernel the one that ends first: rounds of tiles
 // over the compute units times a tile's width.  256 states x 151,936 tokens x
 // 4,096: 3 rounds of 256 take 221 us, 2 of 320 201; 2,048 x 128,256: 16 of 256
@@ -799,7 +846,7 @@ void launch_wide(HeadArgs a, bool bf16, hipStream_t s) {
 void launch_product(const HeadArgs &a, bool bf16, hipStream_t s) {
     if (a.B <= 32) return launch_small<32, 64, 1, 4, 4>(a, bf16, false, s);
     if (a.B <= 64) return launch_small<64, 128, 1, 4, 3>(a, bf16, false, s);
-    if (a.B <= kWideRows) return launch_small<128, 128, 2, 4, 3>(a, bf16, false, s);
+    if (!takes_wide(a)) return launch_small<128, 128, 2, 4, 3>(a, bf16, false, s);
     if (a.counts) launch_small<64, 128, 1, 4, 3>(a, bf16, true, s);
     const int64_t rounds256 = up((int64_t)up(a.B, 256) * up(a.V, 256), kComputeUnits),
                   rounds320 = up((int64_t)up(a.B, 256) * up(a.V, 320), kComputeUnits);
@@ -901,7 +948,8 @@ extern "C" psc_status psc_head_logits(const void *x, psc_dtype x_dtype, int64_t 
         a.blocks = up(V, kBlockTokens);
         a.counts = counts = reinterpret_cast<int32_t *>(at + ws.counts);
         a.ids = ids = reinterpret_cast<int32_t *>(at + ws.ids);
-        a.gather_most = V / 2;
+        // half of them; a quarter where wide_kernel, which is closer to the compute units' rate, takes all
+        a.gather_most = takes_wide(a) ? V / 4 : V / 2;
     }
     const dim3 grid((uint32_t)((int64_t)B + a.blocks)), block(kQuantBlock);
     int8_t *q = reinterpret_cast<int8_t *>(at);

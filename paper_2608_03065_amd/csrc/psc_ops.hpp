@@ -85,6 +85,72 @@ __device__ __forceinline__ void store_logit(void *row, int64_t v, float f) {
     else static_cast<float *>(row)[v] = f;
 }
 
+// ---------------------------------------------------------------- masking
+
+// Rows are masked in tiles of kTileBytes of memory, cut at 128-byte lines, so
+// that full lines are written whole whatever a row's alignment.
+constexpr int kTileBytes = 4096, kLineBytes = 128;
+constexpr int32_t tiles_of_row(int64_t V, int32_t elem) {      // for any alignment of the row
+    return (int32_t)((V * elem + kLineBytes - elem + kTileBytes - 1) / kTileBytes);
+}
+
+// -inf in the forbidden logits of tiles t0 .. t0 + kTiles - 1 of a row, by one
+// wavefront, with stores alone: other logits are neither read nor written.  The
+// words of all the tiles are loaded first.  Lane l has the bits of elements 32 l
+// .. 32 l + 31 of a tile, put together from the two words that they lie in; a
+// line that is forbidden whole is written in vectors, of the others 64
+// elements at a time, whose bits are the store's execution mask.
+template <bool kBf16, int kTiles>
+__device__ __forceinline__ void forbid_tiles(void *row, const uint32_t *__restrict__ words, int32_t V, int32_t W, int32_t t0, int lane) {
+    constexpr int kElem = kBf16 ? 2 : 4, kWords = kTileBytes / kElem / 32, kVecsPerWord = 2 * kElem;
+    const uintptr_t addr = reinterpret_cast<uintptr_t>(row);
+    char *const line = reinterpret_cast<char *>(addr & ~(uintptr_t)(kLineBytes - 1));
+    const int32_t delta = (int32_t)(addr & (kLineBytes - 1)) / kElem;      // elements of the line before the row
+    const int32_t before = (delta + 31) / 32, shift = before * 32 - delta;
+    uint32_t drop[kTiles];
+#pragma unroll
+    for (int i = 0; i < kTiles; i++) {
+        const int64_t w = (int64_t)(t0 + i) * kWords + lane - before;
+        const bool mine = lane < kWords;
+        const uint32_t lo = mine && w >= 0 && w < W ? words[w] : 0, hi = mine && shift && w >= -1 && w + 1 < W ? words[w + 1] : 0;
+        const int64_t p0 = ((int64_t)(t0 + i) * kWords + lane) * 32, left = (int64_t)delta + V - p0;
+        uint32_t inside = mine ? ~0u : 0u;
+        if (p0 < delta) inside &= delta - p0 >= 32 ? 0u : ~0u << (delta - p0);
+        if (left < 32) inside &= left <= 0 ? 0u : ~(~0u << left);
+        drop[i] = ~__builtin_amdgcn_alignbit(hi, lo, shift) & inside;
+    }
+    constexpr uint32_t kInf = kBf16 ? 0xFF80FF80u : 0xFF800000u;
+    // written through at device scope (16), whole lines as a stream (2): they need not stay in a cache
+    constexpr int kWhole = 16 | 2, kPart = 16;
+#pragma unroll
+    for (int i = 0; i < kTiles; i++) {
+        if (!__ballot(drop[i])) continue;
+        const __amdgpu_buffer_rsrc_t rsrc = buffer_of(line + (int64_t)(t0 + i) * kTileBytes, kTileBytes);
+        const uint32_t other = kBf16 ? dpp_from<0xB1, 0xF>(drop[i], 0u) : ~0u;      // a bfloat16 line is two words: the pair's other lane
+        const bool full = drop[i] == ~0u && other == ~0u;
+        const uint64_t lines = __ballot(full);
+        const u32x4 inf = {kInf, kInf, kInf, kInf};
+#pragma unroll
+        for (int j = 0; j < kTileBytes / 16 / kWave; j++) {
+            const int v = j * kWave + lane;
+            if ((lines >> (v / kVecsPerWord)) & 1) __builtin_amdgcn_raw_buffer_store_b128(inf, rsrc, (uint32_t)v * 16u, 0, kWhole);
+        }
+        const uint32_t rest = full ? 0u : drop[i];
+        const uint64_t some = __ballot(rest != 0);
+        if (!some) continue;
+#pragma unroll
+        for (int k = 0; k < kWords; k += 2) {
+            if (!((some >> k) & 3)) continue;
+            const uint64_t bits = lane_value(rest, k) | (uint64_t)lane_value(rest, k + 1) << 32;
+            if (__builtin_amdgcn_inverse_ballot_w64(bits)) {
+                const uint32_t at = (uint32_t)(k * 32 + lane) * kElem;
+                if (kBf16) __builtin_amdgcn_raw_buffer_store_b16((short)0xFF80, rsrc, at, 0, kPart);
+                else __builtin_amdgcn_raw_buffer_store_b32(0xFF800000u, rsrc, at, 0, kPart);
+            }
+        }
+    }
+}
+
 // ---------------------------------------------------------------- host side
 
 inline psc_status refuse(const char *what, const std::string &why) {

@@ -19,8 +19,6 @@ using namespace psc;
 namespace {
 
 constexpr int kScanBlock = 256;
-constexpr int kTileBytes = 4096;
-constexpr int kLineBytes = 128;
 constexpr int kGroup = 64;                          // tokens per group
 constexpr int kVecs = kTileBytes / 16 / kWave;      // 16-byte vectors per lane
 constexpr uint32_t kOffSkip = 0x80000000u;
@@ -531,9 +529,7 @@ pick_kernel(const SampleArgs a) {
     }
 }
 
-int32_t tiles_of(int32_t V, psc_dtype dtype) {
-    return (int32_t)(((int64_t)V * size_of(dtype) + kLineBytes - 1 + kTileBytes - 1) / kTileBytes);
-}
+int32_t tiles_of(int32_t V, psc_dtype dtype) { return tiles_of_row(V, (int32_t)size_of(dtype)); }
 
 template <bool kBf16>
 void launch_sample(const SampleArgs &a, int32_t B, hipStream_t s) {

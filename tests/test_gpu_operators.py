@@ -547,3 +547,43 @@ def test_head_logits_of_states_and_weights_that_lie_apart():
     scales = (torch.rand(700, generator=g) / 9000).to(DEV)
     y = head_exact(x, wide[:, :9000], scales)
     close(psc.head_logits(rows_apart(x.to(DEV), 7), wide[:, :9000], scales), y, head_bound(y, 0))
+
+
+@pytest.mark.parametrize("V,cap,biases", [(33, 64, 5), (513, 600, 9), (5000, 1500, 0), (4001, 4096, 40), (79616, 3000, 3),
+                                          (79617, 16000, 1024), (160001, 32767, 0), (90001, 40000, 7)])
+@pytest.mark.parametrize("dtype,masked,gap", [("bf16", True, 0), ("f32", True, 1), ("bf16", False, 3), ("f32", False, 0)])
+def test_penalize_rows_with_more_tokens_than_lines(V, cap, biases, dtype, masked, gap):
+    """Rows that are gone through in order, beside rows of few tokens in the same call; every alignment of a row."""
+    r, B = np.random.default_rng(cap), 9
+    x = torch.from_numpy(r.normal(0, 4, (B, V))).to(TYPES[dtype])
+    x[:, 3::13] = -math.inf
+    history = np.where(r.random((B, cap)) < 0.3, r.integers(0, 6, (B, cap)), r.integers(-3, V + 3, (B, cap))).astype(np.int32)
+    history[2] = V - 1                                # one token, cap times
+    lens = np.full(B, cap, np.int32)
+    lens[3], lens[4], lens[5] = 3, 0, cap // 2
+    prompts = np.array([0, cap, 1, 2, 0, 5, cap // 3, cap - 1, 1024], np.int32)
+    rep, pres, freq = r.uniform(0.8, 1.6, B), r.uniform(-1, 1, B), r.uniform(0, 0.5, B)
+    ids = r.integers(-1, V, (B, biases)).astype(np.int32)
+    if biases > 4:
+        ids[:, 3], ids[:, 1], ids[:, 4] = ids[:, 0], history[:, 0], V - 1
+    values = r.normal(0, 5, (B, biases))
+    words, keep = mask(B, V, cap, (0.5, 0.97, 1.0, 0.9, 0.02, 0.0)) if masked else (None, None)
+    t = lambda a: torch.from_numpy(a.astype(np.float32) if a.dtype == np.float64 else a).to(DEV)  # noqa: E731
+    back = lambda a: a.astype(np.float32).astype(np.float64)  # noqa: E731
+    got = rows_apart(x.to(DEV), gap)
+    psc.penalize(got, t(history), t(lens), prompt_lens=t(prompts), repetition=t(rep), presence=t(pres), frequency=t(freq),
+                 bias_ids=t(ids) if biases else None, bias_values=t(values) if biases else None, bitmask=words)
+    want, size = penalized(x.double().numpy(), history, lens, prompts, back(rep), back(pres), back(freq), ids, back(values),
+                           keep)
+    close(got, want, 8 * U * size)
+    assert around(got, gap)
+
+
+def test_penalize_in_order_leaves_other_logits_bits_alone():
+    x = torch.full((3, 900), -0.0, device=DEV)
+    x.view(torch.int32)[:, 5::2] = 0x7FC12345
+    before = x.view(torch.int32).clone()
+    history = (torch.arange(600, dtype=torch.int32, device=DEV) % 64 * 2).expand(3, 600).contiguous()
+    psc.penalize(x, history, torch.full((3,), 600, dtype=torch.int32, device=DEV), presence=torch.ones(3, device=DEV))
+    changed = (x.view(torch.int32) != before).nonzero().cpu().tolist()
+    assert changed == [[b, 2 * i] for b in range(3) for i in range(64)]
