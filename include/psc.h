@@ -572,8 +572,8 @@ psc_status psc_quantize_rows(const void *x, psc_dtype dtype, int64_t x_stride, i
  *             lies between D and w_stride does not matter.
  *  w_scales   float32 [V];  bias  float32 [V] or NULL.
  *  workspace  psc_head_workspace(B, D, V) bytes, 16-byte aligned.
- * 1 <= D <= 131,072 (up to there no sum can overflow).  B == 0 or V == 0 is a
- * no-op.  Errors: PSC_E_INVALID_ARG, PSC_E_DEVICE.
+ * 1 <= D <= 131,072 (up to there no sum can overflow), V <= 2^26.  B == 0 or V ==
+ * 0 is a no-op.  Errors: PSC_E_INVALID_ARG, PSC_E_DEVICE.
  */
 size_t psc_head_workspace(int32_t B, int32_t D, int32_t V);
 psc_status psc_head_logits(const void *x, psc_dtype x_dtype, int64_t x_stride, int32_t B, int32_t D,
@@ -651,8 +651,8 @@ typedef struct {
  * ids, id_logprobs and logprobs may be NULL.  A NaN counts above every number,
  * as in psc_compute_and_argmax; in a row whose best logit is NaN or +inf the
  * log-probabilities are NaN and the best token is taken.  1 <= k <= 64, B <=
- * 65,535, rows of at most 2 MiB; workspace: psc_sample_workspace bytes,
- * 16-byte aligned.  B == 0 is a no-op.  Errors: PSC_E_INVALID_ARG, PSC_E_DEVICE.
+ * 65,535, rows of at most 2 MiB less 128 bytes; workspace: psc_sample_workspace
+ * bytes, 16-byte aligned.  B == 0 is a no-op.  Errors: PSC_E_INVALID_ARG, PSC_E_DEVICE.
  */
 size_t psc_sample_workspace(int32_t B, int32_t V, psc_dtype dtype);
 psc_status psc_sample(const void *logits, psc_dtype dtype, int64_t stride, int32_t B, int32_t V,

@@ -855,6 +855,8 @@ void launch_product(const HeadArgs &a, bool bf16, hipStream_t s) {
 }
 
 constexpr int32_t kMostD = 131072;       // |sum| <= 127 * 128 * D stays below 2^31
+constexpr int32_t kMostV = 1 << 26;      // offsets into a tile's rows of the mask fit 32 bits
+static_assert((int64_t)kMostRows * (kMostV / 32) * 4 < kMostBytes, "and are inside a resource");
 int32_t whole_steps(int32_t D) { return up(D, kStep) * kStep; }
 
 // The workspace: quantised states [B][whole_steps(D)], their scales, the needed
@@ -901,7 +903,7 @@ extern "C" psc_status psc_quantize_rows(const void *x, psc_dtype dtype, int64_t 
 }
 
 extern "C" size_t psc_head_workspace(int32_t B, int32_t D, int32_t V) {
-    return B <= 0 || D <= 0 || D > kMostD || V <= 0 ? 0 : Workspace(B, D, V).total;
+    return B <= 0 || D <= 0 || D > kMostD || V <= 0 || V > kMostV ? 0 : Workspace(B, D, V).total;
 }
 
 extern "C" psc_status psc_head_logits(const void *x, psc_dtype x_dtype, int64_t x_stride, int32_t B, int32_t D,
@@ -912,6 +914,7 @@ extern "C" psc_status psc_head_logits(const void *x, psc_dtype x_dtype, int64_t 
     if (psc_status st = check_rows(what, logits, dtype, stride, B, V)) return st;
     if (!is_dtype(x_dtype)) return refuse(what, "bad dtype of x");
     if (D < 1 || D > kMostD) return refuse(what, "D outside [1, 131072]");
+    if (V > kMostV) return refuse(what, "V > 2^26");
     if (B == 0 || V == 0) return PSC_OK;
     if (!x || !w || !w_scales || !workspace) return refuse(what, "null pointer");
     if (x_stride < 0 || !aligned_to(x, size_of(x_dtype))) return refuse(what, "negative stride, or x off its elements' alignment");

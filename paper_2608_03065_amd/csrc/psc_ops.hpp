@@ -91,7 +91,7 @@ __device__ __forceinline__ void store_logit(void *row, int64_t v, float f) {
 // that full lines are written whole whatever a row's alignment.
 constexpr int kTileBytes = 4096, kLineBytes = 128;
 constexpr int32_t tiles_of_row(int64_t V, int32_t elem) {      // for any alignment of the row
-    return (int32_t)((V * elem + kLineBytes - elem + kTileBytes - 1) / kTileBytes);
+    return (int32_t)(((int64_t)V * elem + kLineBytes - elem + kTileBytes - 1) / kTileBytes);
 }
 
 // -inf in the forbidden logits of tiles t0 .. t0 + kTiles - 1 of a row, by one

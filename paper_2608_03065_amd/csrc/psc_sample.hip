@@ -543,7 +543,7 @@ void launch_sample(const SampleArgs &a, int32_t B, hipStream_t s) {
     else hipLaunchKernelGGL((pick_kernel<kBf16, 64>), rows, block, 0, s, a);
 }
 
-constexpr int32_t kMostTiles = kPickBlock * 64 / Row<true>::kTileGroups;       // 2 MiB of logits a row
+constexpr int32_t kMostTiles = kPickBlock * 64 / Row<true>::kTileGroups;       // 2 MiB of logits a row, less a line
 
 }  // namespace
 
@@ -563,7 +563,7 @@ extern "C" psc_status psc_sample(const void *logits, psc_dtype dtype, int64_t st
     if (B == 0) return PSC_OK;
     if (V == 0) return refuse(what, "an empty vocabulary");
     if (!tokens || !workspace) return refuse(what, "null pointer");
-    if (tiles_of(V, dtype) > kMostTiles) return refuse(what, "rows of more than 2 MiB");
+    if (tiles_of(V, dtype) > kMostTiles) return refuse(what, "rows of more than 2 MiB less 128 bytes");
     if (workspace_bytes < psc_sample_workspace(B, V, dtype) || !aligned_to(workspace, 16))
         return refuse(what, "the workspace is too small or not 16-byte aligned");
     SampleArgs a{};

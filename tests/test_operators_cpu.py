@@ -95,3 +95,21 @@ def test_the_binding_refuses_tensors_that_the_library_cannot_check():
                  lambda: psc.append_tokens(x, x, x)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_head_logits_refuses_vocabularies_whose_masks_pass_32_bit_offsets():
+    V = (1 << 26) + 1
+    assert psc.lib().psc_head_workspace(2, 64, V) == 0
+    assert head(V=V, stride=V) == INVALID and b"2^26" in psc.lib().psc_last_error()
+    # the last one that is taken gets as far as the workspace's check
+    assert head(V=V - 1, stride=V, ws_bytes=1) == INVALID and b"workspace" in psc.lib().psc_last_error()
+
+
+def test_sample_refuses_rows_past_two_mib_less_a_line():
+    most = ((2 << 20) - 128) // 2
+    assert sample(dtype=1, V=most + 2, stride=most + 2, ws_bytes=1) == INVALID and b"2 MiB" in psc.lib().psc_last_error()
+    assert sample(dtype=1, V=most, stride=most, ws_bytes=1) == INVALID and b"workspace" in psc.lib().psc_last_error()
+    # sizes in bytes that pass 32 bits
+    for V in (1 << 29, 1 << 30, (1 << 31) - 1):
+        for dtype in (0, 1):
+            assert sample(dtype=dtype, V=V, stride=V) == INVALID and b"2 MiB" in psc.lib().psc_last_error()
