@@ -99,7 +99,6 @@ template <bool kBf16>
 __global__ void __launch_bounds__(kScanBlock)
 scan_kernel(const SampleArgs a) {
     using R = Row<kBf16>;
-    constexpr uint32_t kAll = (1u << R::kPerVec) - 1;
     const int lane = threadIdx.x % kWave;
     const int64_t b = blockIdx.y;
     const int32_t t = blockIdx.x * (kScanBlock / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -271,21 +270,34 @@ __device__ uint32_t kth_key(const uint32_t (&key)[kPer], uint32_t k, PickShared 
     return lo;
 }
 
+// Places for each lane's n entries in a list of *count so far: the first of them.
+__device__ __forceinline__ uint32_t reserve(uint32_t *count, uint32_t n, int lane) {
+    const uint32_t upto = wave_scan(n, 0u, kAdd), all = lane_value(upto, kWave - 1);
+    uint32_t at = 0;
+    if (all && lane == 0) at = atomicAdd(count, all);
+    return lane_value(at, 0) + upto - n;
+}
+
+// The next two are for few rows, and calls, for pick_kernel's length is time in
+// every row: with both inlined it took 25 us for 256 rows of 8,000 float32, 12
+// without.  They take values only, as a reference to the kernel's arguments
+// would have them all copied to memory, and a caller passes a barrier after
+// them: the compiler may otherwise keep what it has read of LDS over the call.
+
 // Exactly the k best tokens into s.found, whatever the row: the k groups, then
 // k of their tokens, ties to the lower ones.  Groups and tokens are dealt to
 // the threads in ascending order, so that a sum over the threads before this
 // one is a place in that order.
 template <bool kBf16, int kPer>
-__device__ __attribute__((noinline)) void pick_exactly(const SampleArgs &a, int64_t b, PickShared &s) {
-    using R = Row<kBf16>;
+__device__ __attribute__((noinline)) void pick_exactly(Row<kBf16> row, const uint32_t *words, int32_t V, int32_t W, uint32_t k,
+                                                       int32_t groups, const uint32_t *keys, PickShared *shared) {
+    PickShared &s = *shared;
     const int tid = threadIdx.x;
-    const uint32_t k = (uint32_t)a.k;
-    const int32_t groups = a.tiles * R::kTileGroups;
     uint32_t key[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; i++) {
         const int32_t l = tid * kPer + i;
-        key[i] = l < groups ? a.group_keys[b * groups + l] : 0;
+        key[i] = l < groups ? keys[l] : 0;
     }
     s.found[tid] = 0;
     uint32_t above;
@@ -310,10 +322,9 @@ __device__ __attribute__((noinline)) void pick_exactly(const SampleArgs &a, int6
     int64_t v = 0;
     const uint32_t g = (uint32_t)tid / (kGroup / kMine);
     if (g < s.n_groups) {
-        const R row(a, b);
         const int64_t at = (int64_t)s.groups[g] * kGroup + (tid % (kGroup / kMine)) * kMine;
         v = at - row.delta;
-        const uint32_t keep = allowed_bits(a.bitmask ? a.bitmask + b * a.W : nullptr, v, kMine, a.V, a.W);
+        const uint32_t keep = allowed_bits(words, v, kMine, V, W);
 #pragma unroll
         for (int e = 0; e < kMine; e++)
             if ((keep >> e) & 1) mine[e] = key_of(load_logit<kBf16>(row.line, at + e));
@@ -336,12 +347,44 @@ __device__ __attribute__((noinline)) void pick_exactly(const SampleArgs &a, int6
     __syncthreads();
 }
 
-// Places for each lane's n entries in a list of *count so far: the first of them.
-__device__ __forceinline__ uint32_t reserve(uint32_t *count, uint32_t n, int lane) {
-    const uint32_t upto = wave_scan(n, 0u, kAdd), all = lane_value(upto, kWave - 1);
-    uint32_t at = 0;
-    if (all && lane == 0) at = atomicAdd(count, all);
-    return lane_value(at, 0) + upto - n;
+// s.found anew, where more than kMostFound of the groups' tokens have a key of
+// at least lo: those from a higher threshold on, found among the tokens' keys
+// themselves.  hi: the row's largest key.
+template <bool kBf16>
+__device__ __attribute__((noinline)) void thin_out(Row<kBf16> row, const uint32_t *words, int32_t V, uint32_t k, uint32_t lo, uint32_t hi,
+                                                   PickShared *shared) {
+    PickShared &s = *shared;
+    const int tid = threadIdx.x, lane = tid % kWave;
+    constexpr int kMine = kMostGroups * kGroup / kPickBlock;
+    const int32_t tokens = (int32_t)s.n_groups * kGroup;
+    uint32_t key[kMine];
+    const auto id_of = [&](int i) {
+        const int32_t n = i * kPickBlock + tid;
+        return n < tokens ? s.groups[n / kGroup] * kGroup + n % kGroup - row.delta : -1;
+    };
+#pragma unroll
+    for (int i = 0; i < kMine; i++) {
+        const int32_t v = id_of(i);
+        const bool is = v >= 0 && v < V;
+        const float x = is ? load_logit<kBf16>(row.line, (int64_t)v + row.delta) : 0;
+        key[i] = is && (!words || words[v >> 5] >> (v & 31) & 1) ? key_of(x) : 0;
+    }
+    __syncthreads();
+    s.found[tid] = 0;
+    if (tid == 0) s.n_found = 0;
+    uint32_t above = 0, in_bin;
+    do narrow<kMine>(key, k, s, lo, hi, above, in_bin);
+    while (above + in_bin > kMostFound && lo != hi);
+    uint32_t hits = 0;
+    static_assert(kMine <= 32, "a bit per token of a thread");
+#pragma unroll
+    for (int i = 0; i < kMine; i++) hits |= (uint32_t)(key[i] >= lo) << i;
+    uint32_t to = reserve(&s.n_found, __popc(hits), lane);
+    for (; hits; hits &= hits - 1, to++) {
+        const int32_t v = id_of(__ffs((int)hits) - 1);
+        if (to < kMostFound) s.found[to] = ranked(key_of(load_logit<kBf16>(row.line, (int64_t)v + row.delta)), v);
+    }
+    __syncthreads();
 }
 
 template <bool kBf16, int kPer>
@@ -400,11 +443,14 @@ pick_kernel(const SampleArgs a) {
         lo = max(lo, s.least[i]);
     }
     const bool some = hi != 0;
+    const uint32_t largest_key = hi;
     uint32_t above = 0, in_bin = 0;
-    // One round leaves little more than k groups, unless many maxima are equal
-    // or nearly so.  Where a row has fewer than k, all of them are taken.
+    // One round mostly leaves little more than k groups; where the keys' range
+    // crosses zero its bins are coarse.  Where a row has fewer than k, all of
+    // them are taken.
     if (some) {
-        narrow<kPer>(key, k, s, lo, hi, above, in_bin);
+        do narrow<kPer>(key, k, s, lo, hi, above, in_bin);
+        while (above + in_bin > kMostGroups && lo != hi);
         if (!in_bin) lo = 1;
     }
     {
@@ -419,9 +465,9 @@ pick_kernel(const SampleArgs a) {
     const uint32_t n_groups = s.n_groups;
     // their tokens, kMine at a time; every load is under way before the first is used
     constexpr int kMine = 8, kParts = kGroup / kMine, kTurns = kMostGroups * kParts / kPickBlock;
+    const R row(a, b);
+    const uint32_t *words = a.bitmask ? a.bitmask + b * a.W : nullptr;
     if (n_groups <= kMostGroups) {
-        const R row(a, b);
-        const uint32_t *words = a.bitmask ? a.bitmask + b * a.W : nullptr;
         constexpr int kVecsMine = kMine / R::kPerVec;
         const __amdgpu_buffer_rsrc_t rsrc = buffer_of(row.line, (uint32_t)a.tiles * kTileBytes);
         u32x4 x[kTurns][kVecsMine];
@@ -478,7 +524,14 @@ pick_kernel(const SampleArgs a) {
         }
     }
     __syncthreads();
-    if (n_groups > kMostGroups || s.n_found > kMostFound) pick_exactly<kBf16, kPer>(a, b, s);
+    if (s.n_found > kMostFound) {        // fewer than k groups, or many tokens about as large as the k-th
+        thin_out<kBf16>(row, words, a.V, k, lo, largest_key, &s);
+        __syncthreads();
+    }
+    if (n_groups > kMostGroups || s.n_found > kMostFound) {        // many equal ones
+        pick_exactly<kBf16, kPer>(row, words, a.V, a.W, k, groups, a.group_keys + b * groups, &s);
+        __syncthreads();
+    }
     // the place of every token found, by counting those before it
     const uint32_t n_found = s.n_found;
     if ((uint32_t)tid < n_found) {

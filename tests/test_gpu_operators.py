@@ -587,3 +587,39 @@ def test_penalize_in_order_leaves_other_logits_bits_alone():
     psc.penalize(x, history, torch.full((3,), 600, dtype=torch.int32, device=DEV), presence=torch.ones(3, device=DEV))
     changed = (x.view(torch.int32) != before).nonzero().cpu().tolist()
     assert changed == [[b, 2 * i] for b in range(3) for i in range(64)]
+
+
+# ---------------------------------------------------------------- sampling: thresholds that take more than one round
+
+@pytest.mark.parametrize("V,k", [(257, 64), (300, 20), (600, 50), (1000, 64), (3000, 50), (4096, 64), (8191, 64)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_sample_of_fewer_groups_than_k(V, k, dtype):
+    """Rows of up to k groups of 64 tokens, which all count: bells, one sign only, a NaN among them, ties at the k-th
+    place, a flat row, and few tokens of any size."""
+    r = np.random.default_rng(V + k)
+    x = r.normal(0, 2, (9, V))
+    x[1], x[2] = np.abs(x[1]) + 1, -np.abs(x[2]) - 1
+    x[3, [5, V - 1]] = np.nan
+    x[4] = np.round(x[4])
+    x[5] = 0.25
+    x[6, r.random(V) < 0.98] = -np.inf
+    x[7, ::2] = -np.inf
+    x[8] = np.where(r.random(V) < 0.3, 3.0, x[8])
+    gap = V % 3
+    check_sample(rows_apart(torch.from_numpy(x).to(TYPES[dtype]).to(DEV), gap), k,
+                 noise=(r.exponential(1, (9, k)) + 1e-9).astype(np.float32), temperature=np.full(9, 0.8, np.float32))
+    words, keep = mask(9, V, k, (0.9, 0.5))
+    check_sample(rows_apart(torch.from_numpy(x).to(TYPES[dtype]).to(DEV), gap), k, words, keep)
+
+
+@pytest.mark.parametrize("V", [20000, 32000, 70001, 151937])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_sample_of_sparse_rows_around_zero(V, dtype):
+    """Some tokens allowed, so that the groups' maxima lie on both sides of zero, densely and thinly."""
+    r = np.random.default_rng(V)
+    x = r.normal(0, 1, (8, V))
+    x[4:6] *= 1e-3
+    x[6] = np.where(r.random(V) < 0.5, 1e-6, -1e-6) * r.random(V)
+    words, keep = mask(8, V, 1, (0.04, 0.01, 0.02, 0.004))
+    for k in (1, 50, 64):
+        check_sample(torch.from_numpy(x).to(TYPES[dtype]).to(DEV), k, words, keep)
