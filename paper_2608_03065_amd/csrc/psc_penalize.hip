@@ -4,6 +4,7 @@
 #include "psc_ops.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 using namespace psc;
 
@@ -79,15 +80,23 @@ struct PenArgs {
 //  away changes its logit; a counter is cleared only where a token stands.  The
 //  mask is applied by tiles, with stores alone.  No branch parts the lanes on
 //  this way (what a lane has nothing to do with goes to a counter or an offset
-//  of nobody's), so that a lane's accesses are under way together.
+//  of nobody's), so that a lane's accesses are under way together.  Bound by
+//  them: each token reads and writes a piece of a line of its own, 256 rows of
+//  151,665 bf16 take 19 us with 1,000 tokens each, 36 with 4,000, 60 with 8,000.
 //
-//  At least four tokens per 128-byte line of the row (`in_order`): the history's
-//  tokens stand in no order, and going by them would fetch every line several
-//  times (256 rows of 151,665 bf16 with 8,000 tokens each on average, no mask:
-//  71 us).  Then each wavefront goes through counters in order, lists those that
-//  are not 0, and changes the listed logits two a lane, neighbours by neighbours.
-//  (Going through the logits themselves, 16 bytes with their counters at a time,
-//  took 73 us: its arithmetic is done for all the tokens that do not change.)
+//  At least 3.5 tokens per 128-byte line of the row (`in_order`): the history's
+//  tokens stand in no order, and going by them fetches every line several times.
+//  Then each wavefront goes through counters in order, lists those that are not
+//  0, and changes the listed logits two a lane, neighbours by neighbours: the
+//  same rows with 9,400 tokens take 50 us, the other way 73 (under masks of
+//  every kind 57 and 63; at 8,000 the ways are 55 and 58), where reading and
+//  writing all the logits takes 32.  (Three a lane took 65 for 62 us, for their
+//  list takes LDS from the counters.  Going through the logits themselves, 16
+//  bytes with their counters at a time, took 73: its arithmetic is done for all
+//  the tokens that do not change.)
+//
+// A workgroup takes all LDS of a compute unit; two or four a compute unit, with
+// fewer slices each, took 75 and 83 us for the 65 of this split.
 //
 // The biased tokens' logits are written by the threads that hold the biases,
 // which take their counters away before.
@@ -117,11 +126,17 @@ penalize_kernel(const PenArgs a) {
     if (a.lens) n = min(max(a.lens[b], 0), a.cap);
     if (counts) {
         if (a.lens) {
-            // what lies past the history's end, in the buffer, is loaded and not used
-            const __amdgpu_buffer_rsrc_t rsrc = buffer_of(history, (uint32_t)min((int64_t)a.cap * 4, (int64_t)kHeld * kPenBlock * 4));
+            // The first ones are loaded before the length is known: what lies past
+            // the history's end, in the buffer, is not used.
+            constexpr int kFirst = kHeld < 4 ? kHeld : 4;
+            const __amdgpu_buffer_rsrc_t rsrc = buffer_of(history, (uint32_t)min(a.cap, kFirst * kPenBlock) * 4u);
 #pragma unroll
-            for (int k = 0; k < kHeld; k++)
+            for (int k = 0; k < kFirst; k++)
                 held[k] = (int32_t)__builtin_amdgcn_raw_buffer_load_b32(rsrc, (uint32_t)(k * kPenBlock + tid) * 4u, 0, 0);
+            const __amdgpu_buffer_rsrc_t rest = buffer_of(history, (uint32_t)min(n, kHeld * kPenBlock) * 4u);
+#pragma unroll
+            for (int k = kFirst; k < kHeld; k++)
+                held[k] = (int32_t)__builtin_amdgcn_raw_buffer_load_b32(rest, (uint32_t)(k * kPenBlock + tid) * 4u, 0, 0);
             prompt = a.prompt_lens ? min(max(a.prompt_lens[b], 0), n) : 0;
         }
         if (a.repetition) r = a.repetition[b];
@@ -134,7 +149,7 @@ penalize_kernel(const PenArgs a) {
         }
         if (a.n_bias) s_bias_ids[tid] = bias_id;
     }
-    const bool in_order = (int64_t)n * kLineBytes >= 4 * (int64_t)a.V * kElem;
+    const bool in_order = 2 * (int64_t)n * kLineBytes >= 7 * (int64_t)a.V * kElem;
     if (words) {
         const int32_t pieces = (tiles_of_row(a.V, kElem) + kMaskTiles - 1) / kMaskTiles;
         for (int32_t u = part * kPenWaves + wave; u < pieces; u += parts * kPenWaves)
@@ -289,24 +304,45 @@ penalize_kernel(const PenArgs a) {
             __syncthreads();
             continue;
         }
-        uint32_t count[kHeld], word[kHeld];
-        float x[kHeld];
+        // kGroup of the held tokens together from the g-th on; of all 16 at once
+        // the values would not fit the registers.
+        const auto change_held = [&](auto group, int g) {
+            constexpr int kGroup = decltype(group)::value;
+            uint32_t count[kGroup], word[kGroup];
+            float x[kGroup];
 #pragma unroll
-        for (int k = 0; k < kHeld; k++) count[k] = k * kPenBlock < n ? counters.take(place(held[k], k * kPenBlock + tid < n)) : 0;
-        // nothing is loaded of logits that another occurrence or a bias has taken, or that are forbidden
+            for (int e = 0; e < kGroup; e++) {
+                const int k = g + e;
+                count[e] = k * kPenBlock < n ? counters.take(place(held[k], k * kPenBlock + tid < n)) : 0;
+            }
+            // nothing is loaded of logits that another occurrence or a bias has taken, or that are forbidden
 #pragma unroll
-        for (int k = 0; k < kHeld; k++) {
-            const bool mine = k * kPenBlock + tid < n && place(held[k], true) < size;
-            count[k] = mine ? count[k] : 0;
-            word[k] = word_at(held[k] >> 5, count[k] != 0);
+            for (int e = 0; e < kGroup; e++) {
+                const int k = g + e;
+                const bool mine = k * kPenBlock + tid < n && place(held[k], true) < size;
+                count[e] = mine ? count[e] : 0;
+                word[e] = word_at(held[k] >> 5, count[e] != 0);
+            }
+#pragma unroll
+            for (int e = 0; e < kGroup; e++) {
+                const int32_t t = held[g + e];
+                count[e] = word[e] >> (t & 31) & 1 ? count[e] : 0;
+                x[e] = load(t, count[e] != 0);
+            }
+#pragma unroll
+            for (int e = 0; e < kGroup; e++) store(held[g + e], count[e] != 0 && x[e] != kMinusInf, changed(x[e], count[e], 0.0f));
+        };
+        // Accesses to nowhere cost time too: a short history in a long buffer goes
+        // alone (256 rows of 500 tokens of 16,384: 10.7 us, by eight 13.4).
+        if (n <= kPenBlock) {
+            change_held(std::integral_constant<int, 1>{}, 0);
+        } else if constexpr (kHeld == 4) {
+            change_held(std::integral_constant<int, 4>{}, 0);
+        } else if constexpr (kHeld == 16) {
+            change_held(std::integral_constant<int, 8>{}, 0);
+            if (n > 8 * kPenBlock) change_held(std::integral_constant<int, 8>{}, 8);
         }
-#pragma unroll
-        for (int k = 0; k < kHeld; k++) {
-            count[k] = word[k] >> (held[k] & 31) & 1 ? count[k] : 0;
-            x[k] = load(held[k], count[k] != 0);
-        }
-#pragma unroll
-        for (int k = 0; k < kHeld; k++) store(held[k], count[k] != 0 && x[k] != kMinusInf, changed(x[k], count[k], 0.0f));
+        static_assert(kHeld == 1 || kHeld == 4 || kHeld == 16, "the numbers handled here");
         for (int32_t i = kHeld * kPenBlock + tid; i < n; i += kPenBlock) {
             const int32_t t = history[i];
             const uint32_t at = place(t, true);
