@@ -700,6 +700,12 @@ def _rows(t, name: str, dev: int | None = None, shape: tuple | None = None):
     """(dtype code, row stride) of t, a float32 or bfloat16 matrix on the
     current device whose rows do not overlap and whose elements are adjacent."""
     T = _T or _torch_types()
+    if type(t) is T["tensor"] and t.dim() == 2:      # no message is put together on the common path
+        (rows, cols), (apart, step) = t.shape, t.stride()
+        code, at = T["codes"].get(t.dtype), t.get_device()
+        if (code is not None and (shape is None or (rows, cols) == shape) and step == 1 and apart >= cols
+                and at >= 0 and at == T["device"]() and (dev is None or at == dev)):
+            return code, apart if rows > 1 else cols
     _require(isinstance(t, T["tensor"]) and t.dim() == 2, f"{name} to be a matrix")
     code = T["codes"].get(t.dtype)
     _require(code is not None, f"float32 or bfloat16 {name}, not {t.dtype}")
@@ -758,15 +764,16 @@ def head_logits(x, w, w_scales, dtype=None, bias=None, bitmask=None, out=None, s
     x_code, x_stride = _rows(x, "x")
     B, D = x.shape
     dev = x.get_device()
-    _require(isinstance(w, T["tensor"]) and w.dtype is T["i8"] and w.dim() == 2 and w.shape[1] == D and D > 0,
-             f"w to be an int8 matrix of rows of {D} elements")
+    if not (isinstance(w, T["tensor"]) and w.dtype is T["i8"] and w.dim() == 2 and w.shape[1] == D and D > 0):
+        _require(False, f"w to be an int8 matrix of rows of {D} elements")
     V = w.shape[0]
     w_stride = w.stride(0) if V > 1 else (D + 15) // 16 * 16
     _require(w.get_device() == dev and (D == 1 or w.stride(1) == 1) and w_stride >= D and w_stride % 16 == 0
              and w.data_ptr() % 16 == 0, "w on x's device, with adjacent elements and rows that start at 16 bytes")
     if out is None:
         code, y_stride = T["codes"].get(x.dtype if dtype is None else dtype), V
-        _require(code is not None, f"float32 or bfloat16 logits, not {dtype}")
+        if code is None:
+            _require(False, f"float32 or bfloat16 logits, not {dtype}")
         out = _new((B, V), ("f32", "bf16")[code], x.device, stream)
     else:
         _require(dtype is None or dtype == out.dtype, "dtype to be that of out")
@@ -834,7 +841,8 @@ def sample(logits, k, bitmask=None, temperature=None, top_k=None, top_p=None, mi
     code, stride = _rows(logits, "logits")
     (B, V), dev = logits.shape, logits.get_device()
     k = int(k)
-    _require(1 <= k <= SAMPLE_MAX_K, f"k in [1, {SAMPLE_MAX_K}]")
+    if not 1 <= k <= SAMPLE_MAX_K:
+        _require(False, f"k in [1, {SAMPLE_MAX_K}]")
     _require(V > 0, "logits of at least one token")
     rows = (B,)
     p = _Sampling(_vector(temperature, "temperature", "f32", dev, rows), _vector(top_k, "top_k", "i32", dev, rows),
