@@ -93,12 +93,12 @@ struct Row {
 // Bits of the `count` tokens from v on (v may be negative): 1 where a token
 // is in the vocabulary and allowed.  Without branches, so that the words' loads
 // overlap what else is loaded.
-__device__ __forceinline__ uint32_t allowed_bits(const uint32_t *__restrict__ words, int64_t v, int count, int32_t V, int32_t W) {
+__device__ __forceinline__ uint32_t allowed_bits(const uint32_t *__restrict__ words, int32_t v, int count, int32_t V, int32_t W) {
     uint32_t in = (1u << count) - 1;
     if (v < 0) in = v > -count ? in & ~0u << -v : 0;
     if (v + count > V) in = v < V ? in & ((1u << (V - v)) - 1) : 0;
     if (!words) return in;
-    const int32_t w = (int32_t)(v >> 5), last = W - 1;
+    const int32_t w = v >> 5, last = W - 1;
     const uint32_t lo = words[min(max(w, 0), last)], hi = words[min(max(w + 1, 0), last)];
     return __builtin_amdgcn_alignbit(hi, lo, (uint32_t)v & 31) & in;
 }
@@ -114,7 +114,7 @@ scan_kernel(const SampleArgs a) {
     const R row(a, b);
     const char *tile = row.line + (int64_t)t * kTileBytes;
     const uint32_t *words = a.bitmask ? a.bitmask + b * a.W : nullptr;
-    const float c = inverse_temperature(a.temperature, b);
+    const float c = inverse_temperature(a.temperature, b) * kLog2e;
     const __amdgpu_buffer_rsrc_t rsrc = buffer_of(tile, kTileBytes);
     uint32_t keep[kVecs];
     u32x4 x[kVecs];
@@ -122,7 +122,7 @@ scan_kernel(const SampleArgs a) {
 #pragma unroll
     for (int j = 0; j < kVecs; j++) {
         const int at = (j * kWave + lane) * R::kPerVec;
-        const int64_t v = (int64_t)t * (kTileBytes / R::kElem) + at - row.delta;
+        const int32_t v = t * (kTileBytes / R::kElem) + at - row.delta;
         keep[j] = allowed_bits(words, v, R::kPerVec, a.V, a.W);
         // a vector that reaches out of the row is read by element
         const bool whole = v >= 0 && v + R::kPerVec <= a.V;
@@ -133,7 +133,7 @@ scan_kernel(const SampleArgs a) {
 #pragma unroll
         for (int j = 0; j < kVecs; j++) {
             const int at = (j * kWave + lane) * R::kPerVec;
-            const int64_t v = (int64_t)t * (kTileBytes / R::kElem) + at - row.delta;
+            const int32_t v = t * (kTileBytes / R::kElem) + at - row.delta;
             if (!keep[j] || (v >= 0 && v + R::kPerVec <= a.V)) continue;
 #pragma unroll
             for (int e = 0; e < R::kPerVec; e++) {
@@ -143,9 +143,23 @@ scan_kernel(const SampleArgs a) {
             }
         }
     }
+    // -inf in place of what is not allowed; most tiles without a mask have none
+    constexpr uint32_t kWhole = (1u << R::kPerVec) - 1;
+    bool part = false;
+#pragma unroll
+    for (int j = 0; j < kVecs; j++) part |= keep[j] != kWhole;
+    if (__ballot(part)) {
+#pragma unroll
+        for (int j = 0; j < kVecs; j++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const auto bit = [&](int i) { return (uint32_t)((int32_t)(keep[j] << (31 - i)) >> 31); };
+                const uint32_t is = kBf16 ? (bit(2 * e) & 0xFFFFu) | (bit(2 * e + 1) & 0xFFFF0000u) : bit(e);
+                x[j][e] = (x[j][e] & is) | ((kBf16 ? 0xFF80FF80u : 0xFF800000u) & ~is);
+            }
+    }
     const auto value = [&](int j, int e) {
-        const uint32_t u = kBf16 ? (e % 2 ? x[j][e / 2] & 0xFFFF0000u : x[j][e / 2] << 16) : x[j][e];
-        return (keep[j] >> e) & 1 ? __builtin_bit_cast(float, u) : kMinusInf;
+        return __builtin_bit_cast(float, kBf16 ? (e % 2 ? x[j][e / 2] & 0xFFFF0000u : x[j][e / 2] << 16) : x[j][e]);
     };
     float most = kMinusInf;
     uint32_t *keys = a.group_keys + (b * a.tiles + t) * R::kTileGroups;
@@ -168,7 +182,7 @@ scan_kernel(const SampleArgs a) {
 #pragma unroll
         for (int j = 0; j < kVecs; j++)
 #pragma unroll
-            for (int e = 0; e < R::kPerVec; e++) sum += exp_scaled(value(j, e) - most, c);
+            for (int e = 0; e < R::kPerVec; e++) sum += __builtin_amdgcn_exp2f((value(j, e) - most) * c);
     }
     sum = wave_all(sum, 0.0f, kAdd);
     if (lane == 0) a.parts[b * a.tiles + t] = make_float2(most, sum);
@@ -327,10 +341,10 @@ __device__ __attribute__((noinline)) void pick_exactly(Row<kBf16> row, const uin
     __syncthreads();
     constexpr int kMine = kMostK * kGroup / kPickBlock;
     uint32_t mine[kMine] = {};
-    int64_t v = 0;
+    int32_t v = 0;
     const uint32_t g = (uint32_t)tid / (kGroup / kMine);
     if (g < s.n_groups) {
-        const int64_t at = (int64_t)s.groups[g] * kGroup + (tid % (kGroup / kMine)) * kMine;
+        const int32_t at = s.groups[g] * kGroup + (tid % (kGroup / kMine)) * kMine;
         v = at - row.delta;
         const uint32_t keep = allowed_bits(words, v, kMine, V, W);
 #pragma unroll
@@ -347,7 +361,7 @@ __device__ __attribute__((noinline)) void pick_exactly(Row<kBf16> row, const uin
 #pragma unroll
     for (int e = 0; e < kMine; e++) {
         const bool more = mine[e] > t, same = mine[e] == t && t;
-        if (more || (same && eq < quota)) s.found[gt + min(eq, quota)] = ranked(mine[e], (int32_t)(v + e));
+        if (more || (same && eq < quota)) s.found[gt + min(eq, quota)] = ranked(mine[e], v + e);
         gt += more;
         eq += same;
     }
