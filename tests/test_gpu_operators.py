@@ -623,3 +623,26 @@ def test_sample_of_sparse_rows_around_zero(V, dtype):
     words, keep = mask(8, V, 1, (0.04, 0.01, 0.02, 0.004))
     for k in (1, 50, 64):
         check_sample(torch.from_numpy(x).to(TYPES[dtype]).to(DEV), k, words, keep)
+
+
+@pytest.mark.parametrize("V,cap", [(262145, 30000), (262145, 4096), (262145, 1024), (300001, 40000)])
+@pytest.mark.parametrize("dtype,masked", [("f32", True), ("bf16", False)])
+def test_penalize_by_the_history_at_every_length(V, cap, dtype, masked):
+    """Rows of few tokens a line, with lengths on both sides of what threads hold at once and change together."""
+    r = np.random.default_rng(V + cap)
+    lens = np.array([n for n in (1, 500, 1023, 1024, 1025, 4095, 4096, 4097, 8191, 8192, 8193, 16383, 16384, 16385, 28000)
+                     if n <= cap], np.int32)
+    B = lens.size
+    x = torch.from_numpy(r.normal(0, 4, (B, V))).to(TYPES[dtype])
+    history = np.where(r.random((B, cap)) < 0.2, r.integers(0, 9, (B, cap)), r.integers(-3, V + 3, (B, cap))).astype(np.int32)
+    prompts = (lens * r.random(B)).astype(np.int32)
+    rep, pres, freq = (a.astype(np.float32) for a in (r.uniform(0.8, 1.6, B), r.uniform(-1, 1, B), r.uniform(0, 0.5, B)))
+    words, keep = mask(B, V, cap, (0.5, 0.97, 0.02)) if masked else (None, None)
+    t = lambda a: torch.from_numpy(a).to(DEV)  # noqa: E731
+    got = rows_apart(x.to(DEV), 3)
+    psc.penalize(got, t(history), t(lens), prompt_lens=t(prompts), repetition=t(rep), presence=t(pres), frequency=t(freq),
+                 bitmask=words)
+    want, size = penalized(x.double().numpy(), history, lens, prompts, *(a.astype(np.float64) for a in (rep, pres, freq)),
+                           keep=keep)
+    close(got, want, 8 * U * size)
+    assert around(got, 3)
