@@ -554,7 +554,8 @@ psc_status psc_compute_and_argmax_dense(const psc_handle *h, const int32_t *stac
  * elements apart; rows of q are q_stride bytes apart, a multiple of 16 and
  * >= D, start at 16-byte addresses, and their bytes from D up to the next
  * multiple of 16 become zeros.  For the weights of psc_head_logits (once, a
- * row per token) and other operands of the kind.  n_rows == 0 is a no-op.
+ * row per token) and other operands of the kind.  n_rows < 2^31; n_rows == 0 is
+ * a no-op.
  * Errors: PSC_E_INVALID_ARG, PSC_E_DEVICE.
  */
 psc_status psc_quantize_rows(const void *x, psc_dtype dtype, int64_t x_stride, int64_t n_rows, int32_t D,
@@ -572,8 +573,9 @@ psc_status psc_quantize_rows(const void *x, psc_dtype dtype, int64_t x_stride, i
  *             lies between D and w_stride does not matter.
  *  w_scales   float32 [V];  bias  float32 [V] or NULL.
  *  workspace  psc_head_workspace(B, D, V) bytes, 16-byte aligned.
- * 1 <= D <= 131,072 (up to there no sum can overflow), V <= 2^26.  B == 0 or V ==
- * 0 is a no-op.  Errors: PSC_E_INVALID_ARG, PSC_E_DEVICE.
+ * 1 <= D <= 131,072 (up to there no sum can overflow), V <= 2^26, ceil(B / 64) *
+ * ceil(V / 512) < 2^24.  B == 0 or V == 0 is a no-op.  Errors: PSC_E_INVALID_ARG,
+ * PSC_E_DEVICE.
  */
 size_t psc_head_workspace(int32_t B, int32_t D, int32_t V);
 psc_status psc_head_logits(const void *x, psc_dtype x_dtype, int64_t x_stride, int32_t B, int32_t D,

@@ -225,17 +225,17 @@ __device__ __forceinline__ void needed_block(const HeadArgs &a, int32_t block, i
     for (; any; any &= any - 1) *to++ = w * 32 + __ffs((int)any) - 1;
 }
 
-// Workgroups 0 .. B - 1: a row of states each; the others a block of needed
+// Workgroups 0 .. rows - 1: a row of states each; the others a block of needed
 // tokens each; all of them clear the arrival counters.
 template <bool kBf16>
 __global__ void __launch_bounds__(kQuantBlock)
-prepare_kernel(const HeadArgs a, const void *__restrict__ x, int64_t x_stride, int8_t *__restrict__ q,
+prepare_kernel(const HeadArgs a, int32_t rows, const void *__restrict__ x, int64_t x_stride, int8_t *__restrict__ q,
                float *__restrict__ scales, int32_t *__restrict__ counts, int32_t *__restrict__ ids) {
     __shared__ uint32_t shared[kQuantBlock / kWave][kBlockWords];
     for (int64_t i = (int64_t)blockIdx.x * kQuantBlock + threadIdx.x; i < a.arrivals_most; i += (int64_t)gridDim.x * kQuantBlock)
         a.arrivals[i] = 0;
-    if ((int64_t)blockIdx.x < a.B) quantize_row<kBf16>(x, x_stride, blockIdx.x, a.D, (int32_t)a.x_stride, q, a.x_stride, scales, shared[0]);
-    else needed_block(a, (int32_t)(blockIdx.x - a.B), counts, ids, shared);
+    if ((int32_t)blockIdx.x < rows) quantize_row<kBf16>(x, x_stride, blockIdx.x, a.D, (int32_t)a.x_stride, q, a.x_stride, scales, shared[0]);
+    else needed_block(a, (int32_t)blockIdx.x - rows, counts, ids, shared);
 }
 
 // ---------------------------------------------------------------- results
@@ -799,6 +799,32 @@ constexpr int32_t kWideRows = 128;
 
 int32_t up(int64_t n, int64_t d) { return (int32_t)((n + d - 1) / d); }
 
+// Workgroups of one launch: a grid's threads are fewer than 2^32 in each dimension.
+constexpr int64_t kMostGrid = ((int64_t)1 << 32) / kQuantBlock - 1;
+
+// Rows to 8 bits, a workgroup each, in as many launches as that takes.
+void launch_quantize(const void *x, psc_dtype dtype, int64_t x_stride, int64_t n_rows, int32_t D, int32_t padded, int8_t *q,
+                     int64_t q_stride, float *scales, hipStream_t s) {
+    for (int64_t r = 0; r < n_rows; r += kMostGrid) {
+        const dim3 grid((uint32_t)std::min(kMostGrid, n_rows - r)), block(kQuantBlock);
+        const void *from = static_cast<const char *>(x) + r * x_stride * size_of(dtype);
+        const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, from, x_stride, D, padded, q + r * q_stride, q_stride, scales + r); };
+        if (dtype == PSC_BF16) go(quantize_kernel<true>);
+        else go(quantize_kernel<false>);
+    }
+}
+
+// prepare_kernel with the rows that fit beside the blocks, then the others alone.
+void launch_prepare(const HeadArgs &a, const void *x, psc_dtype dtype, int64_t x_stride, int8_t *q, float *scales, int32_t *counts,
+                    int32_t *ids, hipStream_t s) {
+    const int32_t rows = (int32_t)std::min<int64_t>(a.B, kMostGrid - a.blocks);
+    const dim3 grid((uint32_t)(rows + a.blocks)), block(kQuantBlock);
+    if (dtype == PSC_BF16) hipLaunchKernelGGL(prepare_kernel<true>, grid, block, 0, s, a, rows, x, x_stride, q, scales, counts, ids);
+    else hipLaunchKernelGGL(prepare_kernel<false>, grid, block, 0, s, a, rows, x, x_stride, q, scales, counts, ids);
+    launch_quantize(static_cast<const char *>(x) + rows * x_stride * size_of(dtype), dtype, x_stride, a.B - rows, a.D, (int32_t)a.x_stride,
+                    q + rows * a.x_stride, a.x_stride, scales + rows, s);
+}
+
 // How small_kernel is launched: its tiles of kM by kN, the parts of D, and the
 // workgroups, of which there are enough to split D further when few tokens are needed.
 template <int kM, int kN>
@@ -809,6 +835,7 @@ void shape_small(HeadArgs &a, bool gather_only) {
     // least four steps each.
     const int64_t room = tiles > a.arrivals_most ? 1 : a.partials_most / (tiles * kM * kN);
     a.splits = gather_only ? 1 : (int32_t)std::max<int64_t>(1, std::min<int64_t>({2 * kComputeUnits / tiles, a.steps / 4, kMostSplits, room}));
+    // the entry point has seen to it that units of 256 threads fit a launch (V / 4 tokens at most, where only needed ones are taken)
     a.units = (int32_t)std::max<int64_t>(gather_only ? (int64_t)a.m_tiles * up(a.gather_most, kN) : tiles * a.splits, 2 * kComputeUnits);
 }
 
@@ -904,10 +931,7 @@ extern "C" psc_status psc_quantize_rows(const void *x, psc_dtype dtype, int64_t 
     if (x_stride < 0 || !aligned_to(x, size_of(dtype))) return refuse(what, "negative stride, or x off its elements' alignment");
     if (q_stride % kChunk || q_stride < padded || !aligned_to(q, kChunk))
         return refuse(what, "rows of q start at 16 bytes and hold D elements");
-    const dim3 grid((uint32_t)n_rows), block(kQuantBlock);
-    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    if (dtype == PSC_BF16) hipLaunchKernelGGL(quantize_kernel<true>, grid, block, 0, s, x, x_stride, D, (int32_t)padded, q, q_stride, scales);
-    else hipLaunchKernelGGL(quantize_kernel<false>, grid, block, 0, s, x, x_stride, D, (int32_t)padded, q, q_stride, scales);
+    launch_quantize(x, dtype, x_stride, n_rows, D, (int32_t)padded, q, q_stride, scales, reinterpret_cast<hipStream_t>(stream));
     return launched_op(what);
 }
 
@@ -925,6 +949,7 @@ extern "C" psc_status psc_head_logits(const void *x, psc_dtype x_dtype, int64_t 
     if (D < 1 || D > kMostD) return refuse(what, "D outside [1, 131072]");
     if (V > kMostV) return refuse(what, "V > 2^26");
     if (B == 0 || V == 0) return PSC_OK;
+    if ((int64_t)up(B, 64) * up(V, 512) > kMostGrid) return refuse(what, "ceil(B / 64) * ceil(V / 512) >= 2^24");
     if (!x || !w || !w_scales || !workspace) return refuse(what, "null pointer");
     if (x_stride < 0 || !aligned_to(x, size_of(x_dtype))) return refuse(what, "negative stride, or x off its elements' alignment");
     if (w_stride % kChunk || w_stride < D || w_stride > INT32_MAX / 512 || !aligned_to(w, kChunk))
@@ -963,11 +988,9 @@ extern "C" psc_status psc_head_logits(const void *x, psc_dtype x_dtype, int64_t 
         // half of them; a quarter where wide_kernel, which is closer to the compute units' rate, takes all
         a.gather_most = takes_wide(a) ? V / 4 : V / 2;
     }
-    const dim3 grid((uint32_t)((int64_t)B + a.blocks)), block(kQuantBlock);
-    int8_t *q = reinterpret_cast<int8_t *>(at);
-    float *scales = reinterpret_cast<float *>(at + ws.scales);
-    if (x_dtype == PSC_BF16) hipLaunchKernelGGL(prepare_kernel<true>, grid, block, 0, s, a, x, x_stride, q, scales, counts, ids);
-    else hipLaunchKernelGGL(prepare_kernel<false>, grid, block, 0, s, a, x, x_stride, q, scales, counts, ids);
+    launch_prepare(a, x, x_dtype, x_stride, reinterpret_cast<int8_t *>(at), reinterpret_cast<float *>(at + ws.scales), counts, ids, s);
+    // the product would go by whatever the workspace holds
+    if (psc_status st = launched_op(what)) return st;
     launch_product(a, dtype == PSC_BF16, s);
     return launched_op(what);
 }

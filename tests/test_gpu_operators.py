@@ -646,3 +646,48 @@ def test_penalize_by_the_history_at_every_length(V, cap, dtype, masked):
                            keep=keep)
     close(got, want, 8 * U * size)
     assert around(got, 3)
+
+
+# ---------------------------------------------------------------- more rows than a launch has workgroups
+
+MANY = (1 << 24) + 70
+
+
+def ends(n):
+    """Rows at both ends, and around the last one of a launch."""
+    return [*range(0, 300), *range((1 << 24) - 400, (1 << 24) + 10), *range(n - 50, n)]
+
+
+def test_quantize_more_rows_than_one_launch_takes():
+    x = torch.empty(MANY, 3, device=DEV).uniform_(-1, 1, generator=torch.Generator(DEV).manual_seed(1))
+    q, s = psc.quantize_rows(x)
+    at = torch.tensor(ends(MANY), device=DEV)
+    want, scale = quantized(x[at])
+    assert np.array_equal(host(q[at]), want) and np.array_equal(s[at].cpu().numpy(), scale)
+    # every row's largest element becomes 127 of its own scale
+    most = x.abs().amax(1)
+    assert torch.equal(q.abs().amax(1), torch.full_like(s, 127).to(torch.int8)) and torch.equal(s, most / torch.full_like(most, 127))
+
+
+@pytest.mark.parametrize("masked", [False, True])
+def test_head_logits_of_more_rows_than_one_launch_takes(masked):
+    g = torch.Generator(DEV).manual_seed(2)
+    D, V = 2, 33
+    x = torch.empty(MANY, D, device=DEV).uniform_(-1, 1, generator=g)
+    w = torch.randint(-128, 128, (V, 16), generator=g, dtype=torch.int8, device=DEV)[:, :D]
+    scales = torch.rand(V, generator=g, device=DEV)
+    words = keep = None
+    if masked:
+        words = torch.zeros(MANY, 2, dtype=torch.int32, device=DEV)
+        words[::2, 0] = 0b1010000
+        words[-1, 1] = 1
+        keep = np.zeros((MANY, V), bool)
+        keep[::2, 4] = keep[::2, 6] = keep[-1, 32] = True
+    got = psc.head_logits(x, w, scales, bitmask=words)
+    at = ends(MANY)
+    rows = torch.tensor(at, device=DEV)
+    y = head_exact(x[rows], w, scales)
+    close(got[rows], np.where(keep[at], y, -np.inf) if masked else y, head_bound(y, 0))
+    if masked:
+        bits = torch.from_numpy(keep).to(DEV)
+        assert bool(torch.isneginf(got[~bits]).all()) and bool(torch.isfinite(got[bits]).all())

@@ -113,3 +113,12 @@ def test_sample_refuses_rows_past_two_mib_less_a_line():
     for V in (1 << 29, 1 << 30, (1 << 31) - 1):
         for dtype in (0, 1):
             assert sample(dtype=dtype, V=V, stride=V) == INVALID and b"2 MiB" in psc.lib().psc_last_error()
+
+
+def test_head_logits_refuses_more_tiles_than_a_launch_holds():
+    most = ((1 << 24) - 1) * 64
+    for B, V in ((most + 1, 8), (most + 1, 512), (most // 2, 513), ((1 << 31) - 1, 1)):
+        assert head(B=B, V=V, stride=V, ws_bytes=1 << 62) == INVALID and b"2^24" in psc.lib().psc_last_error()
+    # the last one that is taken gets as far as the workspace's check
+    for B, V in ((most, 512), (((1 << 23) - 1) * 64, 1024), (64, 1 << 26)):
+        assert head(B=B, V=V, stride=V, ws_bytes=1) == INVALID and b"workspace" in psc.lib().psc_last_error()
