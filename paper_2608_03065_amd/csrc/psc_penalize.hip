@@ -379,11 +379,12 @@ constexpr int32_t kComputeUnits = 256;
 
 template <bool kBf16>
 void launch_penalize(const PenArgs &a, int32_t B, hipStream_t s) {
-    for (int32_t b = 0; b < B; b += kMostRows) {
-        const int32_t rows = std::min(kMostRows, B - b);
+    // b passes 31 bits after the last rows
+    for (int64_t b = 0; b < B; b += kMostRows) {
+        const int32_t rows = (int32_t)std::min<int64_t>(kMostRows, B - b);
         PenArgs p = a;
         p.logits = static_cast<char *>(a.logits) + b * a.stride * (kBf16 ? 2 : 4);
-        if (a.bitmask) p.bitmask = a.bitmask + (int64_t)b * a.W;
+        if (a.bitmask) p.bitmask = a.bitmask + b * a.W;
         const int32_t tiles = tiles_of_row(a.V, kBf16 ? 2 : 4);
         if (!a.lens && !a.n_bias) {
             constexpr int kTiles = kMaskTiles * kBlock / kWave;
@@ -392,12 +393,12 @@ void launch_penalize(const PenArgs &a, int32_t B, hipStream_t s) {
                                    a.V, p.bitmask, a.W);
             continue;
         }
-        if (a.lens) p.history = a.history + (int64_t)b * a.cap, p.lens = a.lens + b;
+        if (a.lens) p.history = a.history + b * a.cap, p.lens = a.lens + b;
         if (a.prompt_lens) p.prompt_lens = a.prompt_lens + b;
         if (a.repetition) p.repetition = a.repetition + b;
         if (a.presence) p.presence = a.presence + b;
         if (a.frequency) p.frequency = a.frequency + b;
-        if (a.n_bias) p.bias_ids = a.bias_ids + (int64_t)b * a.n_bias, p.bias_values = a.bias_values + (int64_t)b * a.n_bias;
+        if (a.n_bias) p.bias_ids = a.bias_ids + b * a.n_bias, p.bias_values = a.bias_values + b * a.n_bias;
         // As many workgroups a row as it has slices, or shares of tiles to mask,
         // up to one per compute unit in all.
         const bool half = a.cap <= kHalfCap;

@@ -691,3 +691,27 @@ def test_head_logits_of_more_rows_than_one_launch_takes(masked):
     if masked:
         bits = torch.from_numpy(keep).to(DEV)
         assert bool(torch.isneginf(got[~bits]).all()) and bool(torch.isfinite(got[bits]).all())
+
+
+def test_penalize_more_rows_than_one_launch_takes():
+    """Every argument with a row's own values, on both sides of 65,535 rows."""
+    r, B, V, cap, n_bias = np.random.default_rng(6), 70000, 33, 7, 3
+    x = torch.from_numpy(r.normal(0, 4, (B, V)).astype(np.float32))
+    history, ids = (r.integers(-1, V + 1, (B, n)).astype(np.int32) for n in (cap, n_bias))
+    lens, prompts = r.integers(0, cap + 1, B).astype(np.int32), r.integers(0, 3, B).astype(np.int32)
+    rep, pres, freq = (a.astype(np.float32) for a in (r.uniform(0.8, 1.6, B), r.uniform(-1, 1, B), r.uniform(0, 0.5, B)))
+    values = r.normal(0, 5, (B, n_bias)).astype(np.float32)
+    words = np.stack([r.integers(-2 ** 31, 2 ** 31, B), r.integers(0, 2, B)], 1).astype(np.int32)
+    t = lambda a: torch.from_numpy(a).to(DEV)  # noqa: E731
+    got = rows_apart(x.to(DEV), 3)
+    psc.penalize(got, t(history), t(lens), prompt_lens=t(prompts), repetition=t(rep), presence=t(pres), frequency=t(freq),
+                 bias_ids=t(ids), bias_values=t(values), bitmask=t(words))
+    at = np.array([*range(0, 50), *range(65500, 65600), *range(B - 50, B)])
+    keep = np.unpackbits(words[at].view(np.uint8), axis=1, bitorder="little")[:, :V].astype(bool)
+    want, size = penalized(x.double().numpy()[at], history[at], lens[at], prompts[at],
+                           *(a[at].astype(np.float64) for a in (rep, pres, freq)), ids[at], values[at].astype(np.float64), keep)
+    close(got[torch.from_numpy(at).to(DEV)], want, 8 * U * size)
+    assert around(got, 3)
+    # without history and biases the mask goes its own way
+    got = psc.penalize(x.to(DEV), bitmask=t(words))
+    close(got[torch.from_numpy(at).to(DEV)], np.where(keep, x.double().numpy()[at], -np.inf), 0)

@@ -1,6 +1,9 @@
 """Refusals of the operators around the logits: what their C entry points and
 their binding turn down before anything reaches a GPU."""
 import ctypes as C
+import os
+import subprocess
+import sys
 
 import pytest
 
@@ -122,3 +125,12 @@ def test_head_logits_refuses_more_tiles_than_a_launch_holds():
     # the last one that is taken gets as far as the workspace's check
     for B, V in ((most, 512), (((1 << 23) - 1) * 64, 1024), (64, 1 << 26)):
         assert head(B=B, V=V, stride=V, ws_bytes=1) == INVALID and b"workspace" in psc.lib().psc_last_error()
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are no device's: every launch has to fail")
+def test_penalize_ends_after_the_last_of_the_most_rows():
+    """Rows are dealt over launches; the number of those done passes 31 bits after the last ones of 2^31 - 1."""
+    code = ("from paper_2608_03065_amd import psc; import ctypes as C; at = C.addressof(C.create_string_buffer(64)); "
+            "assert psc.lib().psc_penalize(at, 0, 1, 2**31 - 1, 1, None, at, None) == -5")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    assert subprocess.run([sys.executable, "-c", code], cwd=root, timeout=60).returncode == 0
