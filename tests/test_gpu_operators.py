@@ -715,3 +715,54 @@ def test_penalize_more_rows_than_one_launch_takes():
     # without history and biases the mask goes its own way
     got = psc.penalize(x.to(DEV), bitmask=t(words))
     close(got[torch.from_numpy(at).to(DEV)], np.where(keep, x.double().numpy()[at], -np.inf), 0)
+
+
+# ---------------------------------------------------------------- head: masks beyond the list of needed tokens, and at its bounds
+
+@pytest.mark.parametrize("B", [3, 140])
+@pytest.mark.parametrize("shares", [(0.0,), (0.9, 0.001, 0.0, 0.05)])
+def test_head_logits_masked_with_more_tokens_than_are_listed(B, shares):
+    V = (1 << 20) + 33
+    x, w, scales, bias = head_inputs(B, 16, V, B)
+    words, keep = mask(B, V, B, shares)
+    y = head_exact(x, w, scales)
+    got = psc.head_logits(x, w, scales, dtype=torch.float32, bias=bias, bitmask=words)
+    close(got, np.where(keep, y + host(bias), -np.inf), head_bound(y, host(bias)))
+
+
+@pytest.mark.parametrize("B", [2, 140])
+@pytest.mark.parametrize("masked", [False, True])
+def test_head_logits_of_more_than_four_gib_of_weights(B, masked):
+    D, V, some = 16400, 262147, 16384
+    g = torch.Generator(DEV).manual_seed(B)
+    x = torch.randn(B, D, generator=g, device=DEV).to(torch.bfloat16)
+    w = torch.randint(-128, 128, (V, D), generator=g, dtype=torch.int8, device=DEV)
+    assert w.numel() > 1 << 32
+    scales = torch.rand(V, generator=g, device=DEV) / D
+    words, keep = mask(B, V, B, (0.9, 0.001)) if masked else (None, np.ones((B, V), bool))
+    got = psc.head_logits(x, w, scales, dtype=torch.float32, bitmask=words)
+    q, s = quantized(x)
+    q, s = torch.from_numpy(q).double().to(DEV), torch.from_numpy(s).double().to(DEV)
+    for at in range(0, V, some):
+        y = host((q @ w[at:at + some].double().t().contiguous()) * s[:, None] * scales[at:at + some].double())
+        close(got[:, at:at + some], np.where(keep[:, at:at + some], y, -np.inf), head_bound(y, 0))
+
+
+@pytest.mark.parametrize("B", [300, 600])
+@pytest.mark.parametrize("needed", [0, 1, 40, 9999, 10000, 10001, 39999])
+def test_head_logits_of_many_rows_and_few_tokens(B, needed):
+    """Several blocks of rows, and unions on both sides of a quarter of the tokens."""
+    V = 40000
+    x, w, scales, bias = head_inputs(B, 200, V, needed)
+    r = np.random.default_rng(needed)
+    union = np.zeros(V, bool)
+    union[r.permutation(V)[:needed]] = True
+    keep = union & (r.random((B, V)) < 0.3)
+    keep[B - 1] = union
+    words = torch.from_numpy(np.packbits(keep, axis=1, bitorder="little").view(np.int32).copy()).to(DEV)
+    y = head_exact(x, w, scales)
+    dtype, gap = ((torch.float32, 1), (torch.bfloat16, 0))[needed % 2]
+    out = rows_apart(torch.zeros(B, V, dtype=dtype, device=DEV), gap)
+    psc.head_logits(x, w, scales, bias=bias, bitmask=words, out=out)
+    close(out, np.where(keep, y + host(bias), -np.inf), head_bound(y, host(bias)))
+    assert around(out, gap)
