@@ -177,10 +177,9 @@ penalize_kernel(const PenArgs a) {
     const __amdgpu_buffer_rsrc_t mask = buffer_of(words, words ? (uint32_t)a.W * 4u : 0);
     constexpr uint32_t kNowhere = 0xFFFF8000u;
     // the value of a changed logit: its token's counter, and what is added last
-    const float inverse_r = 1.0f / r;
     const auto changed = [&](float x, uint32_t count, float add) {
         float y = x;
-        if (count) y *= y > 0 ? inverse_r : r;
+        if (count) y = y > 0 ? y / r : y * r;
         if (count >= 2) y = y - (float)(count >> 1) * frequency - presence;
         return y + add;
     };

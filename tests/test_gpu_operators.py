@@ -766,3 +766,24 @@ def test_head_logits_of_many_rows_and_few_tokens(B, needed):
     psc.head_logits(x, w, scales, bias=bias, bitmask=words, out=out)
     close(out, np.where(keep, y + host(bias), -np.inf), head_bound(y, host(bias)))
     assert around(out, gap)
+
+
+@pytest.mark.parametrize("V,cap,order", [(5000, 5000, True), (70001, 5000, False), (70001, 900, False), (70001, 20000, True),
+                                         (262145, 40000, True), (524289, 40000, False)])
+def test_repetition_is_one_rounding_of_the_quotient_or_product(V, cap, order):
+    """float32 logits under a repetition penalty alone are the correctly rounded x / r or x * r, also where 1 / r
+    rounds, overflows or is subnormal.  `order`: whether the history passes 3.5 tokens per line of 128 bytes."""
+    assert (2 * cap * 128 >= 7 * V * 4) == order
+    rep = np.array([1.1, 0.7, 3.0, 1.3e38, 1e-38, 1e-39, 1.4e-45, 2.0 ** 127, 1e10], np.float32)
+    r, B = np.random.default_rng(V + cap), rep.size
+    x = r.normal(0, 4, (B, V)).astype(np.float32)
+    x[:, ::5] *= np.float32(1e-38)
+    x[:, 1::9] = 0
+    history = np.stack([r.permutation(V)[:cap] if cap <= V else r.integers(0, V, cap) for _ in range(B)]).astype(np.int32)
+    said = np.zeros((B, V), bool)
+    np.put_along_axis(said, history.astype(np.int64), True, 1)
+    t = lambda a: torch.from_numpy(a).to(DEV)  # noqa: E731
+    got = psc.penalize(t(x), t(history), t(np.full(B, cap, np.int32)), repetition=t(rep)).cpu().numpy()
+    with np.errstate(over="ignore", under="ignore"):
+        want = np.where(said, np.where(x > 0, x / rep[:, None], x * rep[:, None]), x)
+    assert np.array_equal(got, want)
