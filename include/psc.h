@@ -565,8 +565,9 @@ psc_status psc_quantize_rows(const void *x, psc_dtype dtype, int64_t x_stride, i
  * Hidden states to logits, in 8-bit integers:
  *   logits[b][v] = s_b * w_scales[v] * sum_d q[b][d] * w[v][d] + bias[v]
  * where (q, s) are the rows of x quantised as by psc_quantize_rows; -inf where
- * `bitmask` forbids v.  The sum is exact (32-bit integers); scales and bias are
- * float32, and the result is rounded once, to `dtype`.
+ * `bitmask` forbids v.  The sum is exact (32-bit integers).  The rest is float32:
+ * the sum's product with s_b, and, with one rounding, that one's with w_scales[v]
+ * plus bias[v]; the result is rounded to `dtype`.
  *  x          [B] rows of D elements, float32 or bfloat16, x_stride apart.
  *  w          int8 [V] rows of D, w_stride bytes apart (a multiple of 16,
  *             >= D, at most 4,194,303), starting at 16-byte addresses; what

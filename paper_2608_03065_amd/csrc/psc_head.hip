@@ -240,8 +240,10 @@ prepare_kernel(const HeadArgs a, int32_t rows, const void *__restrict__ x, int64
 
 // ---------------------------------------------------------------- results
 
-// sum * xs * ws + bias, in this order, each operation rounded to float32
-__device__ __forceinline__ float scaled(int32_t sum, float xs, float ws, float bias) { return (float)sum * xs * ws + bias; }
+// sum * xs * ws + bias: the sum and its product with xs rounded to float32, the
+// product with ws and the bias as one operation with one rounding.  Named, so
+// that every kernel rounds alike.
+__device__ __forceinline__ float scaled(int32_t sum, float xs, float ws, float bias) { return __builtin_fmaf((float)sum * xs, ws, bias); }
 
 // Four consecutive logits of a row from token v on, a multiple of 4; bit e of
 // `allowed` is token v + e's.

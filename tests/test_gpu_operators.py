@@ -787,3 +787,34 @@ def test_repetition_is_one_rounding_of_the_quotient_or_product(V, cap, order):
     with np.errstate(over="ignore", under="ignore"):
         want = np.where(said, np.where(x > 0, x / rep[:, None], x * rep[:, None]), x)
     assert np.array_equal(got, want)
+
+
+def fused(a, b, c):
+    """a * b + c of float32 arrays with one rounding to float32: a float64 sum, made odd where it is not exact."""
+    product, c = a.astype(np.float64) * b.astype(np.float64), c.astype(np.float64)      # the product is exact
+    s = product + c
+    part = s - product
+    error = (product - (s - part)) + (c - part)
+    even = (s.view(np.int64) & 1) == 0
+    return np.where((error != 0) & even, np.nextafter(s, np.copysign(np.inf, error)), s).astype(np.float32)
+
+
+@pytest.mark.parametrize("B,D,V", [(7, 300, 500), (50, 4096, 1000), (100, 200, 3000), (300, 256, 20000), (520, 128, 20001)])
+def test_head_logits_rounds_alike_everywhere(B, D, V):
+    """Bit for bit, by every kernel: the sum times the state's scale, then times the token's plus the bias with one
+    rounding.  Some biases take nearly all of a product away."""
+    x, w, scales, bias = head_inputs(B, D, V, B + 1)
+    q, s = quantized(x)
+    sums = (torch.from_numpy(q).double() @ w.cpu().double().T).numpy()
+    first = sums.astype(np.float32) * s[:, None]
+    ws = scales.cpu().numpy()
+    bias[::2] = torch.from_numpy(-(first[1 % B] * ws)[::2]).to(DEV)
+    b = bias.cpu().numpy()
+    want = fused(first, np.broadcast_to(ws, first.shape), np.broadcast_to(b, first.shape))
+    assert np.array_equal(psc.head_logits(x, w, scales, dtype=torch.float32, bias=bias).cpu().numpy(), want)
+    plain = fused(first, np.broadcast_to(ws, first.shape), np.zeros_like(first))
+    assert np.array_equal(psc.head_logits(x, w, scales, dtype=torch.float32).cpu().numpy(), plain)
+    for shares in ((0.9,), (20 / V,)):
+        words, keep = mask(B, V, 1, shares)
+        got = psc.head_logits(x, w, scales, dtype=torch.float32, bias=bias, bitmask=words).cpu().numpy()
+        assert np.array_equal(got, np.where(keep, want, -np.inf))
