@@ -605,7 +605,7 @@ typedef struct {
 } psc_penalties;
 
 /*
- * In place on logits [B][V], for every token v of row b:
+ * In place on logits [B][V], for every token v of row b, in this order:
  *   v in the history:                   x = x > 0 ? x / repetition : x * repetition
  *   n > 0 times in it after the prompt: x = x - n * frequency - presence
  *   v among the biases:                 x = x + value

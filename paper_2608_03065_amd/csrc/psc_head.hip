@@ -5,15 +5,17 @@
 //
 // A call launches prepare_kernel (the states to 8 bits and, under a mask, the
 // list of tokens that any row allows), then the product: small_kernel for up to
-// 128 rows, wide_kernel above.  Where the mask leaves few tokens, the product
-// is taken of the listed tokens' weights only (small_kernel, `gather`).  Where there are
-// too few tiles for the GPU, D is split over workgroups; the last one of a tile
-// to end adds their sums, which are integers: any order gives the same.
+// 128 rows, and for more where the large tiles would be too few (takes_wide),
+// wide_kernel for the others.  Where the mask leaves few tokens, the product is
+// taken of the listed tokens' weights only (small_kernel, `gather`; beside
+// wide_kernel in a launch of its own).  Where there are too few tiles for the GPU, D
+// is split over workgroups; the last one of a tile to end adds their sums, which
+// are integers: any order gives the same.
 //
 // Few rows are bound by the weights' bytes, each read once: 64 x 151,665 x 2,048
 // takes 73 us, 4.5 TB/s, where a large copy reaches 4.8.  Many rows are bound by
-// the matrix cores: 2,048 x 128,256 x 4,096 takes 900 us, 2.4 P integer
-// operations a second.  Calls that need few tokens' weights (8 rows, 160
+// the matrix cores: 2,048 x 128,256 x 4,096 takes 900 to 935 us, 2.3 to 2.4 P
+// integer operations a second.  Calls that need few tokens' weights (8 rows, 160
 // tokens: 11 us) are bound by their chain of waits: the list, the weights, the
 // parts' sums.
 #include "psc_ops.hpp"
@@ -29,6 +31,9 @@ namespace {
 // x[d] = scale * q[d]: scale = max |x| / 127 and q = rint(x / scale) (ties to
 // even), both divisions in float32.  A row of zeros has scale 0; a row with an
 // infinity or a NaN has scale NaN and q 0, so that every product with it is NaN.
+// Weights of 128,256 x 4,096 take 453 us from float32 (2.6 GB, 5.8 TB/s), and 432
+// from bfloat16, of 1.6 GB: there a row's chain is the bound, loads, maximum,
+// barrier and the divisions, which are the same in number.
 constexpr int kQuantBlock = 256;
 constexpr int kQuantVec = 8;      // elements per load
 
@@ -151,6 +156,9 @@ struct HeadArgs {
     int32_t arrivals_most;
 };
 
+// Parts of D at most.  us with at most 4, 8 and 16: 64 x 128,256 x 8,192 with few
+// tokens needed 34.5, 32.5, 35.1; 32 x 32,000 x 2,048 17.6, 17.0, 17.4; but 64 x 8,000
+// x 4,096 18.3, 20.9, 20.9 and 1 x 4,096 x 8,192 14.1, 15.9, 16.0.
 constexpr int32_t kMostSplits = 8;
 
 // How a call is carried out: which columns (all tokens, or the needed ones),
@@ -170,6 +178,7 @@ __device__ __forceinline__ Plan plan_of(const HeadArgs &a, int32_t total) {
         p.tiles = (total + kN - 1) / kN;
         const int32_t tiles = max(p.tiles * a.m_tiles, 1);
         const int32_t room = tiles > a.arrivals_most ? 1 : a.partials_most / (tiles * kM * kN);
+        // of at least two steps; one or four make no difference (8 x 128,256 x 4,096 with 160 tokens needed: 14.0, 14.1)
         p.splits = max(1, min(min(a.units / tiles, room), min(a.steps / 2, kMostSplits)));
     }
     return p;
@@ -363,8 +372,8 @@ __device__ __forceinline__ u32x4 rows_from(const int8_t *p, int64_t bytes) {
     const uintptr_t at = reinterpret_cast<uintptr_t>(p);
     return u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, (uint32_t)min(max(bytes, (int64_t)0), (int64_t)kMostBytes), 0x00020000u};
 }
-// The weights from row `row` on; what lies behind the last row's D elements
-// (up to 16 bytes) is not touched.
+// The weights from row `row` on, up to the first multiple of 16 bytes at or
+// after the last row's D elements: nothing behind that is touched.
 __device__ __forceinline__ int64_t weight_bytes(const HeadArgs &a, int32_t row) {
     return (int64_t)(a.V - row - 1) * a.w_stride + (a.D + kChunk - 1) / kChunk * kChunk;
 }
@@ -680,7 +689,9 @@ __device__ __forceinline__ void wide_body(const HeadArgs &a) {
                 for (int i = 0; i < kTn; i++) fw[i] = *reinterpret_cast<const i32x4 *>(pw + i * 16 * kStep + place);
 #pragma unroll
                 for (int j = 0; j < kTm; j++) fx[j] = *reinterpret_cast<const i32x4 *>(px + j * 16 * kStep + place);
-                // Into the buffers of the step before, which the second group left two turns ago.
+                // Into the buffers of the step before.  The second group read the
+                // last of them in the turn that has just ended: its wait for these
+                // reads and that turn's barrier are all that lies between.
                 if (k == 0) {
                     fetch_x();
                     fetch_w();
@@ -834,7 +845,11 @@ void shape_small(HeadArgs &a, bool gather_only) {
     a.m_tiles = up(a.B, kM);
     const int64_t tiles = (int64_t)a.m_tiles * up(a.V, kN);
     // Parts of D where the tiles alone would leave compute units idle, of at
-    // least four steps each.
+    // least four steps each.  us in parts of at least 1, 4 and 8 steps, and whole:
+    // 64 x 16,000 x 1,024 18.7, 15.3, 11.8, 11.9; 128 x 4,000 x 2,048 20.1, 16.0, 16.7,
+    // 16.6; 16 x 2,000 x 4,096 11.3, 11.3, 10.5, 13.2; 1 x 4,096 x 8,192 16.0, 15.9,
+    // 15.9, 19.8.  128 x 16,000 x 4,096, 125 tiles, would be better off whole: 40.1 in
+    // parts, 29.7.
     const int64_t room = tiles > a.arrivals_most ? 1 : a.partials_most / (tiles * kM * kN);
     a.splits = gather_only ? 1 : (int32_t)std::max<int64_t>(1, std::min<int64_t>({2 * kComputeUnits / tiles, a.steps / 4, kMostSplits, room}));
     // the entry point has seen to it that units of 256 threads fit a launch (V / 4 tokens at most, where only needed ones are taken)
@@ -881,6 +896,15 @@ bool takes_wide(const HeadArgs &a) {
 // over the compute units times a tile's width.  256 states x 151,936 tokens x
 // 4,096: 3 rounds of 256 take 221 us, 2 of 320 201; 2,048 x 128,256: 16 of 256
 // 922, 13 of 320 936.
+//
+// The tiles of small_kernel grow with the rows.  us by tiles of 32 x 64, 64 x 128 and 128
+// x 128, times 128,256 x 4,096: 32 rows 111, 124, 128; 33 rows 169, 124, 128; 64 rows 174,
+// 129, 133; 65 rows 221, 153, 134; 128 rows 349, 167, 146.  Above 64 rows on small
+// vocabularies the middle ones are ahead: 128 x 32,000 x 2,048 43, 28, 32.
+//
+// Beside wide_kernel the needed tokens' launch is made before it is known whether
+// they are few.  Where they are not, it takes 4.5 us, and the list and it together 12
+// of the 222 of 256 x 151,936 x 4,096.
 void launch_product(const HeadArgs &a, bool bf16, hipStream_t s) {
     if (a.B <= 32) return launch_small<32, 64, 1, 4, 4>(a, bf16, false, s);
     if (a.B <= 64) return launch_small<64, 128, 1, 4, 3>(a, bf16, false, s);
@@ -987,7 +1011,10 @@ extern "C" psc_status psc_head_logits(const void *x, psc_dtype x_dtype, int64_t 
         a.blocks = up(V, kBlockTokens);
         a.counts = counts = reinterpret_cast<int32_t *>(at + ws.counts);
         a.ids = ids = reinterpret_cast<int32_t *>(at + ws.ids);
-        // half of them; a quarter where wide_kernel, which is closer to the compute units' rate, takes all
+        // Half of them; a quarter where wide_kernel, which is closer to the compute units' rate, takes all.  us with
+        // the needed ones only and with all: 8 x 128,256 x 4,096 74 and 108 where half are needed, 83 and 107 at 0.6; 64 x
+        // 151,665 x 2,048 69 and 78 at a half, 77 and 78 at 0.6, 86 and 78 at 0.8; by wide_kernel 256 x 151,936 x 4,096 146
+        // and 220 at 0.2, 195 and 216 at 0.3, 240 and 216 at 0.4; 512 x 128,256 x 2,048 109 and 182 at 0.1, 176 and 173 at 0.2.
         a.gather_most = takes_wide(a) ? V / 4 : V / 2;
     }
     launch_prepare(a, x, x_dtype, x_stride, reinterpret_cast<int8_t *>(at), reinterpret_cast<float *>(at + ws.scales), counts, ids, s);

@@ -14,7 +14,9 @@ constexpr int kBlock = 256;
 
 // ---------------------------------------------------------------- mask
 
-// A wavefront per kMaskTiles tiles of a row.
+// A wavefront per kMaskTiles tiles of a row.  Bound by the stores: 256 rows of
+// 151,936 bf16 under masks of every kind (70 MB, of which 5 are the masks) take
+// 14.3 us, 4.9 TB/s.
 constexpr int kMaskTiles = 2;
 
 template <bool kBf16>
@@ -82,22 +84,26 @@ struct PenArgs {
 //  this way (what a lane has nothing to do with goes to a counter or an offset
 //  of nobody's), so that a lane's accesses are under way together.  Bound by
 //  them: each token reads and writes a piece of a line of its own, 256 rows of
-//  151,665 bf16 with 300 biases take 19 us with 1,000 tokens each, 36 with 4,000,
-//  60 with 8,000.
+//  151,665 bf16 with 300 biases take 19 us with 1,000 tokens each, 40 with 4,000,
+//  59 with 8,000.
 //
 //  At least 3.5 tokens per 128-byte line of the row (`in_order`): the history's
 //  tokens stand in no order, and going by them fetches every line several times.
 //  Then each wavefront goes through counters in order, lists those that are not
 //  0, and changes the listed logits two a lane, neighbours by neighbours: the
-//  same rows with 9,400 tokens take 50 us, the other way 73 (under masks of
-//  every kind 57 and 63; at 8,000 the ways are 55 and 58), where reading and
-//  writing all the logits takes 32.  (Three a lane took 65 for 62 us, for their
-//  list takes LDS from the counters.  Going through the logits themselves, 16
-//  bytes with their counters at a time, took 73: its arithmetic is done for all
-//  the tokens that do not change.)
+//  same rows with 9,400 tokens take 47 us, the other way 66, and under masks of
+//  every kind both 52; with 4,000 41 and 40, under masks 47 and 39.  In float32
+//  it is ahead from fewer tokens on: 2 a line, without biases, 72 and 82.  (Three a
+//  lane took 65 for 62 us, for their list takes LDS from the counters.  Going
+//  through the logits themselves, 16 bytes with their counters at a time, took
+//  73: its arithmetic is done for all the tokens that do not change.)
+//  The number is that of large vocabularies.  All counters are cleared and dealt
+//  to the wavefronts however many of them there are tokens for, so that on small
+//  ones this way takes longer: 256 rows of 32,000 bf16 with 1,750 tokens 14.9 us and
+//  the other way 12.6, with 3,500 17.1 and 15.2; of 5,000 with 273 tokens 10.5 and 4.5.
 //
 // A workgroup takes all LDS of a compute unit; two or four a compute unit, with
-// fewer slices each, took 75 and 83 us for the 65 of this split.
+// fewer slices each, took 75 and 83 us where this split took 65.
 //
 // The biased tokens' logits are written by the threads that hold the biases,
 // which take their counters away before.
@@ -356,6 +362,7 @@ penalize_kernel(const PenArgs a) {
     }
 }
 
+// One wait and one store: 1.5 us for 256 rows.
 __global__ void __launch_bounds__(kBlock)
 append_kernel(int32_t *__restrict__ history, int32_t cap, int32_t *__restrict__ lens, int32_t B,
               const int32_t *__restrict__ tokens, int32_t *__restrict__ status) {
