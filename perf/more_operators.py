@@ -1,0 +1,425 @@
+"""Performance cases of the operators around quantised rows: what makes them, what reads them, and the output projection by
+4-bit weights.
+
+  pack    rows of float32 or bfloat16 in microscaled 4- or 8-bit floating point (32 elements share a power of two)
+  lookup  rows of a quantised table by token: the embedding that shares the output projection's weights
+  norm    root-mean-square norm with the residual's addition, its result in float or quantised
+  head    hidden states -> logits: states in 4 or 8 bits, times 4-bit weights, plus a bias per token, forbidden tokens -inf
+
+What is held in 4 or 8 bits is returned as the values that it stands for, in bfloat16, which holds those of the microscaled
+formats without a loss.  Vocabulary sizes are those of common tokenizers (32,000, 128,256, 151,665, 151,936), one of them odd.
+Hidden sizes are powers of two and, among the drawn cases, any number.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+DEVICE = "cuda"
+DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+#: No drawn case is larger than the largest listed one of its operator in any of these.
+MOST_PRODUCTS = 2048 * 128256 * 4096
+MOST_WEIGHTS = 151936 * 4096
+MOST_HEAD_LOGITS = 2048 * 128256
+MOST_PACKED = 128256 * 4096           # elements of a pack case
+MOST_NORMED = 8192 * 4096             # elements of a norm or lookup case
+KINDS = ("none", "mixed", "few")      # no mask; rows of every kind; rows that allow a few tokens each
+FEW = 40
+BLOCK = 32                            # elements that share a scale
+E2M1 = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+
+
+# ---------------------------------------------------------------- cases
+
+def pack(N, D, bits, dtype="bf16", name=None):
+    c = {"op": "pack", "N": N, "D": D, "bits": bits, "dtype": dtype}
+    return dict(c, name=name) if name else c
+
+
+def lookup(N, V, D, form, name=None):
+    c = {"op": "lookup", "N": N, "V": V, "D": D, "form": form}
+    return dict(c, name=name) if name else c
+
+
+def norm(N, D, to, dtype="bf16", stream="bf16", name=None):
+    """dtype: of x; stream: of the residual, "none" without one."""
+    c = {"op": "norm", "N": N, "D": D, "to": to, "dtype": dtype, "stream": stream}
+    return dict(c, name=name) if name else c
+
+
+def head(B, D, V, states="mx8", dtype="bf16", mask="none", bias=False, name=None):
+    c = {"op": "head", "B": B, "D": D, "V": V, "states": states, "dtype": dtype, "mask": mask, "bias": bias}
+    return dict(c, name=name) if name else c
+
+
+def listed():
+    return [
+        # a decoding batch's states, as a product in 8 bits takes them
+        pack(64, 4096, 8, name="pack_states_64"),
+        # a model's output weights when it is loaded: once, the whole vocabulary
+        pack(128256, 4096, 4, name="pack_weights"),
+        # the last tokens of a few streams, out of weights in 4 bits
+        lookup(8, 128256, 4096, "mx4", name="lookup_8"),
+        # a prompt's tokens, out of weights in 8-bit integers
+        lookup(8192, 151936, 4096, "i8", name="lookup_prompt"),
+        # one user's stream on a small model
+        norm(1, 2048, "i8", name="norm_single"),
+        # a decoding batch, the residual stream in float32
+        norm(64, 4096, "mx8", stream="f32", name="norm_64"),
+        # a prompt
+        norm(8192, 4096, "i8", name="norm_prompt"),
+        # one user's stream on a small model: the weights are read for a single row
+        head(1, 2048, 32000, dtype="f32", name="head_single"),
+        # function calling, every stream inside a fixed key or an enumeration: few tokens are needed at all
+        head(8, 4096, 128256, mask="few", name="head_schema_8"),
+        # a server's batch on an unpadded vocabulary, the streams in all kinds of grammar states, both sides in 4 bits
+        head(64, 2048, 151665, "mx4", mask="mixed", bias=True, name="head_odd_64"),
+        # a large decoding batch
+        head(256, 4096, 151936, name="head_256"),
+        # scores of every position of a prompt, both sides in 4 bits: the largest product
+        head(2048, 4096, 128256, "mx4", name="head_prompt_2048"),
+    ]
+
+
+def spread(rng, low, high):
+    return int(math.exp(rng.uniform(math.log(low), math.log(high + 1))))
+
+
+def hidden(rng, most):
+    D = spread(rng, 64, 8192)
+    return max(1, min(D // 64 * 64 if rng.random() < 0.6 else D, most))
+
+
+def draw(rng):
+    op = rng.choice(("pack", "lookup", "norm", "head", "head"))
+    dtype = rng.choice(("bf16", "f32"))
+    if op == "pack":
+        D = hidden(rng, 8192)
+        return pack(spread(rng, 1, MOST_PACKED // D // (1 if dtype == "bf16" else 2)), D, rng.choice((4, 8)), dtype)
+    if op == "norm":
+        D = hidden(rng, 8192)
+        return norm(spread(rng, 1, MOST_NORMED // D // 2), D, rng.choice(("bf16", "f32", "i8", "mx8")), dtype,
+                    rng.choice(("none", "bf16", "f32")))
+    V = spread(rng, 513, 262145)
+    if rng.random() < 0.5:
+        V = max(544, V // 32 * 32)
+    D = hidden(rng, MOST_WEIGHTS // V)
+    if op == "lookup":
+        return lookup(spread(rng, 1, MOST_NORMED // D), V, D, rng.choice(("i8", "mx4", "mx8")))
+    most = min(2048, MOST_PRODUCTS // (V * D), MOST_HEAD_LOGITS // V // (1 if dtype == "bf16" else 2))
+    return head(spread(rng, 1, most), D, V, rng.choice(("mx4", "mx8")), dtype, rng.choice(KINDS), rng.random() < 0.4)
+
+
+# ---------------------------------------------------------------- inputs
+
+def bitmask_of(c, g):
+    """int32 [B, ceil(V / 32)], bit v & 31 of word v >> 5 set where token v is allowed.  Rows of few tokens (inside a key
+    of a schema), of some (an expression is expected), of most (inside a string), and, where the kinds are mixed, now and
+    then of none (a stream that is done)."""
+    if c["mask"] == "none":
+        return None
+    B, V, W = c["B"], c["V"], (c["V"] + 31) // 32
+    few = torch.rand(B, generator=g, device=DEVICE) * (FEW / V)
+    share = few
+    if c["mask"] == "mixed":
+        pick = torch.rand(B, generator=g, device=DEVICE)
+        share = torch.where(pick < 0.3, few, torch.where(pick < 0.6, 0.04, torch.where(pick < 0.97, 0.96, 0.0)))
+    out = torch.empty(B, W, dtype=torch.int32, device=DEVICE)
+    weights = torch.ones(32, dtype=torch.int64, device=DEVICE) << torch.arange(32, device=DEVICE)
+    for at in range(0, B, 128):
+        part = share[at:at + 128, None]
+        bits = torch.zeros(part.shape[0], W * 32, dtype=torch.bool, device=DEVICE)
+        bits[:, :V] = torch.rand(part.shape[0], V, generator=g, device=DEVICE) < part
+        words = (bits.view(part.shape[0], W, 32) * weights).sum(-1)
+        out[at:at + 128] = torch.where(words >= 1 << 31, words - (1 << 32), words).to(torch.int32)
+    return out
+
+
+def states_of(n, D, g):
+    """Hidden states have a few channels far larger than the others."""
+    x = torch.randn(n, D, generator=g, device=DEVICE)
+    x[:, torch.randint(0, D, (max(1, D // 256),), generator=g, device=DEVICE)] *= 8
+    return x
+
+
+def rows_at_16_bytes(n, wide, dtype):
+    """A matrix of rows of `wide` bytes, each from a multiple of 16 bytes on."""
+    return torch.zeros(n, (wide + 15) // 16 * 16, dtype=torch.uint8, device=DEVICE)[:, :wide].view(dtype)
+
+
+def table_of(V, D, form, g):
+    """(q, scales) of random weights as a checkpoint of them holds these: in 8-bit integers with a scale a row; or in
+    4 or 8 bits of floating point, the even elements in the low halves of bytes, with a power of two a block."""
+    blocks = (D + BLOCK - 1) // BLOCK
+    if form == "i8":
+        q = rows_at_16_bytes(V, D, torch.int8)
+        q += torch.randint(-63, 64, (V, D), generator=g, device=DEVICE, dtype=torch.int8)
+        q += torch.randint(-63, 64, (V, D), generator=g, device=DEVICE, dtype=torch.int8)
+        return q, (0.5 + torch.rand(V, generator=g, device=DEVICE)) / (40 * math.sqrt(D))
+    q = rows_at_16_bytes(V, (D + 1) // 2 if form == "mx4" else D, torch.uint8 if form == "mx4" else torch.float8_e4m3fn)
+    scales = rows_at_16_bytes(V, blocks, torch.uint8)
+    for at in range(0, V, 16384):
+        w = torch.randn(min(16384, V - at), D, generator=g, device=DEVICE) / math.sqrt(D)
+        values, e = plain_mx(w, 4 if form == "mx4" else 8)
+        scales[at:at + 16384] = (e + 127).to(torch.uint8)
+        if form == "mx8":
+            q[at:at + 16384] = values.to(torch.float8_e4m3fn)
+            continue
+        size = values.abs()
+        codes = torch.where(size < 2, 2 * size, torch.where(size < 4, 2 + size, 4 + size / 2)).to(torch.uint8)
+        codes = codes + 8 * (values < 0)
+        if D % 2:
+            codes = torch.nn.functional.pad(codes, (0, 1))
+        q[at:at + 16384] = codes[:, ::2] + 16 * codes[:, 1::2]
+    return q, scales
+
+
+def prepare(c, seed):
+    g = torch.Generator(DEVICE).manual_seed(seed)
+    D, s = c["D"], dict(c)
+    if c["op"] == "pack":
+        s["x"] = torch.empty(c["N"], D, dtype=DTYPES[c["dtype"]], device=DEVICE)
+        for at in range(0, c["N"], 16384):
+            s["x"][at:at + 16384] = states_of(min(16384, c["N"] - at), D, g)
+        return s
+    if c["op"] == "norm":
+        s["x"] = states_of(c["N"], D, g).to(DTYPES[c["dtype"]])
+        s["residual"] = None
+        if c["stream"] != "none":
+            s["residual"] = (3 * states_of(c["N"], D, g)).to(DTYPES[c["stream"]])
+        s["gain"] = 1 + 0.2 * torch.randn(D, generator=g, device=DEVICE)
+        s["eps"] = 1e-6
+        return s
+    s["q"], s["scales"] = table_of(c["V"], D, c.get("form", "mx4"), g)
+    if c["op"] == "lookup":
+        s["ids"] = torch.randint(0, c["V"], (c["N"],), generator=g, device=DEVICE, dtype=torch.int32)
+        return s
+    s["x"] = states_of(c["B"], D, g).to(torch.bfloat16)
+    s["bias"] = torch.randn(c["V"], generator=g, device=DEVICE) if c["bias"] else None
+    s["bitmask"] = bitmask_of(c, g)
+    return s
+
+
+# ---------------------------------------------------------------- the plain forms
+
+def times_two_to(x, e):
+    """x * 2 ^ e without a rounding, for e in [-126, 127]; 2 ^ -127 counts as 0, as it scales blocks of zeros alone."""
+    return x * ((e + 127).to(torch.int32) << 23).view(torch.float32)
+
+
+def blocks_of(x):
+    """x [N, D] as [N, blocks, 32], zeros past D."""
+    return torch.nn.functional.pad(x, (0, -x.shape[1] % BLOCK)).view(x.shape[0], -1, BLOCK)
+
+
+def plain_mx(x, bits):
+    """(values [N, D], exponents [N, blocks]) of float32 rows: x is about values * 2 ^ exponents.  A block's exponent is that
+    of its largest element less the largest one of the format, and elements past the format's range become its end."""
+    t = blocks_of(x)
+    most = t.abs().amax(-1, keepdim=True)
+    e = torch.where(most > 0, torch.frexp(most).exponent - 1 - (2 if bits == 4 else 8), -127).clamp(min=-127)
+    t = times_two_to(t, -e)
+    size = t.abs()
+    if bits == 4:
+        step = torch.where(size < 2, 0.5, torch.where(size < 4, 1.0, 2.0))
+        t = (torch.round(t / step) * step).clamp(-6, 6)
+    else:
+        step = times_two_to(torch.ones_like(size), (torch.frexp(size).exponent - 1).clamp(min=-6) - 3)
+        t = (torch.round(t / step) * step).clamp(-448, 448)
+    return t.reshape(x.shape[0], -1)[:, :x.shape[1]], e[:, :, 0]
+
+
+def scaled(values, e):
+    return times_two_to(blocks_of(values), e[:, :, None]).reshape(values.shape[0], -1)[:, :values.shape[1]]
+
+
+def plain_i8(x):
+    """The values of float32 rows in 8-bit integers with a scale each."""
+    scales = x.abs().amax(1, keepdim=True)
+    scales = scales / torch.full_like(scales, 127)      # by a plain 127 torch would multiply with its reciprocal
+    return torch.where(scales > 0, torch.round(x / scales), 0) * scales
+
+
+def table_values(q, scales, D):
+    """Rows of a table as float32."""
+    if q.dtype == torch.int8:
+        return q.float() * scales[:, None]
+    if q.dtype == torch.uint8:
+        codes = torch.stack((q & 15, q >> 4), -1).view(q.shape[0], -1)[:, :D].long()
+        values = torch.tensor(E2M1 + tuple(-v for v in E2M1), device=q.device)[codes]
+    else:
+        values = q.float()
+    return scaled(values, scales.int() - 127)
+
+
+def plain_pack(s):
+    return scaled(*plain_mx(s["x"].float(), s["bits"])).to(torch.bfloat16)
+
+
+def plain_lookup(s):
+    ids = s["ids"].long()
+    q = s["q"].view(torch.uint8)[ids].view(s["q"].dtype)
+    return table_values(q, s["scales"][ids], s["D"]).to(torch.bfloat16)
+
+
+def plain_norm(s):
+    x = s["x"].float()
+    if s["residual"] is not None:
+        s["residual"].copy_(x + s["residual"])
+        x = s["residual"].float()
+    y = x / (x.square().mean(1, keepdim=True) + s["eps"]).sqrt() * s["gain"]
+    if s["to"] == "i8":
+        y = plain_i8(y).to(torch.bfloat16)
+    elif s["to"] == "mx8":
+        y = scaled(*plain_mx(y, 8)).to(torch.bfloat16)
+    else:
+        y = y.to(DTYPES[s["to"]])
+    return (y,) if s["residual"] is None else (y, s["residual"])
+
+
+def allowed(s):
+    """The mask as booleans [B, V]."""
+    words = s["bitmask"]
+    bits = (words[:, :, None] >> torch.arange(32, dtype=torch.int32, device=words.device)) & 1
+    return bits.reshape(words.shape[0], -1)[:, :s["V"]].bool()
+
+
+def plain_head(s):
+    x = scaled(*plain_mx(s["x"].float(), 4 if s["states"] == "mx4" else 8))
+    y = x @ table_values(s["q"], s["scales"], s["D"]).T
+    if s["bias"] is not None:
+        y = y + s["bias"]
+    if s["bitmask"] is not None:
+        y = y.masked_fill(~allowed(s), -math.inf)
+    return y.to(DTYPES[s["dtype"]])
+
+
+PLAIN = {"pack": plain_pack, "lookup": plain_lookup, "norm": plain_norm, "head": plain_head}
+
+
+def run(s):
+    if not own:
+        return PLAIN[s["op"]](s)
+    from paper_2608_03065_amd import psc
+    if s["op"] == "pack":
+        return psc.lookup_rows(*psc.quantize_mx(s["x"], s["bits"]), D=s["D"])
+    if s["op"] == "lookup":
+        return psc.lookup_rows(s["q"], s["scales"], s["ids"], D=s["D"])
+    if s["op"] == "norm":
+        to = DTYPES.get(s["to"], s["to"])
+        y = psc.add_rms_norm(s["x"], s["gain"], residual=s["residual"], eps=s["eps"], to=to)
+        if s["to"] not in DTYPES:
+            y = psc.lookup_rows(*y, D=s["D"])
+        return (y,) if s["residual"] is None else (y, s["residual"])
+    return psc.head_logits_mx(s["x"], s["q"], s["scales"], states=s["states"], dtype=DTYPES[s["dtype"]], bias=s["bias"],
+                              bitmask=s["bitmask"])
+
+
+# ---------------------------------------------------------------- what a pass cannot do without
+
+def packed_bytes(D, form):
+    """Of a quantised row."""
+    return D + 4 if form == "i8" else (D + 1) // 2 * (1 if form == "mx4" else 2) + (D + BLOCK - 1) // BLOCK
+
+
+def work(c):
+    """Every input read once and every output written once, less what the mask makes needless: weights of tokens that no
+    row allows.  Quantised rows that are returned as values count as what they are held in, and their values."""
+    D = c["D"]
+    if c["op"] == "pack":
+        form = "mx4" if c["bits"] == 4 else "mx8"
+        return {"bytes": c["N"] * (D * DTYPES[c["dtype"]].itemsize + 2 * packed_bytes(D, form) + 2 * D), "flops": 0}
+    if c["op"] == "lookup":
+        return {"bytes": c["N"] * (4 + packed_bytes(D, c["form"]) + 2 * D), "flops": 0}
+    if c["op"] == "norm":
+        out = D * DTYPES[c["to"]].itemsize if c["to"] in DTYPES else 2 * packed_bytes(D, c["to"]) + 2 * D
+        stream = 0 if c["stream"] == "none" else 2 * D * DTYPES[c["stream"]].itemsize
+        return {"bytes": c["N"] * (D * DTYPES[c["dtype"]].itemsize + stream + out) + 4 * D, "flops": 4 * c["N"] * D}
+    B, V, size = c["B"], c["V"], DTYPES[c["dtype"]].itemsize
+    words = 0 if c["mask"] == "none" else 4 * B * ((V + 31) // 32)
+    share = {"none": 1.0, "few": FEW / 2 / V, "mixed": 0.3 * FEW / 2 / V + 0.3 * 0.04 + 0.37 * 0.96}[c["mask"]]
+    rows = min(V, B * FEW / 2) if c["mask"] == "few" else V
+    return {"bytes": rows * (packed_bytes(D, "mx4") + 4 * c["bias"]) + 2 * B * D + words + B * V * size,
+            "flops": 2 * B * V * share * D}
+
+
+# ---------------------------------------------------------------- the definitions in 64 bits
+
+def host(t):
+    return None if t is None else t.double().cpu().numpy() if t.is_floating_point() else t.cpu().numpy()
+
+
+def exact_mx(x, bits):
+    """The values that rows of 64-bit numbers take in the format: of all its numbers the nearest one, of two as near ones
+    the one with an even code."""
+    if bits == 4:
+        grid = np.array(E2M1)
+    else:
+        grid = np.array([(m / 8) * 2.0 ** -6 if not k else (1 + m / 8) * 2.0 ** (k - 7) for k in range(16) for m in range(8)][:127])
+    n, D = x.shape
+    t = np.concatenate([x, np.zeros((n, -D % BLOCK))], 1).reshape(n, -1, BLOCK)
+    most = np.abs(t).max(-1, keepdims=True)
+    with np.errstate(divide="ignore"):
+        e = np.floor(np.log2(most))
+    e = np.maximum(e - (2 if bits == 4 else 8), -127)
+    size = np.abs(t) * 2.0 ** -e
+    between = (grid[1:] + grid[:-1]) / 2
+    low, high = np.searchsorted(between, size, "left"), np.searchsorted(between, size, "right")
+    code = np.where(low % 2 == 0, low, high)
+    return (np.copysign(grid[code], t) * 2.0 ** e).reshape(n, -1)[:, :D]
+
+
+def exact_table(q, scales, D):
+    if q.dtype == torch.int8:
+        return host(q).astype(np.float64) * host(scales)[:, None]
+    if q.dtype == torch.uint8:
+        b = host(q)
+        codes = np.stack([b % 16, b // 16], -1).reshape(b.shape[0], -1)[:, :D]
+        values = np.where(codes >= 8, -1.0, 1.0) * np.array(E2M1)[codes % 8]
+    else:
+        values = host(q.float())
+    return values * np.repeat(2.0 ** (host(scales).astype(np.float64) - 127), BLOCK, 1)[:, :D]
+
+
+def exact_norm(s):
+    x = host(s["x"])
+    if s["residual"] is not None:
+        # the residual is a value of its own type by definition; what follows goes by that
+        x = host((s["x"].float() + s["residual"].float()).to(s["residual"].dtype))
+    y = x / np.sqrt((x * x).mean(1, keepdims=True) + s["eps"]) * host(s["gain"])
+    if s["to"] == "i8":
+        scales = np.abs(y).max(1, keepdims=True) / 127
+        y = np.rint(np.divide(y, scales, out=np.zeros_like(y), where=scales > 0)) * scales
+    elif s["to"] == "mx8":
+        y = exact_mx(y, 8)
+    return (y,) if s["residual"] is None else (y, x)
+
+
+def exact_head(s):
+    x = exact_mx(host(s["x"]), 4 if s["states"] == "mx4" else 8)
+    y = np.empty((x.shape[0], s["V"]))
+    for at in range(0, s["V"], 16384):
+        y[:, at:at + 16384] = x @ exact_table(s["q"][at:at + 16384], s["scales"][at:at + 16384], s["D"]).T
+    if s["bias"] is not None:
+        y += host(s["bias"])
+    if s["bitmask"] is not None:
+        bits = np.unpackbits(np.ascontiguousarray(host(s["bitmask"])).view(np.uint8), axis=1, bitorder="little")
+        y[~bits[:, :s["V"]].astype(bool)] = -np.inf
+    return y
+
+
+def exact(c, seed):
+    # over 20 seconds
+    if c["op"] == "head" and (c["B"] * c["V"] * c["D"] > 2e11 or c["V"] * c["D"] > 3.2e8):
+        return None
+    if c["op"] in ("pack", "norm") and c["D"] * c["N"] > 5e7:
+        return None
+    s = prepare(c, seed)
+    if c["op"] == "pack":
+        return exact_mx(host(s["x"]), c["bits"])
+    if c["op"] == "lookup":
+        ids = s["ids"].long()
+        return exact_table(s["q"].view(torch.uint8)[ids].view(s["q"].dtype), s["scales"][ids], c["D"])
+    return {"norm": exact_norm, "head": exact_head}[c["op"]](s)
