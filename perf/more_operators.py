@@ -1,13 +1,13 @@
 """Performance cases of the operators around quantised rows: what makes them, what reads them, and the output projection by
 4-bit weights.
 
-  pack    rows of float32 or bfloat16 in microscaled 4- or 8-bit floating point (32 elements share a power of two)
+  pack    rows of float32 or bfloat16 in microscaled 4-bit floating point (32 elements share a power of two)
   lookup  rows of a quantised table by token: the embedding that shares the output projection's weights
   norm    root-mean-square norm with the residual's addition, its result in float or quantised
-  head    hidden states -> logits: states in 4 or 8 bits, times 4-bit weights, plus a bias per token, forbidden tokens -inf
+  head    hidden states -> logits: states in bfloat16 or 4 bits, times 4-bit weights, plus a bias per token, forbidden tokens -inf
 
 What is held in 4 or 8 bits is returned as the values that it stands for, in bfloat16, which holds those of the microscaled
-formats without a loss.  Vocabulary sizes are those of common tokenizers (32,000, 128,256, 151,665, 151,936), one of them odd.
+format without a loss.  Vocabulary sizes are those of common tokenizers (32,000, 128,256, 151,665, 151,936), one of them odd.
 Hidden sizes are powers of two and, among the drawn cases, any number.
 """
 import math
@@ -33,8 +33,8 @@ E2M1 = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
 
 # ---------------------------------------------------------------- cases
 
-def pack(N, D, bits, dtype="bf16", name=None):
-    c = {"op": "pack", "N": N, "D": D, "bits": bits, "dtype": dtype}
+def pack(N, D, dtype="bf16", name=None):
+    c = {"op": "pack", "N": N, "D": D, "dtype": dtype}
     return dict(c, name=name) if name else c
 
 
@@ -49,17 +49,17 @@ def norm(N, D, to, dtype="bf16", stream="bf16", name=None):
     return dict(c, name=name) if name else c
 
 
-def head(B, D, V, states="mx8", dtype="bf16", mask="none", bias=False, name=None):
+def head(B, D, V, states="bf16", dtype="bf16", mask="none", bias=False, name=None):
     c = {"op": "head", "B": B, "D": D, "V": V, "states": states, "dtype": dtype, "mask": mask, "bias": bias}
     return dict(c, name=name) if name else c
 
 
 def listed():
     return [
-        # a decoding batch's states, as a product in 8 bits takes them
-        pack(64, 4096, 8, name="pack_states_64"),
+        # a decoding batch's states, as a product in 4 bits takes them
+        pack(64, 4096, name="pack_states_64"),
         # a model's output weights when it is loaded: once, the whole vocabulary
-        pack(128256, 4096, 4, name="pack_weights"),
+        pack(128256, 4096, name="pack_weights"),
         # the last tokens of a few streams, out of weights in 4 bits
         lookup(8, 128256, 4096, "mx4", name="lookup_8"),
         # a prompt's tokens, out of weights in 8-bit integers
@@ -67,7 +67,7 @@ def listed():
         # one user's stream on a small model
         norm(1, 2048, "i8", name="norm_single"),
         # a decoding batch, the residual stream in float32
-        norm(64, 4096, "mx8", stream="f32", name="norm_64"),
+        norm(64, 4096, "bf16", stream="f32", name="norm_64"),
         # a prompt
         norm(8192, 4096, "i8", name="norm_prompt"),
         # one user's stream on a small model: the weights are read for a single row
@@ -97,19 +97,19 @@ def draw(rng):
     dtype = rng.choice(("bf16", "f32"))
     if op == "pack":
         D = hidden(rng, 8192)
-        return pack(spread(rng, 1, MOST_PACKED // D // (1 if dtype == "bf16" else 2)), D, rng.choice((4, 8)), dtype)
+        return pack(spread(rng, 1, MOST_PACKED // D // (1 if dtype == "bf16" else 2)), D, dtype)
     if op == "norm":
         D = hidden(rng, 8192)
-        return norm(spread(rng, 1, MOST_NORMED // D // 2), D, rng.choice(("bf16", "f32", "i8", "mx8")), dtype,
+        return norm(spread(rng, 1, MOST_NORMED // D // 2), D, rng.choice(("bf16", "f32", "i8")), dtype,
                     rng.choice(("none", "bf16", "f32")))
     V = spread(rng, 513, 262145)
     if rng.random() < 0.5:
         V = max(544, V // 32 * 32)
     D = hidden(rng, MOST_WEIGHTS // V)
     if op == "lookup":
-        return lookup(spread(rng, 1, MOST_NORMED // D), V, D, rng.choice(("i8", "mx4", "mx8")))
+        return lookup(spread(rng, 1, MOST_NORMED // D), V, D, rng.choice(("i8", "mx4")))
     most = min(2048, MOST_PRODUCTS // (V * D), MOST_HEAD_LOGITS // V // (1 if dtype == "bf16" else 2))
-    return head(spread(rng, 1, most), D, V, rng.choice(("mx4", "mx8")), dtype, rng.choice(KINDS), rng.random() < 0.4)
+    return head(spread(rng, 1, most), D, V, rng.choice(("bf16", "mx4")), dtype, rng.choice(KINDS), rng.random() < 0.4)
 
 
 # ---------------------------------------------------------------- inputs
@@ -146,27 +146,24 @@ def states_of(n, D, g):
 
 def rows_at_16_bytes(n, wide, dtype):
     """A matrix of rows of `wide` bytes, each from a multiple of 16 bytes on."""
-    return torch.zeros(n, (wide + 15) // 16 * 16, dtype=torch.uint8, device=DEVICE)[:, :wide].view(dtype)
+    return torch.zeros(n, (wide + 15) // 16 * 16, dtype=dtype, device=DEVICE)[:, :wide]
 
 
 def table_of(V, D, form, g):
     """(q, scales) of random weights as a checkpoint of them holds these: in 8-bit integers with a scale a row; or in
-    4 or 8 bits of floating point, the even elements in the low halves of bytes, with a power of two a block."""
+    4 bits of floating point, the even elements in the low halves of bytes, with a power of two a block."""
     blocks = (D + BLOCK - 1) // BLOCK
     if form == "i8":
         q = rows_at_16_bytes(V, D, torch.int8)
         q += torch.randint(-63, 64, (V, D), generator=g, device=DEVICE, dtype=torch.int8)
         q += torch.randint(-63, 64, (V, D), generator=g, device=DEVICE, dtype=torch.int8)
         return q, (0.5 + torch.rand(V, generator=g, device=DEVICE)) / (40 * math.sqrt(D))
-    q = rows_at_16_bytes(V, (D + 1) // 2 if form == "mx4" else D, torch.uint8 if form == "mx4" else torch.float8_e4m3fn)
+    q = rows_at_16_bytes(V, (D + 1) // 2, torch.uint8)
     scales = rows_at_16_bytes(V, blocks, torch.uint8)
     for at in range(0, V, 16384):
         w = torch.randn(min(16384, V - at), D, generator=g, device=DEVICE) / math.sqrt(D)
-        values, e = plain_mx(w, 4 if form == "mx4" else 8)
+        values, e = plain_mx(w)
         scales[at:at + 16384] = (e + 127).to(torch.uint8)
-        if form == "mx8":
-            q[at:at + 16384] = values.to(torch.float8_e4m3fn)
-            continue
         size = values.abs()
         codes = torch.where(size < 2, 2 * size, torch.where(size < 4, 2 + size, 4 + size / 2)).to(torch.uint8)
         codes = codes + 8 * (values < 0)
@@ -214,20 +211,16 @@ def blocks_of(x):
     return torch.nn.functional.pad(x, (0, -x.shape[1] % BLOCK)).view(x.shape[0], -1, BLOCK)
 
 
-def plain_mx(x, bits):
+def plain_mx(x):
     """(values [N, D], exponents [N, blocks]) of float32 rows: x is about values * 2 ^ exponents.  A block's exponent is that
-    of its largest element less the largest one of the format, and elements past the format's range become its end."""
+    of its largest element less 2, that of the format's largest number, and elements past its range become its end."""
     t = blocks_of(x)
     most = t.abs().amax(-1, keepdim=True)
-    e = torch.where(most > 0, torch.frexp(most).exponent - 1 - (2 if bits == 4 else 8), -127).clamp(min=-127)
+    e = torch.where(most > 0, torch.frexp(most).exponent - 3, -127).clamp(min=-127)
     t = times_two_to(t, -e)
     size = t.abs()
-    if bits == 4:
-        step = torch.where(size < 2, 0.5, torch.where(size < 4, 1.0, 2.0))
-        t = (torch.round(t / step) * step).clamp(-6, 6)
-    else:
-        step = times_two_to(torch.ones_like(size), (torch.frexp(size).exponent - 1).clamp(min=-6) - 3)
-        t = (torch.round(t / step) * step).clamp(-448, 448)
+    step = torch.where(size < 2, 0.5, torch.where(size < 4, 1.0, 2.0))
+    t = (torch.round(t / step) * step).clamp(-6, 6)
     return t.reshape(x.shape[0], -1)[:, :x.shape[1]], e[:, :, 0]
 
 
@@ -246,22 +239,18 @@ def table_values(q, scales, D):
     """Rows of a table as float32."""
     if q.dtype == torch.int8:
         return q.float() * scales[:, None]
-    if q.dtype == torch.uint8:
-        codes = torch.stack((q & 15, q >> 4), -1).view(q.shape[0], -1)[:, :D].long()
-        values = torch.tensor(E2M1 + tuple(-v for v in E2M1), device=q.device)[codes]
-    else:
-        values = q.float()
+    codes = torch.stack((q & 15, q >> 4), -1).view(q.shape[0], -1)[:, :D].long()
+    values = torch.tensor(E2M1 + tuple(-v for v in E2M1), device=q.device)[codes]
     return scaled(values, scales.int() - 127)
 
 
 def plain_pack(s):
-    return scaled(*plain_mx(s["x"].float(), s["bits"])).to(torch.bfloat16)
+    return scaled(*plain_mx(s["x"].float())).to(torch.bfloat16)
 
 
 def plain_lookup(s):
     ids = s["ids"].long()
-    q = s["q"].view(torch.uint8)[ids].view(s["q"].dtype)
-    return table_values(q, s["scales"][ids], s["D"]).to(torch.bfloat16)
+    return table_values(s["q"][ids], s["scales"][ids], s["D"]).to(torch.bfloat16)
 
 
 def plain_norm(s):
@@ -272,8 +261,6 @@ def plain_norm(s):
     y = x / (x.square().mean(1, keepdim=True) + s["eps"]).sqrt() * s["gain"]
     if s["to"] == "i8":
         y = plain_i8(y).to(torch.bfloat16)
-    elif s["to"] == "mx8":
-        y = scaled(*plain_mx(y, 8)).to(torch.bfloat16)
     else:
         y = y.to(DTYPES[s["to"]])
     return (y,) if s["residual"] is None else (y, s["residual"])
@@ -287,7 +274,9 @@ def allowed(s):
 
 
 def plain_head(s):
-    x = scaled(*plain_mx(s["x"].float(), 4 if s["states"] == "mx4" else 8))
+    x = s["x"].float()
+    if s["states"] == "mx4":
+        x = scaled(*plain_mx(x))
     y = x @ table_values(s["q"], s["scales"], s["D"]).T
     if s["bias"] is not None:
         y = y + s["bias"]
@@ -304,7 +293,7 @@ def run(s):
         return PLAIN[s["op"]](s)
     from paper_2608_03065_amd import psc
     if s["op"] == "pack":
-        return psc.lookup_rows(*psc.quantize_mx(s["x"], s["bits"]), D=s["D"])
+        return psc.lookup_rows(*psc.quantize_mx(s["x"]), D=s["D"])
     if s["op"] == "lookup":
         return psc.lookup_rows(s["q"], s["scales"], s["ids"], D=s["D"])
     if s["op"] == "norm":
@@ -321,7 +310,7 @@ def run(s):
 
 def packed_bytes(D, form):
     """Of a quantised row."""
-    return D + 4 if form == "i8" else (D + 1) // 2 * (1 if form == "mx4" else 2) + (D + BLOCK - 1) // BLOCK
+    return D + 4 if form == "i8" else (D + 1) // 2 + (D + BLOCK - 1) // BLOCK
 
 
 def work(c):
@@ -329,12 +318,11 @@ def work(c):
     row allows.  Quantised rows that are returned as values count as what they are held in, and their values."""
     D = c["D"]
     if c["op"] == "pack":
-        form = "mx4" if c["bits"] == 4 else "mx8"
-        return {"bytes": c["N"] * (D * DTYPES[c["dtype"]].itemsize + 2 * packed_bytes(D, form) + 2 * D), "flops": 0}
+        return {"bytes": c["N"] * (D * DTYPES[c["dtype"]].itemsize + 2 * packed_bytes(D, "mx4") + 2 * D), "flops": 0}
     if c["op"] == "lookup":
         return {"bytes": c["N"] * (4 + packed_bytes(D, c["form"]) + 2 * D), "flops": 0}
     if c["op"] == "norm":
-        out = D * DTYPES[c["to"]].itemsize if c["to"] in DTYPES else 2 * packed_bytes(D, c["to"]) + 2 * D
+        out = D * DTYPES[c["to"]].itemsize if c["to"] in DTYPES else 2 * packed_bytes(D, "i8") + 2 * D
         stream = 0 if c["stream"] == "none" else 2 * D * DTYPES[c["stream"]].itemsize
         return {"bytes": c["N"] * (D * DTYPES[c["dtype"]].itemsize + stream + out) + 4 * D, "flops": 4 * c["N"] * D}
     B, V, size = c["B"], c["V"], DTYPES[c["dtype"]].itemsize
@@ -351,19 +339,16 @@ def host(t):
     return None if t is None else t.double().cpu().numpy() if t.is_floating_point() else t.cpu().numpy()
 
 
-def exact_mx(x, bits):
+def exact_mx(x):
     """The values that rows of 64-bit numbers take in the format: of all its numbers the nearest one, of two as near ones
     the one with an even code."""
-    if bits == 4:
-        grid = np.array(E2M1)
-    else:
-        grid = np.array([(m / 8) * 2.0 ** -6 if not k else (1 + m / 8) * 2.0 ** (k - 7) for k in range(16) for m in range(8)][:127])
+    grid = np.array(E2M1)
     n, D = x.shape
     t = np.concatenate([x, np.zeros((n, -D % BLOCK))], 1).reshape(n, -1, BLOCK)
     most = np.abs(t).max(-1, keepdims=True)
     with np.errstate(divide="ignore"):
         e = np.floor(np.log2(most))
-    e = np.maximum(e - (2 if bits == 4 else 8), -127)
+    e = np.maximum(e - 2, -127)
     size = np.abs(t) * 2.0 ** -e
     between = (grid[1:] + grid[:-1]) / 2
     low, high = np.searchsorted(between, size, "left"), np.searchsorted(between, size, "right")
@@ -374,12 +359,9 @@ def exact_mx(x, bits):
 def exact_table(q, scales, D):
     if q.dtype == torch.int8:
         return host(q).astype(np.float64) * host(scales)[:, None]
-    if q.dtype == torch.uint8:
-        b = host(q)
-        codes = np.stack([b % 16, b // 16], -1).reshape(b.shape[0], -1)[:, :D]
-        values = np.where(codes >= 8, -1.0, 1.0) * np.array(E2M1)[codes % 8]
-    else:
-        values = host(q.float())
+    b = host(q)
+    codes = np.stack([b % 16, b // 16], -1).reshape(b.shape[0], -1)[:, :D]
+    values = np.where(codes >= 8, -1.0, 1.0) * np.array(E2M1)[codes % 8]
     return values * np.repeat(2.0 ** (host(scales).astype(np.float64) - 127), BLOCK, 1)[:, :D]
 
 
@@ -392,13 +374,13 @@ def exact_norm(s):
     if s["to"] == "i8":
         scales = np.abs(y).max(1, keepdims=True) / 127
         y = np.rint(np.divide(y, scales, out=np.zeros_like(y), where=scales > 0)) * scales
-    elif s["to"] == "mx8":
-        y = exact_mx(y, 8)
     return (y,) if s["residual"] is None else (y, x)
 
 
 def exact_head(s):
-    x = exact_mx(host(s["x"]), 4 if s["states"] == "mx4" else 8)
+    x = host(s["x"])
+    if s["states"] == "mx4":
+        x = exact_mx(x)
     y = np.empty((x.shape[0], s["V"]))
     for at in range(0, s["V"], 16384):
         y[:, at:at + 16384] = x @ exact_table(s["q"][at:at + 16384], s["scales"][at:at + 16384], s["D"]).T
@@ -418,8 +400,8 @@ def exact(c, seed):
         return None
     s = prepare(c, seed)
     if c["op"] == "pack":
-        return exact_mx(host(s["x"]), c["bits"])
+        return exact_mx(host(s["x"]))
     if c["op"] == "lookup":
         ids = s["ids"].long()
-        return exact_table(s["q"].view(torch.uint8)[ids].view(s["q"].dtype), s["scales"][ids], c["D"])
+        return exact_table(s["q"][ids], s["scales"][ids], c["D"])
     return {"norm": exact_norm, "head": exact_head}[c["op"]](s)
