@@ -535,7 +535,9 @@ psc_status psc_compute_and_argmax_dense(const psc_handle *h, const int32_t *stac
 
 /*
  * Operators around a step's logits: the output projection that makes them
- * (psc_quantize_rows, psc_head_logits), what a request changes in them
+ * (psc_quantize_rows, psc_head_logits; by 4-bit weights psc_quantize_mx,
+ * psc_head_logits_mx), the norm before it and the embedding that shares its
+ * weights (psc_add_rms_norm, psc_lookup_rows), what a request changes in them
  * (psc_penalize, psc_append_tokens), and the token that is drawn from them
  * (psc_sample).  They need no handle.  Rows are `stride` elements apart
  * (>= V), their elements adjacent and at their own alignment; `bitmask` is
@@ -583,6 +585,111 @@ psc_status psc_head_logits(const void *x, psc_dtype x_dtype, int64_t x_stride, i
                            const int8_t *w, int64_t w_stride, const float *w_scales, int32_t V,
                            const float *bias, const uint32_t *bitmask, void *logits, psc_dtype dtype,
                            int64_t stride, void *workspace, size_t workspace_bytes, void *stream);
+
+/* What a row's elements are held in. */
+typedef enum {
+    PSC_FORM_F32 = 0,
+    PSC_FORM_BF16 = 1,
+    PSC_FORM_I8 = 2,  /* 8-bit integers, a float32 scale a row (psc_quantize_rows)          */
+    PSC_FORM_MX4 = 3  /* 4-bit floating point, a power of two a block (psc_quantize_mx)     */
+} psc_form;
+
+/* psc_head_logits of states that are in 8 bits already: rows of q (as
+ * psc_quantize_rows and psc_add_rms_norm write them, q_stride bytes apart) with
+ * their scales.  Values of -128 count as they are; what lies between D and
+ * q_stride does not matter.  The same workspace, refusals and errors. */
+psc_status psc_head_logits_i8(const int8_t *q, int64_t q_stride, const float *scales, int32_t B, int32_t D,
+                              const int8_t *w, int64_t w_stride, const float *w_scales, int32_t V,
+                              const float *bias, const uint32_t *bitmask, void *logits, psc_dtype dtype,
+                              int64_t stride, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Rows of float32 or bfloat16 in microscaled 4-bit floating point: every 32
+ * consecutive elements of a row (the last block may be shorter) share a power
+ * of two, 2^(s - 127) for a byte s,
+ *   s = max(floor(log2(max |x|)) - 2 + 127, 0),  x is about 2^(s - 127) * e,
+ * where e is the one of +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} that is nearest to x / 2^(s -
+ * 127), of two the one with an even code (its place in the list), +-6 past that.
+ * A code has the sign in its bit 3.  A block of zeros has s = 0; one with an
+ * infinity or NaN has s = 255, which stands for NaN, and zeros.  Element d of a
+ * row is in bits 4 * (d % 2) .. + 3 of its byte d / 2.  Rows of q are q_stride bytes
+ * apart, a multiple of 16, and start at 16-byte addresses, and their codes from D
+ * up to the end of the last block become zeros; rows of scales are
+ * scales_stride bytes apart, a multiple of 4, and start at 4-byte addresses.
+ * For the weights of psc_head_logits_mx (once, a row per token).  n_rows < 2^31,
+ * D <= 2^30; n_rows == 0 or D == 0 is a no-op.
+ * Errors: PSC_E_INVALID_ARG, PSC_E_DEVICE.
+ */
+psc_status psc_quantize_mx(const void *x, psc_dtype dtype, int64_t x_stride, int64_t n_rows, int32_t D,
+                           uint8_t *q, int64_t q_stride, uint8_t *scales, int64_t scales_stride, void *stream);
+
+/*
+ * Rows of a quantised table [n_rows][D] as numbers: out[i] is row ids[i], or row i
+ * where ids is NULL (n <= n_rows then).  The embedding of a model that shares
+ * its output projection's weights, and the inverse of both quantisers.  A row
+ * whose id is outside [0, n_rows) becomes zeros (a stream that is done has -1).
+ *  form    PSC_FORM_I8: q as psc_quantize_rows writes it, scales float32 [n_rows]
+ *          (scales_stride is not used); the product with the scale is float32,
+ *          rounded once to `dtype`.  PSC_FORM_MX4: as psc_quantize_mx writes it;
+ *          every value is exact in bfloat16 and float32.
+ *  out     [n] rows, out_stride elements apart (>= D).
+ * n, n_rows < 2^31, D <= 2^30; n == 0 or D == 0 is a no-op.  Errors:
+ * PSC_E_INVALID_ARG, PSC_E_DEVICE.
+ */
+psc_status psc_lookup_rows(psc_form form, const void *q, int64_t q_stride, const void *scales,
+                           int64_t scales_stride, int64_t n_rows, int32_t D, const int32_t *ids, int64_t n,
+                           void *out, psc_dtype dtype, int64_t out_stride, void *stream);
+
+/*
+ * The norm before a projection, with the addition before the norm:
+ *   h = residual + x, rounded to the residual's type and written back to it
+ *   y = h / sqrt(mean_d h[d]^2 + eps) * gain[d]
+ * in float32, squares past its range included.  Without a residual (NULL) h is x.
+ *  x         [n_rows] rows of D, x_stride elements apart.
+ *  residual  rows residual_stride elements apart (>= D), changed in place; not x.
+ *  gain      float32 [D], or NULL for 1.
+ *  to, out   PSC_FORM_F32, PSC_FORM_BF16: y rounded to it, rows out_stride elements
+ *            apart (>= D).  PSC_FORM_I8: y quantised as by psc_quantize_rows, `scales`
+ *            float32 [n_rows].  PSC_FORM_MX4: as by psc_quantize_mx, `scales` bytes
+ *            scales_stride apart.  For these two out_stride is in bytes, a multiple
+ *            of 16, at a 16-byte address; y is not rounded before it is quantised.
+ * eps >= 0.  A row with a NaN becomes NaN; one with an infinity has NaN there and
+ * zeros elsewhere (8 bits: scale NaN).  n_rows < 2^31, D <= 2^30; n_rows == 0 or D == 0
+ * is a no-op.  Errors: PSC_E_INVALID_ARG, PSC_E_DEVICE.
+ */
+psc_status psc_add_rms_norm(const void *x, psc_dtype x_dtype, int64_t x_stride, void *residual,
+                            psc_dtype residual_dtype, int64_t residual_stride, int64_t n_rows, int32_t D,
+                            const float *gain, float eps, psc_form to, void *out, int64_t out_stride,
+                            void *scales, int64_t scales_stride, void *stream);
+
+/*
+ * Hidden states to logits by 4-bit weights:
+ *   logits[b][v] = sum_d x'[b][d] * w'[v][d] + bias[v]
+ * where w' are the weights' values and x' the states, in bfloat16 (`states`
+ * PSC_FORM_BF16: float32 states are rounded to it) or in 4 bits as by
+ * psc_quantize_mx (PSC_FORM_MX4); -inf where `bitmask` forbids v.  Products are exact,
+ * sums and the bias float32, the result is rounded once to `dtype`.  A
+ * weight's row with a scale of 255 gives NaN.
+ *  x          [B] rows of D: x_form PSC_FORM_F32 or PSC_FORM_BF16, x_stride elements
+ *             apart (x_scales is not used); or PSC_FORM_MX4, for `states` of that form,
+ *             codes x_stride bytes apart (a multiple of 16, at a 16-byte address,
+ *             whole blocks) with x_scales, x_scales_stride bytes apart.
+ *  w          codes [V], w_stride bytes apart (a multiple of 16, whole blocks, at
+ *             most 4,194,303), at a 16-byte address; what lies behind the D codes of a
+ *             row does not matter.
+ *  w_scales   bytes [V], w_scales_stride apart (a multiple of 4, at most 4,194,303),
+ *             at a 4-byte address; the same goes for them.
+ *  bias       float32 [V] or NULL.
+ *  workspace  psc_head_mx_workspace(B, D, V, states) bytes, 16-byte aligned.
+ * 1 <= D <= 131,072, V <= 2^26, ceil(B / 64) * ceil(V / 512) < 2^24.  B == 0 or V == 0 is
+ * a no-op.  Errors: PSC_E_INVALID_ARG, PSC_E_DEVICE.
+ */
+size_t psc_head_mx_workspace(int32_t B, int32_t D, int32_t V, psc_form states);
+psc_status psc_head_logits_mx(const void *x, psc_form x_form, int64_t x_stride, const uint8_t *x_scales,
+                              int64_t x_scales_stride, int32_t B, int32_t D, psc_form states, const uint8_t *w,
+                              int64_t w_stride, const uint8_t *w_scales, int64_t w_scales_stride, int32_t V,
+                              const float *bias, const uint32_t *bitmask, void *logits, psc_dtype dtype,
+                              int64_t stride, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * What the requests of a batch change in their logits.  Row b's history is

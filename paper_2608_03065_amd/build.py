@@ -20,7 +20,7 @@ HIP_FLAGS = [
     # never let the compiler form packed-fp32 instructions
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]
-DEVICE_SOURCES = ["psc_device", "psc_head", "psc_penalize", "psc_sample"]
+DEVICE_SOURCES = ["psc_device", "psc_head", "psc_head_mx", "psc_rows", "psc_penalize", "psc_sample"]
 HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function"]
 
 

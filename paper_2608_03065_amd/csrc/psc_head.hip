@@ -18,9 +18,7 @@
 // integer operations a second.  Calls that need few tokens' weights (8 rows, 160
 // tokens: 11 us) are bound by their chain of waits: the list, the weights, the
 // parts' sums.
-#include "psc_ops.hpp"
-
-#include <algorithm>
+#include "psc_head.hpp"
 
 using namespace psc;
 
@@ -34,7 +32,7 @@ namespace {
 // Weights of 128,256 x 4,096 take 453 us from float32 (2.6 GB, 5.8 TB/s), and 432
 // from bfloat16, of 1.6 GB: there a row's chain is the bound, loads, maximum,
 // barrier and the divisions, which are the same in number.
-constexpr int kQuantBlock = 256;
+constexpr int kQuantBlock = kPrepareBlock;
 constexpr int kQuantVec = 8;      // elements per load
 
 template <bool kBf16>
@@ -119,120 +117,16 @@ quantize_kernel(const void *__restrict__ x, int64_t x_stride, int32_t D, int32_t
     quantize_row<kBf16>(x, x_stride, blockIdx.x, D, padded, q, q_stride, scales, s_most);
 }
 
-// ---------------------------------------------------------------- the product's arguments
+// ---------------------------------------------------------------- the product's arguments, and what is prepared for it
 
-constexpr int kStep = 128;        // bytes of a row per step along D: one line
-constexpr int kChunk = 16;        // bytes per lane of a load and of a matrix instruction's operand
-constexpr int kChunks = kStep / kChunk;
-constexpr uint32_t kNowhere = 0xFFFF8000u;        // an offset past any resource: the hardware drops the access
-constexpr uint32_t kMostBytes = 0xFFFF0000u;      // of a resource
-constexpr int32_t kMostRows = 256;                // of a tile
-
-// The tokens that any row allows, in blocks of kBlockWords mask words: each
-// block's number of them, and their ids in ascending order.
-constexpr int kBlockWords = 64, kBlockTokens = kBlockWords * 32;
-constexpr int kMostBlocks = 512;                  // V up to 1,048,576
-
-struct HeadArgs {
+struct HeadArgs : HeadBase {
     const int8_t *x;              // quantised states, rows x_stride apart, zeros from D up to whole steps
     int64_t x_stride;
     const float *x_scales;
     const int8_t *w;
     int64_t w_stride;
-    const float *w_scales, *bias;
-    const uint32_t *bitmask;
-    void *y;
-    int64_t y_stride;
-    int32_t B, D, V, W;
-    int32_t steps, m_tiles;
-    int32_t splits;               // parts of D, where all tokens are taken
-    const int32_t *counts, *ids;  // needed tokens: [blocks], [blocks][kBlockTokens]; null without a mask
-    int32_t blocks;
-    int32_t gather_most;          // most needed tokens at which only they are taken
-    int32_t units;                // workgroups there are for tiles times parts
-    int32_t *partials;            // [tiles][parts][kM * kN] sums, where D is split
-    int32_t partials_most;        // their room
-    uint32_t *arrivals;           // [tiles] parts that have ended: prepare_kernel clears them
-    int32_t arrivals_most;
+    const float *w_scales;
 };
-
-// Parts of D at most.  us with at most 4, 8 and 16: 64 x 128,256 x 8,192 with few
-// tokens needed 34.5, 32.5, 35.1; 32 x 32,000 x 2,048 17.6, 17.0, 17.4; but 64 x 8,000
-// x 4,096 18.3, 20.9, 20.9 and 1 x 4,096 x 8,192 14.1, 15.9, 16.0.
-constexpr int32_t kMostSplits = 8;
-
-// How a call is carried out: which columns (all tokens, or the needed ones),
-// and in how many parts of D each.  Every workgroup works it out alike.
-struct Plan {
-    bool gather;
-    int32_t columns, tiles, splits;
-};
-
-// What is read is the wavefront's; `total` as needed_total gives it.
-template <int kM, int kN>
-__device__ __forceinline__ Plan plan_of(const HeadArgs &a, int32_t total) {
-    Plan p{false, a.V, (a.V + kN - 1) / kN, a.splits};
-    if (a.counts && total <= a.gather_most) {
-        p.gather = true;
-        p.columns = total;
-        p.tiles = (total + kN - 1) / kN;
-        const int32_t tiles = max(p.tiles * a.m_tiles, 1);
-        const int32_t room = tiles > a.arrivals_most ? 1 : a.partials_most / (tiles * kM * kN);
-        // of at least two steps; one or four make no difference (8 x 128,256 x 4,096 with 160 tokens needed: 14.0, 14.1)
-        p.splits = max(1, min(min(a.units / tiles, room), min(a.steps / 2, kMostSplits)));
-    }
-    return p;
-}
-
-// Sum of the blocks' counts up to and with the lane's share of them, kShare
-// consecutive blocks a lane.
-constexpr int kShare = kMostBlocks / kWave;
-__device__ __forceinline__ int32_t needed_upto(const HeadArgs &a, int lane, int32_t (&count)[kShare]) {
-    int32_t sum = 0;
-#pragma unroll
-    for (int i = 0; i < kShare; i++) {
-        const int32_t at = lane * kShare + i;
-        count[i] = at < a.blocks ? a.counts[at] : 0;
-        sum += count[i];
-    }
-    return wave_scan(sum, 0, kAdd);
-}
-
-// ---------------------------------------------------------------- prepare
-
-// Block `block` of the needed tokens: the OR of the rows' words, by one
-// workgroup, its wavefronts over every fourth row.  Most masks allow almost all
-// tokens; as soon as a block has all of its bits, the other rows are not read.
-__device__ __forceinline__ void needed_block(const HeadArgs &a, int32_t block, int32_t *__restrict__ counts,
-                                             int32_t *__restrict__ ids, uint32_t (*s_words)[kBlockWords]) {
-    constexpr int kWaves = kQuantBlock / kWave, kAhead = 16;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int32_t w = block * kBlockWords + lane;
-    const int32_t left = a.V - w * 32;        // tokens from the word's first on
-    const uint32_t inside = left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1;
-    uint32_t any = 0;
-    for (int32_t b = wave; b < a.B; b += kWaves * kAhead) {
-        uint32_t word[kAhead];
-#pragma unroll
-        for (int i = 0; i < kAhead; i++) {
-            const int32_t row = b + i * kWaves;
-            word[i] = inside && row < a.B ? a.bitmask[(int64_t)row * a.W + w] : 0;
-        }
-#pragma unroll
-        for (int i = 0; i < kAhead; i++) any |= word[i];
-        if (!__ballot((any & inside) != inside)) break;
-    }
-    s_words[wave][lane] = any & inside;
-    __syncthreads();
-    if (wave) return;
-#pragma unroll
-    for (int i = 1; i < kWaves; i++) any |= s_words[i][lane];
-    any &= inside;
-    const int32_t n = __popc(any), upto = wave_scan(n, 0, kAdd);
-    if (lane == kWave - 1) counts[block] = upto;
-    int32_t *to = ids + (int64_t)block * kBlockTokens + upto - n;
-    for (; any; any &= any - 1) *to++ = w * 32 + __ffs((int)any) - 1;
-}
 
 // Workgroups 0 .. rows - 1: a row of states each; the others a block of needed
 // tokens each; all of them clear the arrival counters.
@@ -245,6 +139,31 @@ prepare_kernel(const HeadArgs a, int32_t rows, const void *__restrict__ x, int64
         a.arrivals[i] = 0;
     if ((int32_t)blockIdx.x < rows) quantize_row<kBf16>(x, x_stride, blockIdx.x, a.D, (int32_t)a.x_stride, q, a.x_stride, scales, shared[0]);
     else needed_block(a, (int32_t)blockIdx.x - rows, counts, ids, shared);
+}
+
+// The same of states that are in 8 bits already: rows `first` .. are copied, zeros behind them.
+__global__ void __launch_bounds__(kQuantBlock)
+copy_kernel(const HeadArgs a, int32_t first, int32_t rows, const int8_t *__restrict__ x, int64_t x_stride, const float *__restrict__ x_scales,
+            int8_t *__restrict__ q, float *__restrict__ scales, int32_t *__restrict__ counts, int32_t *__restrict__ ids) {
+    __shared__ uint32_t shared[kQuantBlock / kWave][kBlockWords];
+    if (first == 0)
+        for (int64_t i = (int64_t)blockIdx.x * kQuantBlock + threadIdx.x; i < a.arrivals_most; i += (int64_t)gridDim.x * kQuantBlock) a.arrivals[i] = 0;
+    if ((int32_t)blockIdx.x >= rows) {
+        needed_block(a, (int32_t)blockIdx.x - rows, counts, ids, shared);
+        return;
+    }
+    const int64_t r = (int64_t)first + blockIdx.x;
+    for (int32_t d = threadIdx.x * kChunk; d < (int32_t)a.x_stride; d += kQuantBlock * kChunk) {
+        uint32_t t[4] = {};
+        if (d < a.D) __builtin_memcpy(t, x + r * x_stride + d, sizeof t);
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            const int32_t left = a.D - d - 4 * k;
+            if (left < 4) t[k] &= left > 0 ? ~(~0u << (8 * left)) : 0u;
+        }
+        __builtin_memcpy(q + r * a.x_stride + d, t, sizeof t);
+    }
+    if (threadIdx.x == 0) scales[r] = x_scales[r];
 }
 
 // ---------------------------------------------------------------- results
@@ -272,16 +191,6 @@ __device__ __forceinline__ void put_four(const HeadArgs &a, int32_t b, int32_t v
     else
         for (int e = 0; e < 4; e++)
             if (v + e < a.V) to[e] = out[e];
-}
-
-__device__ __forceinline__ uint32_t load_word(__amdgpu_buffer_rsrc_t from, int32_t at) {
-    return __builtin_amdgcn_raw_buffer_load_b32(from, (uint32_t)at * 4u, 0, 0);
-}
-
-// The mask's words from row m0 on; nothing without a mask.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t mask_from(const HeadArgs &a, int32_t m0) {
-    const int64_t rows = a.bitmask ? min(a.B - m0, kMostRows) : 0;
-    return buffer_of(a.bitmask + (a.bitmask ? (int64_t)m0 * a.W : 0), (uint32_t)min(rows * a.W * 4, (int64_t)kMostBytes));
 }
 
 // What kTn by kTm blocks of 16 tokens by 16 states need besides their sums.
@@ -327,51 +236,8 @@ struct Factors {
     }
 };
 
-// -inf in the forbidden logits and nothing else: the allowed ones are written
-// by other workgroups.  `part` of `parts` workgroups; each wavefront takes
-// kTiles tiles of a row at a time.
-template <bool kBf16, int kTiles>
-__device__ __forceinline__ void fill_forbidden(const HeadArgs &a, int32_t part, int32_t parts) {
-    constexpr int kElem = kBf16 ? 2 : 4;
-    const int32_t waves = (int32_t)blockDim.x / kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int32_t pieces = (tiles_of_row(a.V, kElem) + kTiles - 1) / kTiles;
-    const int64_t all = (int64_t)a.B * pieces;
-    for (int64_t u = (int64_t)part * waves + wave; u < all; u += (int64_t)parts * waves) {
-        const int64_t b = u >> 32 ? u / pieces : (int64_t)((uint32_t)u / (uint32_t)pieces);
-        forbid_tiles<kBf16, kTiles>(static_cast<char *>(a.y) + b * a.y_stride * kElem, a.bitmask + b * a.W, a.V, a.W,
-                                    (int32_t)(u - b * pieces) * kTiles, threadIdx.x % kWave);
-    }
-}
-
 // ---------------------------------------------------------------- up to 128 rows
 
-// Wait until at most n of the wavefront's loads are outstanding and its reads
-// of LDS are done, then for the other wavefronts of the workgroup.
-template <int n>
-__device__ __forceinline__ void wait_and_meet() {
-    static_assert(n < 64, "the counter's range");
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(n) : "memory");
-}
-
-// 16 bytes per lane from the resource straight to LDS: lane l's to place l from
-// byte `to` of LDS on (M0; the hardware wants an instruction between its write
-// and the load).  In assembly, because the compiler would wait for all such
-// loads before any read of LDS; wait_and_meet waits for the ones that are due.
-__device__ __forceinline__ void load_to_lds(u32x4 from, uint32_t offset, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(from)
-                 : "memory", "m0");
-}
-
-// The byte of LDS that a pointer into it names.
-__device__ __forceinline__ uint32_t lds_byte(const void *p) {
-    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p;
-}
-
-// The words of buffer_of's resource.
-__device__ __forceinline__ u32x4 rows_from(const int8_t *p, int64_t bytes) {
-    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-    return u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, (uint32_t)min(max(bytes, (int64_t)0), (int64_t)kMostBytes), 0x00020000u};
-}
 // The weights from row `row` on, up to the first multiple of 16 bytes at or
 // after the last row's D elements: nothing behind that is touched.
 __device__ __forceinline__ int64_t weight_bytes(const HeadArgs &a, int32_t row) {
@@ -807,13 +673,7 @@ wide_kernel(const HeadArgs a) {
 
 // ---------------------------------------------------------------- host side
 
-constexpr int32_t kComputeUnits = 256;
 constexpr int32_t kWideRows = 128;
-
-int32_t up(int64_t n, int64_t d) { return (int32_t)((n + d - 1) / d); }
-
-// Workgroups of one launch: a grid's threads are fewer than 2^32 in each dimension.
-constexpr int64_t kMostGrid = ((int64_t)1 << 32) / kQuantBlock - 1;
 
 // Rows to 8 bits, a workgroup each, in as many launches as that takes.
 void launch_quantize(const void *x, psc_dtype dtype, int64_t x_stride, int64_t n_rows, int32_t D, int32_t padded, int8_t *q,
@@ -838,22 +698,16 @@ void launch_prepare(const HeadArgs &a, const void *x, psc_dtype dtype, int64_t x
                     q + rows * a.x_stride, a.x_stride, scales + rows, s);
 }
 
-// How small_kernel is launched: its tiles of kM by kN, the parts of D, and the
-// workgroups, of which there are enough to split D further when few tokens are needed.
-template <int kM, int kN>
-void shape_small(HeadArgs &a, bool gather_only) {
-    a.m_tiles = up(a.B, kM);
-    const int64_t tiles = (int64_t)a.m_tiles * up(a.V, kN);
-    // Parts of D where the tiles alone would leave compute units idle, of at
-    // least four steps each.  us in parts of at least 1, 4 and 8 steps, and whole:
-    // 64 x 16,000 x 1,024 18.7, 15.3, 11.8, 11.9; 128 x 4,000 x 2,048 20.1, 16.0, 16.7,
-    // 16.6; 16 x 2,000 x 4,096 11.3, 11.3, 10.5, 13.2; 1 x 4,096 x 8,192 16.0, 15.9,
-    // 15.9, 19.8.  128 x 16,000 x 4,096, 125 tiles, would be better off whole: 40.1 in
-    // parts, 29.7.
-    const int64_t room = tiles > a.arrivals_most ? 1 : a.partials_most / (tiles * kM * kN);
-    a.splits = gather_only ? 1 : (int32_t)std::max<int64_t>(1, std::min<int64_t>({2 * kComputeUnits / tiles, a.steps / 4, kMostSplits, room}));
-    // the entry point has seen to it that units of 256 threads fit a launch (V / 4 tokens at most, where only needed ones are taken)
-    a.units = (int32_t)std::max<int64_t>(gather_only ? (int64_t)a.m_tiles * up(a.gather_most, kN) : tiles * a.splits, 2 * kComputeUnits);
+// copy_kernel with the rows that fit beside the blocks, then the others alone.
+void launch_copy(const HeadArgs &all, const int8_t *x, int64_t x_stride, const float *x_scales, int8_t *q, float *scales, int32_t *counts,
+                 int32_t *ids, hipStream_t s) {
+    HeadArgs a = all;
+    for (int32_t first = 0; first < all.B; a.blocks = 0) {
+        const int32_t rows = (int32_t)std::min<int64_t>(all.B - first, kMostGrid - a.blocks);
+        hipLaunchKernelGGL(copy_kernel, dim3((uint32_t)(rows + a.blocks)), dim3(kQuantBlock), 0, s, a, first, rows, x, x_stride, x_scales, q, scales,
+                           counts, ids);
+        first += rows;
+    }
 }
 
 template <int kM, int kN, int kWavesM, int kWavesN, int kStages>
@@ -917,14 +771,11 @@ void launch_product(const HeadArgs &a, bool bf16, hipStream_t s) {
 }
 
 constexpr int32_t kMostD = 131072;       // |sum| <= 127 * 128 * D stays below 2^31
-constexpr int32_t kMostV = 1 << 26;      // offsets into a tile's rows of the mask fit 32 bits
-static_assert((int64_t)kMostRows * (kMostV / 32) * 4 < kMostBytes, "and are inside a resource");
 int32_t whole_steps(int32_t D) { return up(D, kStep) * kStep; }
 
 // The workspace: quantised states [B][whole_steps(D)], their scales, the needed
 // tokens, the arrival counters, the partial sums; each from a multiple of 16
 // bytes on.
-constexpr int32_t kMostArrivals = 2 * kComputeUnits;
 struct Workspace {
     size_t scales, counts, ids, arrivals, partials, total;
     int32_t partials_most;
@@ -965,19 +816,28 @@ extern "C" size_t psc_head_workspace(int32_t B, int32_t D, int32_t V) {
     return B <= 0 || D <= 0 || D > kMostD || V <= 0 || V > kMostV ? 0 : Workspace(B, D, V).total;
 }
 
-extern "C" psc_status psc_head_logits(const void *x, psc_dtype x_dtype, int64_t x_stride, int32_t B, int32_t D,
-                                      const int8_t *w, int64_t w_stride, const float *w_scales, int32_t V,
-                                      const float *bias, const uint32_t *bitmask, void *logits, psc_dtype dtype,
-                                      int64_t stride, void *workspace, size_t workspace_bytes, void *stream) {
-    const char *what = "psc_head_logits";
-    if (psc_status st = check_rows(what, logits, dtype, stride, B, V)) return st;
-    if (!is_dtype(x_dtype)) return refuse(what, "bad dtype of x");
+namespace {
+
+// What the caller gives as states: numbers of `dtype`, or where `scales` is not null 8-bit integers.
+struct States {
+    const void *x;
+    psc_dtype dtype;
+    int64_t stride;
+    const float *scales;
+};
+
+psc_status head_logits(const char *what, const States &x, int32_t B, int32_t D, const int8_t *w, int64_t w_stride, const float *w_scales,
+                       int32_t V, const float *bias, const uint32_t *bitmask, void *logits, psc_dtype dtype, int64_t stride,
+                       void *workspace, size_t workspace_bytes, void *stream) {
     if (D < 1 || D > kMostD) return refuse(what, "D outside [1, 131072]");
     if (V > kMostV) return refuse(what, "V > 2^26");
     if (B == 0 || V == 0) return PSC_OK;
     if ((int64_t)up(B, 64) * up(V, 512) > kMostGrid) return refuse(what, "ceil(B / 64) * ceil(V / 512) >= 2^24");
-    if (!x || !w || !w_scales || !workspace) return refuse(what, "null pointer");
-    if (x_stride < 0 || !aligned_to(x, size_of(x_dtype))) return refuse(what, "negative stride, or x off its elements' alignment");
+    if (!x.x || !w || !w_scales || !workspace) return refuse(what, "null pointer");
+    if (x.scales) {
+        if (x.stride % kChunk || x.stride < D || !aligned_to(x.x, kChunk) || !aligned_to(x.scales, 4))
+            return refuse(what, "rows of q start at 16 bytes and hold D elements");
+    } else if (x.stride < 0 || !aligned_to(x.x, size_of(x.dtype))) return refuse(what, "negative stride, or x off its elements' alignment");
     if (w_stride % kChunk || w_stride < D || w_stride > INT32_MAX / 512 || !aligned_to(w, kChunk))
         return refuse(what, "rows of w start at 16 bytes and hold D elements");
     if (workspace_bytes < psc_head_workspace(B, D, V) || !aligned_to(workspace, kChunk))
@@ -1017,9 +877,36 @@ extern "C" psc_status psc_head_logits(const void *x, psc_dtype x_dtype, int64_t 
         // and 220 at 0.2, 195 and 216 at 0.3, 240 and 216 at 0.4; 512 x 128,256 x 2,048 109 and 182 at 0.1, 176 and 173 at 0.2.
         a.gather_most = takes_wide(a) ? V / 4 : V / 2;
     }
-    launch_prepare(a, x, x_dtype, x_stride, reinterpret_cast<int8_t *>(at), reinterpret_cast<float *>(at + ws.scales), counts, ids, s);
+    int8_t *const q = reinterpret_cast<int8_t *>(at);
+    float *const scales = reinterpret_cast<float *>(at + ws.scales);
+    if (x.scales) launch_copy(a, static_cast<const int8_t *>(x.x), x.stride, x.scales, q, scales, counts, ids, s);
+    else launch_prepare(a, x.x, x.dtype, x.stride, q, scales, counts, ids, s);
     // the product would go by whatever the workspace holds
     if (psc_status st = launched_op(what)) return st;
     launch_product(a, dtype == PSC_BF16, s);
     return launched_op(what);
+}
+
+}  // namespace
+
+extern "C" psc_status psc_head_logits(const void *x, psc_dtype x_dtype, int64_t x_stride, int32_t B, int32_t D,
+                                      const int8_t *w, int64_t w_stride, const float *w_scales, int32_t V,
+                                      const float *bias, const uint32_t *bitmask, void *logits, psc_dtype dtype,
+                                      int64_t stride, void *workspace, size_t workspace_bytes, void *stream) {
+    const char *what = "psc_head_logits";
+    if (psc_status st = check_rows(what, logits, dtype, stride, B, V)) return st;
+    if (!is_dtype(x_dtype)) return refuse(what, "bad dtype of x");
+    return head_logits(what, {x, x_dtype, x_stride, nullptr}, B, D, w, w_stride, w_scales, V, bias, bitmask, logits, dtype, stride, workspace,
+                       workspace_bytes, stream);
+}
+
+extern "C" psc_status psc_head_logits_i8(const int8_t *q, int64_t q_stride, const float *scales, int32_t B, int32_t D,
+                                         const int8_t *w, int64_t w_stride, const float *w_scales, int32_t V,
+                                         const float *bias, const uint32_t *bitmask, void *logits, psc_dtype dtype,
+                                         int64_t stride, void *workspace, size_t workspace_bytes, void *stream) {
+    const char *what = "psc_head_logits_i8";
+    if (psc_status st = check_rows(what, logits, dtype, stride, B, V)) return st;
+    if (!scales && B > 0 && V > 0) return refuse(what, "null pointer");
+    return head_logits(what, {q, PSC_F32, q_stride, scales}, B, D, w, w_stride, w_scales, V, bias, bitmask, logits, dtype, stride, workspace,
+                       workspace_bytes, stream);
 }

@@ -1,0 +1,623 @@
+// The output projection by microscaled 4-bit weights (psc_head_logits_mx):
+// states in 4 bits too, or in bfloat16.
+//
+// The matrix instruction of 4-bit operands takes 128 elements of a row, a lane
+// 32 of them: a block, 16 bytes of codes, with the block's power of two.  For
+// bfloat16 states the same 16 bytes are converted to bfloat16 times their power,
+// which holds them exactly, and go through four matrix instructions of 32
+// elements each, of which a lane has 8.  Sums are float32.
+#include "psc_head.hpp"
+#include "psc_mx.hpp"
+
+using namespace psc;
+
+namespace {
+
+typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kStepElems = kStep * 2;              // a line of codes
+constexpr int kStepScales = kStepElems / kMxBlock; // and its scales, in bytes
+constexpr int kWideStep = kStepElems * 2;          // the same elements in bfloat16
+constexpr uint32_t kOne = 127;                     // the scale of 1
+
+struct MxArgs : HeadBase {
+    const void *x;                // states: codes or bfloat16, zeros from D up to whole steps
+    int64_t x_stride;             // in bytes
+    const uint8_t *x_scales;      // of codes, whole steps too
+    int64_t x_scales_stride;
+    const uint8_t *w;
+    int64_t w_stride;
+    const uint8_t *w_scales;
+    int64_t w_scales_stride;
+    int32_t w_blocks;             // scales of a row
+};
+
+// ---------------------------------------------------------------- prepare
+
+// Workgroups 0 .. rows - 1: a row of states each, to codes, or to bfloat16, or
+// copied codes; the others a block of needed tokens each; all of them clear
+// the arrival counters.
+enum class From { kF32, kBf16, kMx };
+
+template <From kFrom, bool kMx>
+__device__ __forceinline__ void prepare_row(const MxArgs &a, int64_t r, const void *__restrict__ x, int64_t x_stride,
+                                            const uint8_t *__restrict__ x_scales, int64_t x_scales_stride, uint8_t *__restrict__ q,
+                                            uint8_t *__restrict__ scales) {
+    const int32_t padded = a.steps * kStepElems, blocks = (a.D + kMxBlock - 1) / kMxBlock;
+    uint8_t *const to = q + r * a.x_stride, *const to_scales = scales + r * a.x_scales_stride;
+    for (int32_t d = threadIdx.x * kVec; d < padded; d += kPrepareBlock * kVec) {
+        if constexpr (kFrom == From::kMx) {
+            const uint8_t *const from = static_cast<const uint8_t *>(x) + r * x_stride;
+            uint32_t codes = 0;
+            if (d < a.D) __builtin_memcpy(&codes, from + d / 2, 4);
+            if (d + kVec > a.D) codes &= d < a.D ? ~(~0u << (4 * (a.D - d))) : 0u;
+            __builtin_memcpy(to + d / 2, &codes, 4);
+            if (threadIdx.x % 4 == 0) to_scales[d / kMxBlock] = d / kMxBlock < blocks ? x_scales[r * x_scales_stride + d / kMxBlock] : 0;
+        } else {
+            float v[kVec];
+            load_eight<kFrom == From::kBf16>(static_cast<const char *>(x) + r * x_stride * (kFrom == From::kBf16 ? 2 : 4), d, a.D, v);
+            if constexpr (kMx) {
+                uint32_t scale;
+                const uint32_t codes = to_mx4(v, scale);
+                __builtin_memcpy(to + d / 2, &codes, 4);
+                if (threadIdx.x % 4 == 0) to_scales[d / kMxBlock] = (uint8_t)scale;
+            } else {
+                store_eight<true>(to, d, padded, v);
+            }
+        }
+    }
+}
+
+template <From kFrom, bool kMx>
+__global__ void __launch_bounds__(kPrepareBlock)
+prepare_mx_kernel(const MxArgs a, int32_t first, int32_t rows, const void *__restrict__ x, int64_t x_stride, const uint8_t *__restrict__ x_scales,
+                  int64_t x_scales_stride, uint8_t *__restrict__ q, uint8_t *__restrict__ scales, int32_t *__restrict__ counts,
+                  int32_t *__restrict__ ids) {
+    __shared__ uint32_t shared[kPrepareBlock / kWave][kBlockWords];
+    if (first == 0)
+        for (int64_t i = (int64_t)blockIdx.x * kPrepareBlock + threadIdx.x; i < a.arrivals_most; i += (int64_t)gridDim.x * kPrepareBlock) a.arrivals[i] = 0;
+    if ((int32_t)blockIdx.x < rows) prepare_row<kFrom, kMx>(a, (int64_t)first + blockIdx.x, x, x_stride, x_scales, x_scales_stride, q, scales);
+    else if ((int32_t)blockIdx.x - rows < a.blocks) needed_block(a, (int32_t)blockIdx.x - rows, counts, ids, shared);
+}
+
+// ---------------------------------------------------------------- results
+
+// Four consecutive logits of a row from token v on, a multiple of 4; bit e of
+// `allowed` is token v + e's.
+template <bool kBf16>
+__device__ __forceinline__ void put_four(const HeadBase &a, int32_t b, int32_t v, const f32x4 &sum, const float (&bias)[4], uint32_t allowed) {
+    using T = typename Logit<kBf16>::type;
+    T out[4];
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        const float y = (allowed >> e) & 1 ? sum[e] + bias[e] : kMinusInf;
+        if constexpr (kBf16) out[e] = to_bf16(y);
+        else out[e] = y;
+    }
+    T *to = static_cast<T *>(a.y) + (int64_t)b * a.y_stride + v;
+    if (v + 4 <= a.V) __builtin_memcpy(to, out, sizeof out);
+    else
+        for (int e = 0; e < 4; e++)
+            if (v + e < a.V) to[e] = out[e];
+}
+
+// What kTn by kTm blocks of 16 tokens by 16 states need besides their sums.
+// The lane's tokens of block i are v + 16 i .. + 3, its state of block j is m0 +
+// b + 16 j.  Places outside, a bias or a mask that there is not give zeros.
+template <int kTn, int kTm, bool kPlain>
+struct Extras {
+    float bias[kTn][4];
+    uint32_t words[kTn][kTm];
+
+    __device__ __forceinline__ void load(const HeadBase &a, int32_t v, int32_t m0, int32_t b) {
+        if (kPlain) return;
+        const __amdgpu_buffer_rsrc_t from_bias = buffer_of(a.bias, a.bias ? (uint32_t)a.V * 4u : 0), from_mask = mask_from(a, m0);
+#pragma unroll
+        for (int i = 0; i < kTn; i++) {
+#pragma unroll
+            for (int e = 0; e < 4; e++) bias[i][e] = __builtin_bit_cast(float, load_word(from_bias, v + i * 16 + e));
+#pragma unroll
+            for (int j = 0; j < kTm; j++) words[i][j] = load_word(from_mask, (b + j * 16) * a.W + ((v + i * 16) >> 5));
+        }
+    }
+
+    template <bool kBf16>
+    __device__ __forceinline__ void put(const HeadBase &a, int32_t v, int32_t b, const f32x4 (&sum)[kTn][kTm]) const {
+        const uint32_t all = kPlain || !a.bitmask ? 15u : 0u;
+        const float none[4] = {};
+#pragma unroll
+        for (int i = 0; i < kTn; i++)
+#pragma unroll
+            for (int j = 0; j < kTm; j++)
+                if (v + i * 16 < a.V && b + j * 16 < a.B)
+                    put_four<kBf16>(a, b + j * 16, v + i * 16, sum[i][j], kPlain ? none : bias[i],
+                                    kPlain ? 15u : words[i][j] >> ((v + i * 16) & 31) | all);
+    }
+};
+
+// ---------------------------------------------------------------- products
+
+__device__ __forceinline__ f32x4 product(const u32x4 &w, uint32_t w_scale, const u32x4 &x, uint32_t x_scale, const f32x4 &sum) {
+    const i32x8 a = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0}, b = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, sum, 4, 4, 0, (int)w_scale, 0, (int)x_scale);
+}
+
+__device__ __forceinline__ f32x4 product(const bf16x8 &w, const bf16x8 &x, const f32x4 &sum) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, x, sum, 0, 0, 0);
+}
+
+__device__ __forceinline__ bf16x8 widened(uint32_t codes, float power) {
+    uint32_t pairs[4];
+    from_mx4(codes, power, pairs);
+    return __builtin_bit_cast(bf16x8, pairs);
+}
+
+// The weights' rows from `row` on, up to the end of the last one's last block,
+// and their scales: nothing behind that is touched but what shares 4 bytes with it.
+__device__ __forceinline__ int64_t code_bytes(const MxArgs &a, int32_t row) {
+    return (int64_t)(a.V - row - 1) * a.w_stride + (int64_t)a.w_blocks * (kMxBlock / 2);
+}
+__device__ __forceinline__ int64_t scale_bytes(const MxArgs &a, int32_t row) {
+    return (int64_t)(a.V - row - 1) * a.w_scales_stride + (a.w_blocks + 3) / 4 * 4;
+}
+
+// 4 bytes per lane from the resource straight to LDS, as load_to_lds does with 16.
+__device__ __forceinline__ void load_word_to_lds(u32x4 from, uint32_t offset, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(from)
+                 : "memory", "m0");
+}
+
+// One workgroup computes kM states by kN tokens over a part of D.  Steps of 256
+// elements of all its rows go straight from memory into one of kStages buffers
+// in LDS, kStages - 1 steps ahead: a line of codes of every token and 8 bytes
+// of its scales, and of every state the same or four lines of bfloat16.  A
+// row's 16-byte chunk c lies at place c ^ (row & 7) of its line, and of a state in
+// bfloat16 at c ^ (row & 15), so that the 16 rows that a matrix instruction reads
+// at one chunk fall into different banks; since a load puts lane l's chunk at
+// place l, the lane fetches the chunk that belongs there.  Codes past a row's D
+// elements are multiplied by the states' zeros, and by a scale of 1.
+template <int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kMx, bool kBf16, bool kPlain>
+__device__ __forceinline__ void small_mx_body(const MxArgs &a, bool gather_only) {
+    constexpr int kWaves = kWavesM * kWavesN, kXStep = kMx ? kStep : kWideStep;
+    constexpr int kTm = kM / kWavesM / 16, kTn = kN / kWavesN / 16;   // 16 x 16 blocks of a wavefront
+    static_assert(kTm * kWavesM * 16 == kM && kTn * kWavesN * 16 == kN, "whole blocks");
+    // loads of a step: of the codes, the states, the scales of the tokens and those of the states
+    constexpr int kLoadsW = kN * kStep / 1024 / kWaves;
+    static_assert(kLoadsW * kWaves * 1024 == kN * kStep, "every wavefront loads as much");
+    constexpr int kX1024 = kM * kXStep / 1024, kLoadsX = (kX1024 + kWaves - 1) / kWaves;
+    constexpr int kRowsPerWord = 32, kS256 = kN / kRowsPerWord, kLoadsS = (kS256 + kWaves - 1) / kWaves;
+    constexpr int kT256 = kMx ? (kM + kRowsPerWord - 1) / kRowsPerWord : 0, kLoadsT = (kT256 + kWaves - 1) / kWaves;
+    constexpr int kLoads = kLoadsW + kLoadsX + kLoadsS + kLoadsT;
+    static_assert((kStages - 2) * kLoads < 64, "the counter's range");
+    constexpr int kAtX = kN * kStep, kAtS = kAtX + kX1024 * 1024, kAtT = kAtS + kS256 * 256, kStage = kAtT + kT256 * 256;
+    constexpr int kRest = kStages * kStage;       // where loads of nothing go
+    __shared__ __align__(1024) uint8_t lds[kRest + 1024];
+    __shared__ int32_t s_ids[kN];
+    __shared__ uint32_t s_arrived;
+    // until the first loads into lds: the needed tokens before each block
+    int32_t *const s_before = reinterpret_cast<int32_t *>(lds);
+    static_assert(sizeof lds >= (kMostBlocks + 1) * sizeof(int32_t), "room for the blocks");
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int wm = wave % kWavesM, wn = wave / kWavesM;
+
+    int32_t total = 0, count[kShare];
+    if (!kPlain && a.counts) {
+        const int32_t upto = needed_upto(a, lane, count);
+        total = lane_value(upto, kWave - 1);
+        if (total <= a.gather_most && wave == 0) {
+            int32_t before = upto;
+#pragma unroll
+            for (int i = kShare - 1; i >= 0; i--) {
+                s_before[lane * kShare + i + 1] = before;
+                before -= count[i];
+            }
+            if (lane == 0) s_before[0] = 0;
+        }
+    }
+    Plan plan = plan_of<kM, kN>(a, total);
+    if (kPlain) plan.gather = false;
+    if (gather_only && !plan.gather) return;
+    const bool fill = plan.gather && !gather_only;        // else the wide kernel does it
+    const int32_t tiles = plan.tiles * a.m_tiles;
+    if ((int32_t)blockIdx.x >= tiles * plan.splits) {
+        if (fill) fill_forbidden<kBf16, 1>(a, blockIdx.x, gridDim.x);
+        return;
+    }
+    const int32_t split = (int32_t)blockIdx.x / tiles, tile = (int32_t)blockIdx.x - split * tiles;
+    const int32_t m0 = tile % a.m_tiles * kM, n0 = tile / a.m_tiles * kN;
+    const int32_t first = a.steps * split / plan.splits, steps = a.steps * (split + 1) / plan.splits;
+
+    if (plan.gather) {
+        // token n0 + i of the needed ones: its block by bisection of the sums before each
+        __syncthreads();
+        for (int i = threadIdx.x; i < kN; i += kWaves * kWave) {
+            int32_t id = -1;
+            if (n0 + i < plan.columns) {
+                int32_t lo = 0, hi = a.blocks;
+                while (hi - lo > 1) {
+                    const int32_t mid = (lo + hi) / 2;
+                    if (s_before[mid] <= n0 + i) lo = mid;
+                    else hi = mid;
+                }
+                id = a.ids[(int64_t)lo * kBlockTokens + n0 + i - s_before[lo]];
+            }
+            s_ids[i] = id;
+        }
+        __syncthreads();
+    }
+    const int32_t w_row = plan.gather ? 0 : n0;
+    const u32x4 rw = rows_from(a.w + (int64_t)w_row * a.w_stride, code_bytes(a, w_row));
+    const u32x4 rs = rows_from(a.w_scales + (int64_t)w_row * a.w_scales_stride, scale_bytes(a, w_row));
+    const u32x4 rx = rows_from(static_cast<const char *>(a.x) + (int64_t)m0 * a.x_stride, (int64_t)(a.B - m0 - 1) * a.x_stride + (int64_t)a.steps * kXStep);
+    const u32x4 rt = kMx ? rows_from(a.x_scales + (int64_t)m0 * a.x_scales_stride, (int64_t)(a.B - m0) * a.x_scales_stride) : rs;
+    // offsets of the lane's loads; past the last step, and for rows that there are not, they read nothing
+    uint32_t from_w[kLoadsW], from_x[kLoadsX], from_s[kLoadsS], from_t[kLoadsT ? kLoadsT : 1];
+    const auto token = [&](int row, int64_t stride) {
+        if (!plan.gather) return (uint32_t)row * (uint32_t)stride;
+        return s_ids[row] >= 0 ? (uint32_t)s_ids[row] * (uint32_t)stride : kNowhere;
+    };
+#pragma unroll
+    for (int i = 0; i < kLoadsW; i++) {
+        const int row = (i * kWaves + wave) * 8 + lane / 8;
+        const uint32_t at = token(row, a.w_stride);
+        from_w[i] = at == kNowhere ? at : at + (((lane & 7) ^ (row & 7)) * kChunk);
+    }
+#pragma unroll
+    for (int i = 0; i < kLoadsX; i++) {
+        constexpr int kLanes = kXStep / kChunk;       // that take a row
+        const int row = (i * kWaves + wave) * (kWave / kLanes) + lane / kLanes, c = lane % kLanes;
+        from_x[i] = row < kM && m0 + row < a.B ? (uint32_t)row * (uint32_t)a.x_stride + (uint32_t)((kMx ? c ^ (row & 7) : c ^ (row & 15)) * kChunk) : kNowhere;
+    }
+#pragma unroll
+    for (int i = 0; i < kLoadsS; i++) {
+        const int row = (i * kWaves + wave) * kRowsPerWord + lane / 2;
+        const uint32_t at = row < kN ? token(row, a.w_scales_stride) : kNowhere;
+        from_s[i] = at == kNowhere ? at : at + (lane & 1) * 4;
+    }
+#pragma unroll
+    for (int i = 0; i < kLoadsT; i++) {
+        const int row = (i * kWaves + wave) * kRowsPerWord + lane / 2;
+        from_t[i] = row < kM && m0 + row < a.B ? (uint32_t)row * (uint32_t)a.x_scales_stride + (lane & 1) * 4 : kNowhere;
+    }
+    const auto fetch = [&](int32_t step) {
+        const uint32_t base = lds_byte(lds), to = base + (uint32_t)(step % kStages) * kStage;
+        const auto off = [&](uint32_t from, uint32_t bytes) { return step < steps && from != kNowhere ? from + (uint32_t)step * bytes : kNowhere; };
+#pragma unroll
+        for (int i = 0; i < kLoadsW; i++) load_to_lds(rw, off(from_w[i], kStep), to + (uint32_t)(i * kWaves + wave) * 1024u);
+#pragma unroll
+        for (int i = 0; i < kLoadsX; i++) {
+            const int n = i * kWaves + wave;
+            load_to_lds(rx, off(from_x[i], kXStep), n < kX1024 ? to + kAtX + (uint32_t)n * 1024u : base + kRest);
+        }
+#pragma unroll
+        for (int i = 0; i < kLoadsS; i++) {
+            const int n = i * kWaves + wave;
+            load_word_to_lds(rs, off(from_s[i], kStepScales), n < kS256 ? to + kAtS + (uint32_t)n * 256u : base + kRest);
+        }
+#pragma unroll
+        for (int i = 0; i < kLoadsT; i++) {
+            const int n = i * kWaves + wave;
+            load_word_to_lds(rt, off(from_t[i], kStepScales), n < kT256 ? to + kAtT + (uint32_t)n * 256u : base + kRest);
+        }
+    };
+    f32x4 acc[kTn][kTm] = {};
+    const int r16 = lane % 16, quad = lane / 16;
+    const int32_t v0 = n0 + wn * kTn * 16 + quad * 4, b0 = m0 + wm * kTm * 16 + r16;    // the lane's first token and state
+    Extras<kTn, kTm, kPlain> extras;
+    if (!plan.gather && plan.splits == 1) extras.load(a, v0, m0, b0 - m0);
+#pragma unroll
+    for (int s = 0; s < kStages - 1; s++) fetch(first + s);
+    if (fill) fill_forbidden<kBf16, 1>(a, blockIdx.x, gridDim.x);
+    for (int32_t step = first; step < steps; step++) {
+        wait_and_meet<(kStages - 2) * kLoads>();   // the step has landed, and its predecessor's buffer is free
+        fetch(step + kStages - 1);
+        const uint8_t *const at = lds + step % kStages * kStage;
+        const int left = a.w_blocks - step * kStepScales - quad;       // of the lane's first block: blocks up to the row's end
+#pragma unroll
+        for (int k = 0; k < kStepElems / 128; k++) {
+            u32x4 fw[kTn];
+            uint32_t sw[kTn];
+#pragma unroll
+            for (int i = 0; i < kTn; i++) {
+                const int row = (wn * kTn + i) * 16 + r16;
+                fw[i] = *reinterpret_cast<const u32x4 *>(at + row * kStep + (((k * 4 + quad) ^ (row & 7)) * kChunk));
+                const uint32_t word = *reinterpret_cast<const uint32_t *>(at + kAtS + row * kStepScales + k * 4);
+                sw[i] = left > k * 4 ? (word >> (8 * quad)) & 255u : kOne;
+            }
+            if constexpr (kMx) {
+                u32x4 fx[kTm];
+                uint32_t sx[kTm];
+#pragma unroll
+                for (int j = 0; j < kTm; j++) {
+                    const int row = (wm * kTm + j) * 16 + r16;
+                    fx[j] = *reinterpret_cast<const u32x4 *>(at + kAtX + row * kStep + (((k * 4 + quad) ^ (row & 7)) * kChunk));
+                    sx[j] = *reinterpret_cast<const uint32_t *>(at + kAtT + row * kStepScales + k * 4) >> (8 * quad);
+                }
+#pragma unroll
+                for (int i = 0; i < kTn; i++)
+#pragma unroll
+                    for (int j = 0; j < kTm; j++) acc[i][j] = product(fw[i], sw[i], fx[j], sx[j], acc[i][j]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    bf16x8 fx[kTm];
+#pragma unroll
+                    for (int j = 0; j < kTm; j++) {
+                        const int row = (wm * kTm + j) * 16 + r16;
+                        fx[j] = *reinterpret_cast<const bf16x8 *>(at + kAtX + row * kWideStep + (((k * 16 + quad * 4 + e) ^ (row & 15)) * kChunk));
+                    }
+#pragma unroll
+                    for (int i = 0; i < kTn; i++) {
+                        const bf16x8 w = widened(fw[i][e], mx_power(sw[i]));
+#pragma unroll
+                        for (int j = 0; j < kTm; j++) acc[i][j] = product(w, fx[j], acc[i][j]);
+                    }
+                }
+            }
+        }
+    }
+    if (plan.splits > 1) {
+        // The sums go to memory at device scope, which every XCD sees alike, and
+        // only when they are there does the workgroup count itself in; the
+        // last one of the tile adds them all, in the order of the parts.
+        constexpr uint32_t kPart = kM * kN * sizeof(float);
+        constexpr int kDevice = 16;        // the accesses' scope (sc1)
+        const __amdgpu_buffer_rsrc_t sums = buffer_of(a.partials + (int64_t)tile * plan.splits * (kM * kN), (uint32_t)plan.splits * kPart);
+        const auto place = [&](int i, int j) { return (uint32_t)(((i * kTm + j) * kWaves * kWave + (int)threadIdx.x) * 16); };
+#pragma unroll
+        for (int i = 0; i < kTn; i++)
+#pragma unroll
+            for (int j = 0; j < kTm; j++)
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[i][j]), sums, (uint32_t)split * kPart + place(i, j), 0, kDevice);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (threadIdx.x == 0) s_arrived = __hip_atomic_fetch_add(a.arrivals + tile, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        if (s_arrived != (uint32_t)plan.splits - 1) return;
+        if (!plan.gather) extras.load(a, v0, m0, b0 - m0);
+#pragma unroll
+        for (int i = 0; i < kTn; i++)
+#pragma unroll
+            for (int j = 0; j < kTm; j++) acc[i][j] = f32x4{};
+        constexpr int kAtOnce = 4;
+        for (int32_t part = 0; part < plan.splits; part += kAtOnce) {
+            u32x4 t[kAtOnce][kTn][kTm];
+#pragma unroll
+            for (int n = 0; n < kAtOnce; n++)
+#pragma unroll
+                for (int i = 0; i < kTn; i++)
+#pragma unroll
+                    for (int j = 0; j < kTm; j++)      // parts that there are not give zeros
+                        t[n][i][j] = __builtin_amdgcn_raw_buffer_load_b128(sums, part + n < plan.splits ? (uint32_t)(part + n) * kPart + place(i, j) : kNowhere, 0, kDevice);
+#pragma unroll
+            for (int n = 0; n < kAtOnce; n++)
+#pragma unroll
+                for (int i = 0; i < kTn; i++)
+#pragma unroll
+                    for (int j = 0; j < kTm; j++) acc[i][j] += __builtin_bit_cast(f32x4, t[n][i][j]);
+        }
+    }
+    if (!plan.gather) {
+        extras.template put<kBf16>(a, v0, b0, acc);
+        return;
+    }
+    // few of a tile's logits are allowed: first all the bits, at once, then those
+    const __amdgpu_buffer_rsrc_t mask = mask_from(a, m0);
+    uint32_t allowed[kTm] = {};
+#pragma unroll
+    for (int i = 0; i < kTn; i++) {
+        uint32_t words[kTm][4];
+        int32_t v[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            v[e] = s_ids[(wn * kTn + i) * 16 + quad * 4 + e];
+#pragma unroll
+            for (int j = 0; j < kTm; j++)
+                words[j][e] = __builtin_amdgcn_raw_buffer_load_b32(mask, v[e] < 0 ? kNowhere : (uint32_t)((b0 - m0 + j * 16) * a.W + (v[e] >> 5)) * 4u, 0, 0);
+        }
+#pragma unroll
+        for (int j = 0; j < kTm; j++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) allowed[j] |= (words[j][e] >> (v[e] & 31) & 1u) << (i * 4 + e);
+    }
+#pragma unroll
+    for (int j = 0; j < kTm; j++) {
+        const int32_t b = b0 + j * 16;
+        if (b >= a.B || !allowed[j]) continue;
+        using T = typename Logit<kBf16>::type;
+        T *const row = static_cast<T *>(a.y) + (int64_t)b * a.y_stride;
+#pragma unroll
+        for (int i = 0; i < kTn; i++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                if (!((allowed[j] >> (i * 4 + e)) & 1)) continue;
+                const int32_t v = s_ids[(wn * kTn + i) * 16 + quad * 4 + e];
+                store_logit<kBf16>(row, v, acc[i][j][e] + (a.bias ? a.bias[v] : 0.0f));
+            }
+    }
+}
+
+template <int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kMx, bool kBf16, bool kPlain>
+__global__ void __launch_bounds__(kWave * kWavesM * kWavesN)
+small_mx_kernel(const MxArgs a, bool gather_only) {
+    small_mx_body<kM, kN, kWavesM, kWavesN, kStages, kMx, kBf16, kPlain>(a, gather_only);
+}
+
+// ---------------------------------------------------------------- host side
+
+template <int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kMx>
+struct Small {
+    static void shape(MxArgs &a, bool gather_only) { shape_small<kM, kN>(a, gather_only); }
+    static void launch(const MxArgs &a, bool bf16, bool gather_only, hipStream_t s) {
+        const dim3 grid((uint32_t)a.units), block(kWave * kWavesM * kWavesN);
+        const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a, gather_only); };
+        if (a.bitmask || a.bias) {
+            if (bf16) go(small_mx_kernel<kM, kN, kWavesM, kWavesN, kStages, kMx, true, false>);
+            else go(small_mx_kernel<kM, kN, kWavesM, kWavesN, kStages, kMx, false, false>);
+        } else {
+            if (bf16) go(small_mx_kernel<kM, kN, kWavesM, kWavesN, kStages, kMx, true, true>);
+            else go(small_mx_kernel<kM, kN, kWavesM, kWavesN, kStages, kMx, false, true>);
+        }
+    }
+};
+
+constexpr int32_t kMostD = 131072;
+int32_t steps_of(int32_t D) { return up(D, kStepElems); }
+
+// The workspace: states [B] of whole steps, their scales, the needed tokens, the
+// arrival counters, the partial sums; each from a multiple of 16 bytes on.
+struct Workspace {
+    size_t scales, counts, ids, arrivals, partials, total;
+    int64_t x_stride, x_scales_stride;
+    int32_t partials_most;
+    Workspace(int32_t B, int32_t D, int32_t V, bool mx) {
+        const auto whole = [](size_t n) { return (n + 15) / 16 * 16; };
+        const int64_t blocks = up(V, kBlockTokens);
+        x_stride = (int64_t)steps_of(D) * (mx ? kStep : kWideStep);
+        x_scales_stride = mx ? (int64_t)steps_of(D) * kStepScales : 0;
+        scales = (size_t)B * (size_t)x_stride;
+        counts = scales + whole((size_t)B * (size_t)x_scales_stride);
+        ids = counts + whole(blocks <= kMostBlocks ? blocks * sizeof(int32_t) : 0);
+        arrivals = ids + (blocks <= kMostBlocks ? blocks * kBlockTokens * sizeof(int32_t) : 0);
+        partials = arrivals + kMostArrivals * sizeof(uint32_t);
+        // twice the compute units' number of the largest tiles
+        partials_most = (int32_t)std::min<int64_t>((int64_t)kMostArrivals * 128 * 128, (int64_t)16 * up(B, 16) * 16 * (up(V, 128) * 128));
+        total = partials + (size_t)partials_most * sizeof(float);
+    }
+};
+
+// What the caller gives as states.
+struct States {
+    const void *x;
+    psc_form form;
+    int64_t stride;
+    const uint8_t *scales;
+    int64_t scales_stride;
+};
+
+// The rows that fit beside the blocks, then the others alone.
+template <bool kMx>
+void launch_prepare(const MxArgs &a, const States &x, int32_t rows, uint8_t *q, uint8_t *scales, int32_t *counts, int32_t *ids, hipStream_t s) {
+    for (int32_t first = 0; first == 0 || first < rows;) {
+        MxArgs part = a;
+        if (first) part.blocks = 0;
+        const int32_t n = (int32_t)std::min<int64_t>(rows - first, kMostGrid - part.blocks);
+        const dim3 grid((uint32_t)std::max(n + part.blocks, 1)), block(kPrepareBlock);
+        const auto go = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, grid, block, 0, s, part, first, n, x.x, x.stride, x.scales, x.scales_stride, q, scales, counts, ids);
+        };
+        if (x.form == PSC_FORM_MX4) {
+            if constexpr (kMx) go(prepare_mx_kernel<From::kMx, true>);
+        } else if (x.form == PSC_FORM_BF16) go(prepare_mx_kernel<From::kBf16, kMx>);
+        else go(prepare_mx_kernel<From::kF32, kMx>);
+        first += n;
+        if (n == 0) break;
+    }
+}
+
+template <bool kMx>
+psc_status head_mx(const char *what, MxArgs &a, const States &x, bool bf16, uint8_t *q, uint8_t *scales, int32_t *counts, int32_t *ids, bool direct, hipStream_t s) {
+    const auto run = [&](auto small) {
+        small.shape(a, false);
+        if (!direct || a.counts || a.splits > 1) {
+            launch_prepare<kMx>(a, x, direct ? 0 : a.B, q, scales, counts, ids, s);
+            // the product would go by whatever the workspace holds
+            if (psc_status st = launched_op(what)) return st;
+        }
+        small.launch(a, bf16, false, s);
+        return launched_op(what);
+    };
+    if constexpr (kMx) {
+        if (a.B <= 32) return run(Small<32, 64, 1, 4, 4, true>{});
+        if (a.B <= 64) return run(Small<64, 128, 1, 4, 3, true>{});
+        return run(Small<128, 128, 2, 4, 3, true>{});
+    } else {
+        if (a.B <= 16) return run(Small<16, 64, 1, 4, 4, false>{});
+        if (a.B <= 32) return run(Small<32, 64, 1, 4, 3, false>{});
+        return run(Small<64, 128, 1, 8, 3, false>{});
+    }
+}
+
+}  // namespace
+
+extern "C" size_t psc_head_mx_workspace(int32_t B, int32_t D, int32_t V, psc_form states) {
+    if (B <= 0 || D <= 0 || D > kMostD || V <= 0 || V > kMostV || (states != PSC_FORM_BF16 && states != PSC_FORM_MX4)) return 0;
+    return Workspace(B, D, V, states == PSC_FORM_MX4).total;
+}
+
+extern "C" psc_status psc_head_logits_mx(const void *x, psc_form x_form, int64_t x_stride, const uint8_t *x_scales, int64_t x_scales_stride,
+                                         int32_t B, int32_t D, psc_form states, const uint8_t *w, int64_t w_stride,
+                                         const uint8_t *w_scales, int64_t w_scales_stride, int32_t V, const float *bias,
+                                         const uint32_t *bitmask, void *logits, psc_dtype dtype, int64_t stride, void *workspace,
+                                         size_t workspace_bytes, void *stream) {
+    const char *what = "psc_head_logits_mx";
+    if (psc_status st = check_rows(what, logits, dtype, stride, B, V)) return st;
+    if (states != PSC_FORM_BF16 && states != PSC_FORM_MX4) return refuse(what, "states are multiplied in bfloat16 or in 4 bits");
+    if (x_form != PSC_FORM_F32 && x_form != PSC_FORM_BF16 && !(x_form == PSC_FORM_MX4 && states == PSC_FORM_MX4))
+        return refuse(what, "bad form of x");
+    if (D < 1 || D > kMostD) return refuse(what, "D outside [1, 131072]");
+    if (V > kMostV) return refuse(what, "V > 2^26");
+    if (B == 0 || V == 0) return PSC_OK;
+    if ((int64_t)up(B, 64) * up(V, 512) > kMostGrid) return refuse(what, "ceil(B / 64) * ceil(V / 512) >= 2^24");
+    if (!x || !w || !w_scales || !workspace) return refuse(what, "null pointer");
+    const int64_t blocks = up(D, kMxBlock);
+    if (x_form == PSC_FORM_MX4) {
+        if (!x_scales) return refuse(what, "null pointer");
+        if (x_stride % 16 || x_stride < blocks * 16 || !aligned_to(x, 16) || x_scales_stride < blocks)
+            return refuse(what, "rows of x start at 16 bytes and hold D elements, its scales one of every 32");
+    } else if (x_stride < 0 || !aligned_to(x, x_form == PSC_FORM_BF16 ? 2 : 4)) return refuse(what, "negative stride, or x off its elements' alignment");
+    if (w_stride % 16 || w_stride < blocks * 16 || w_stride > INT32_MAX / 512 || !aligned_to(w, 16))
+        return refuse(what, "rows of w start at 16 bytes and hold D elements");
+    if (w_scales_stride % 4 || w_scales_stride < blocks || w_scales_stride > INT32_MAX / 512 || !aligned_to(w_scales, 4))
+        return refuse(what, "rows of w_scales start at 4 bytes and hold one of every 32 elements");
+    if (workspace_bytes < psc_head_mx_workspace(B, D, V, states) || !aligned_to(workspace, kChunk))
+        return refuse(what, "the workspace is too small or not 16-byte aligned");
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    const bool mx = states == PSC_FORM_MX4;
+    const Workspace ws(B, D, V, mx);
+    uint8_t *const at = static_cast<uint8_t *>(workspace);
+    MxArgs a{};
+    a.x = at;
+    a.x_stride = ws.x_stride;
+    a.x_scales = at + ws.scales;
+    a.x_scales_stride = ws.x_scales_stride;
+    // States in bfloat16 that are whole steps at 16-byte addresses are read where they are.
+    const bool direct = !mx && x_form == PSC_FORM_BF16 && D % kStepElems == 0 && aligned_to(x, 16) && x_stride % 8 == 0 && (x_stride >= D || B == 1) &&
+                        x_stride <= (1 << 22);
+    if (direct) {
+        a.x = x;
+        a.x_stride = x_stride * 2;
+    }
+    a.w = w;
+    a.w_stride = w_stride;
+    a.w_scales = w_scales;
+    a.w_scales_stride = w_scales_stride;
+    a.w_blocks = (int32_t)blocks;
+    a.bias = bias;
+    a.bitmask = bitmask;
+    a.y = logits;
+    a.y_stride = stride;
+    a.B = B;
+    a.D = D;
+    a.V = V;
+    a.W = up(V, 32);
+    a.steps = steps_of(D);
+    a.partials = reinterpret_cast<int32_t *>(at + ws.partials);
+    a.partials_most = ws.partials_most;
+    a.arrivals = reinterpret_cast<uint32_t *>(at + ws.arrivals);
+    a.arrivals_most = kMostArrivals;
+    // The needed tokens are listed where offsets of all weights fit 32 bits.
+    int32_t *counts = nullptr, *ids = nullptr;
+    if (bitmask && up(V, kBlockTokens) <= kMostBlocks && (int64_t)V * w_stride < kMostBytes && (int64_t)V * w_scales_stride < kMostBytes) {
+        a.blocks = up(V, kBlockTokens);
+        a.counts = counts = reinterpret_cast<int32_t *>(at + ws.counts);
+        a.ids = ids = reinterpret_cast<int32_t *>(at + ws.ids);
+        a.gather_most = V / 2;
+    }
+    const States given{x, x_form, x_stride, x_scales, x_scales_stride};
+    uint8_t *const scales = at + ws.scales;
+    return mx ? head_mx<true>(what, a, given, dtype == PSC_BF16, at, scales, counts, ids, direct, s)
+              : head_mx<false>(what, a, given, dtype == PSC_BF16, at, scales, counts, ids, direct, s);
+}

@@ -15,6 +15,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpsc.so")
 
 PSC_F32, PSC_BF16 = 0, 1
+FORM_F32, FORM_BF16, FORM_I8, FORM_MX4 = range(4)
 ADV_OK, ADV_REJECTED, ADV_EOS, ADV_OVERFLOW, ADV_BAD_INPUT, ADV_SKIPPED = range(6)
 _STATUS = {0: "PSC_OK", -1: "PSC_E_INVALID_ARG", -2: "PSC_E_GRAMMAR", -3: "PSC_E_NOT_LALR1", -4: "PSC_E_OOM",
            -5: "PSC_E_DEVICE", -6: "PSC_E_NOT_BOUND", -7: "PSC_E_LIMIT", -8: "PSC_E_IO", -9: "PSC_E_FORMAT",
@@ -30,7 +31,8 @@ EXPORTED = ["psc_build", "psc_info", "psc_device_bytes", "psc_bind_device", "psc
             "psc_predictor_fill", "psc_predictor_updates", "psc_timeline_records", "psc_compute_and_apply_timeline",
             "psc_set_options", "psc_compute_and_argmax_noalloc", "psc_grammar_compile", "psc_grammar_view",
             "psc_grammar_symbol_name", "psc_grammar_free", "psc_build_from_text", "psc_quantize_rows",
-            "psc_head_workspace", "psc_head_logits", "psc_penalize", "psc_append_tokens", "psc_sample_workspace",
+            "psc_head_workspace", "psc_head_logits", "psc_head_logits_i8", "psc_quantize_mx", "psc_lookup_rows",
+            "psc_add_rms_norm", "psc_head_mx_workspace", "psc_head_logits_mx", "psc_penalize", "psc_append_tokens", "psc_sample_workspace",
             "psc_sample"]
 
 BIND_FLAT, BIND_SLICED = 1, 2
@@ -234,6 +236,14 @@ def lib() -> C.CDLL:
         L.psc_head_workspace.restype = C.c_size_t
         L.psc_head_logits.argtypes = [P, C.c_int, I64, I32, I32, P, I64, P, I32, P, P, P, C.c_int, I64, P,
                                       C.c_size_t, P]
+        L.psc_head_logits_i8.argtypes = [P, I64, P, I32, I32, P, I64, P, I32, P, P, P, C.c_int, I64, P, C.c_size_t, P]
+        L.psc_quantize_mx.argtypes = [P, C.c_int, I64, I64, I32, P, I64, P, I64, P]
+        L.psc_lookup_rows.argtypes = [C.c_int, P, I64, P, I64, I64, I32, P, I64, P, C.c_int, I64, P]
+        L.psc_add_rms_norm.argtypes = [P, C.c_int, I64, P, C.c_int, I64, I64, I32, P, C.c_float, C.c_int, P, I64, P, I64, P]
+        L.psc_head_mx_workspace.argtypes = [I32, I32, I32, C.c_int]
+        L.psc_head_mx_workspace.restype = C.c_size_t
+        L.psc_head_logits_mx.argtypes = [P, C.c_int, I64, P, I64, I32, I32, C.c_int, P, I64, P, I64, I32, P, P, P, C.c_int,
+                                         I64, P, C.c_size_t, P]
         L.psc_penalize.argtypes = [P, C.c_int, I64, I32, I32, P, P, P]
         L.psc_append_tokens.argtypes = [P, I32, P, I32, P, P, P]
         L.psc_sample_workspace.argtypes = [I32, I32, C.c_int]
@@ -251,7 +261,8 @@ def lib() -> C.CDLL:
                      "psc_compute_and_argmax_n", "psc_predictor_fill", "psc_predictor_updates",
                      "psc_compute_and_apply_timeline", "psc_set_options", "psc_compute_and_argmax_noalloc",
                      "psc_grammar_compile", "psc_grammar_view", "psc_build_from_text", "psc_quantize_rows",
-                     "psc_head_logits", "psc_penalize", "psc_append_tokens", "psc_sample"):
+                     "psc_head_logits", "psc_head_logits_i8", "psc_quantize_mx", "psc_lookup_rows", "psc_add_rms_norm",
+                     "psc_head_logits_mx", "psc_penalize", "psc_append_tokens", "psc_sample"):
             getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -755,13 +766,47 @@ def quantize_rows(x, stream=None):
     return q[:, :D], scales
 
 
-def head_logits(x, w, w_scales, dtype=None, bias=None, bitmask=None, out=None, stream=None):
+def _logits_out(out, dtype, default, B: int, V: int, device, stream):
+    """(out, its dtype code and row stride): logits [B, V], new ones of `dtype` (or `default`) where out is None."""
+    T = _T or _torch_types()
+    if out is not None:
+        _require(dtype is None or dtype == out.dtype, "dtype to be that of out")
+        return (out, *_rows(out, "out", device.index, (B, V)))
+    code = T["codes"].get(default if dtype is None else dtype)
+    if code is None:
+        _require(False, f"float32 or bfloat16 logits, not {dtype}")
+    return _new((B, V), ("f32", "bf16")[code], device, stream), code, V
+
+
+def _packed(t, name: str, dtype: str, cols: int, align: int, dev: int) -> int:
+    """The row stride of t, a matrix of bytes of `dtype` with `cols` adjacent columns and rows that start at multiples
+    of `align` bytes."""
+    T = _T or _torch_types()
+    if not (isinstance(t, T["tensor"]) and t.dtype is T[dtype] and t.dim() == 2 and t.shape[1] == cols and cols > 0):
+        _require(False, f"{name} to be a matrix of {T[dtype]} with {cols} columns")
+    whole = (cols + align - 1) // align * align
+    stride = t.stride(0) if t.shape[0] > 1 else whole
+    _require(t.get_device() == dev and (cols == 1 or t.stride(1) == 1) and stride >= whole and stride % align == 0
+             and t.data_ptr() % align == 0,
+             f"{name} on device {dev}, with adjacent elements and rows that start at multiples of {align} bytes")
+    return stride
+
+
+def head_logits(x, w, w_scales, dtype=None, bias=None, bitmask=None, out=None, stream=None, x_scales=None):
     """Logits [B, V] of hidden states x [B, D] by 8-bit weights w [V, D] with a
     scale per token (quantize_rows), forbidden tokens -inf (psc_head_logits).
     `out`: where to write them (its rows may lie apart); else a new tensor of
-    `dtype`, that of x by default."""
+    `dtype`, that of x by default.  States that are in 8 bits already (x int8
+    with x_scales float32 [B], as quantize_rows and add_rms_norm return them)
+    are taken as they are, to bfloat16 logits by default (psc_head_logits_i8)."""
     T = _T or _torch_types()
-    x_code, x_stride = _rows(x, "x")
+    if x_scales is None:
+        x_code, x_stride = _rows(x, "x")
+        default = x.dtype
+    else:
+        _require(isinstance(x, T["tensor"]) and x.dim() == 2 and x.get_device() >= 0 and x.get_device() == T["device"](),
+                 "x to be a matrix on the current device")
+        x_stride, default = _packed(x, "x", "i8", x.shape[1], 16, x.get_device()), T["bf16"]
     B, D = x.shape
     dev = x.get_device()
     if not (isinstance(w, T["tensor"]) and w.dtype is T["i8"] and w.dim() == 2 and w.shape[1] == D and D > 0):
@@ -770,23 +815,159 @@ def head_logits(x, w, w_scales, dtype=None, bias=None, bitmask=None, out=None, s
     w_stride = w.stride(0) if V > 1 else (D + 15) // 16 * 16
     _require(w.get_device() == dev and (D == 1 or w.stride(1) == 1) and w_stride >= D and w_stride % 16 == 0
              and w.data_ptr() % 16 == 0, "w on x's device, with adjacent elements and rows that start at 16 bytes")
-    if out is None:
-        code, y_stride = T["codes"].get(x.dtype if dtype is None else dtype), V
-        if code is None:
-            _require(False, f"float32 or bfloat16 logits, not {dtype}")
-        out = _new((B, V), ("f32", "bf16")[code], x.device, stream)
-    else:
-        _require(dtype is None or dtype == out.dtype, "dtype to be that of out")
-        code, y_stride = _rows(out, "out", dev, (B, V))
+    out, code, y_stride = _logits_out(out, dtype, default, B, V, x.device, stream)
     L = lib()
     scales = _vector(w_scales, "w_scales", "f32", dev, (V,))
     _require(scales is not None, "w_scales")
     bias = _vector(bias, "bias", "f32", dev, (V,))
     words = _vector(bitmask, "bitmask", "i32", dev, (B, (V + 31) // 32))
+    given = _vector(x_scales, "x_scales", "f32", dev, (B,))
     n = L.psc_head_workspace(B, D, V)
     ws = _new(n, "u8", x.device, stream)
-    _check(L.psc_head_logits(x.data_ptr(), x_code, x_stride, B, D, w.data_ptr(), w_stride, scales, V, bias, words,
-                             out.data_ptr(), code, y_stride, ws.data_ptr(), n, _stream_ptr(stream)))
+    rest = (B, D, w.data_ptr(), w_stride, scales, V, bias, words, out.data_ptr(), code, y_stride, ws.data_ptr(), n,
+            _stream_ptr(stream))
+    _check(L.psc_head_logits(x.data_ptr(), x_code, x_stride, *rest) if given is None
+           else L.psc_head_logits_i8(x.data_ptr(), x_stride, given, *rest))
+    return out
+
+
+MX_BLOCK = 32
+_STATES = {"bf16": FORM_BF16, "mx4": FORM_MX4}
+
+
+def quantize_mx(x, stream=None):
+    """(q, scales): the rows of x [N, D] in microscaled 4-bit floating point
+    (psc_quantize_mx): uint8 [N, ceil(D / 2)], the even elements in the low
+    halves, and of every 32 elements the power of two, uint8 [N, ceil(D / 32)];
+    the rows of both start at multiples of 16 bytes."""
+    code, stride = _rows(x, "x")
+    n, D = x.shape
+    blocks = (D + MX_BLOCK - 1) // MX_BLOCK
+    q_stride, s_stride = blocks * 16, (blocks + 15) // 16 * 16
+    q, scales = _new((n, q_stride), "u8", x.device, stream), _new((n, s_stride), "u8", x.device, stream)
+    _check(lib().psc_quantize_mx(x.data_ptr(), code, stride, n, D, q.data_ptr(), q_stride, scales.data_ptr(), s_stride,
+                                 _stream_ptr(stream)))
+    return q[:, :(D + 1) // 2], scales[:, :blocks]
+
+
+def lookup_rows(q, scales, ids=None, D=None, dtype=None, out=None, stream=None):
+    """Rows `ids` (int32 [n]; None: all, in order) of a quantised table as
+    numbers [n, D] (psc_lookup_rows): q and scales as quantize_rows or
+    quantize_mx return them, D that of the table where it is odd and in 4 bits.
+    A row whose id is outside the table is zeros.  `out`: where to write them;
+    else a new tensor of `dtype`, bfloat16 by default."""
+    T = _T or _torch_types()
+    _require(isinstance(q, T["tensor"]) and q.dim() == 2 and q.dtype in (T["i8"], T["u8"]) and q.get_device() >= 0
+             and q.get_device() == T["device"](), "q to be an int8 or uint8 matrix on the current device")
+    (rows, cols), dev, mx = q.shape, q.get_device(), q.dtype is T["u8"]
+    if D is None:
+        D = cols * 2 if mx else cols
+    _require(cols == ((D + 1) // 2 if mx else D), f"q of rows of {D} elements")
+    n = rows
+    if ids is not None:
+        _require(isinstance(ids, T["tensor"]) and ids.dim() == 1, "ids to be a vector")
+        n = ids.shape[0]
+    if out is None:
+        code, out_stride = T["codes"].get(T["bf16"] if dtype is None else dtype), D
+        if code is None:
+            _require(False, f"float32 or bfloat16 rows, not {dtype}")
+        out = _new((n, D), ("f32", "bf16")[code], q.device, stream)
+    else:
+        _require(dtype is None or dtype == out.dtype, "dtype to be that of out")
+        code, out_stride = _rows(out, "out", dev, (n, D))
+    if D == 0 or n == 0:
+        return out
+    at_ids = _vector(ids, "ids", "i32", dev, (n,))
+    q_stride, s_stride = _packed(q, "q", "u8" if mx else "i8", cols, 16, dev), 0
+    if mx:
+        s_stride = _packed(scales, "scales", "u8", (D + MX_BLOCK - 1) // MX_BLOCK, 4, dev)
+        _require(scales.shape[0] == rows, f"scales of {rows} rows")
+        at = scales.data_ptr()
+    else:
+        at = _vector(scales, "scales", "f32", dev, (rows,))
+        _require(at is not None, "scales")
+    _check(lib().psc_lookup_rows(FORM_MX4 if mx else FORM_I8, q.data_ptr(), q_stride, at, s_stride, rows, D, at_ids, n,
+                                 out.data_ptr(), code, out_stride, _stream_ptr(stream)))
+    return out
+
+
+def add_rms_norm(x, gain=None, residual=None, eps=1e-6, to=None, stream=None):
+    """The root-mean-square norm of x [N, D], or of residual + x, which then
+    becomes the residual [N, D], in place; times gain (float32 [D]) where given
+    (psc_add_rms_norm).  `to`: float32 or bfloat16 (None: x's type), then the
+    result is a matrix; "i8" or "mx4", then it is (q, scales) as quantize_rows
+    or quantize_mx return them, for head_logits and head_logits_mx."""
+    T = _T or _torch_types()
+    code, stride = _rows(x, "x")
+    (n, D), dev = x.shape, x.get_device()
+    r_at, r_code, r_stride = None, PSC_F32, 0
+    if residual is not None:
+        r_code, r_stride = _rows(residual, "residual", dev, (n, D))
+        r_at = residual.data_ptr()
+    at_gain = _vector(gain, "gain", "f32", dev, (D,))
+    eps = float(eps)
+    _require(eps >= 0, "eps of at least 0")
+    scales, s_at, s_stride = None, None, 0
+    if to == "i8":
+        form, o_stride = FORM_I8, (D + 15) // 16 * 16
+        out, scales = _new((n, o_stride), "i8", x.device, stream), _new(n, "f32", x.device, stream)
+        got = out[:, :D], scales
+    elif to == "mx4":
+        blocks = (D + MX_BLOCK - 1) // MX_BLOCK
+        form, o_stride, s_stride = FORM_MX4, blocks * 16, (blocks + 15) // 16 * 16
+        out, scales = _new((n, o_stride), "u8", x.device, stream), _new((n, s_stride), "u8", x.device, stream)
+        got = out[:, :(D + 1) // 2], scales[:, :blocks]
+    else:
+        form, o_stride = T["codes"].get(x.dtype if to is None else to), D
+        if form is None:
+            _require(False, f'to: float32, bfloat16, "i8" or "mx4", not {to}')
+        out = got = _new((n, D), ("f32", "bf16")[form], x.device, stream)
+    if scales is not None:
+        s_at = scales.data_ptr()
+    _check(lib().psc_add_rms_norm(x.data_ptr(), code, stride, r_at, r_code, r_stride, n, D, at_gain, eps, form,
+                                  out.data_ptr(), o_stride, s_at, s_stride, _stream_ptr(stream)))
+    return got
+
+
+def head_logits_mx(x, w, w_scales, states="bf16", x_scales=None, dtype=None, bias=None, bitmask=None, out=None,
+                   stream=None):
+    """Logits [B, V] of hidden states x [B, D] by 4-bit weights w [V, ceil(D / 2)]
+    with w_scales [V, ceil(D / 32)] (quantize_mx), forbidden tokens -inf
+    (psc_head_logits_mx).  `states`: what the products take them in, "bf16", or
+    "mx4", quantised as by quantize_mx.  States that are in 4 bits already (x
+    uint8 with x_scales, as quantize_mx and add_rms_norm return them) are taken
+    as they are.  `out`: where to write the logits; else a new tensor of
+    `dtype`, by default that of x, of states in 4 bits bfloat16."""
+    T = _T or _torch_types()
+    _require(states in _STATES, 'states: "bf16" or "mx4"')
+    x_at, x_s_stride = None, 0
+    if x_scales is None:
+        x_code, x_stride = _rows(x, "x")
+        (B, D), dev, default = x.shape, x.get_device(), x.dtype
+        cols, blocks = (D + 1) // 2, (D + MX_BLOCK - 1) // MX_BLOCK
+    else:
+        _require(isinstance(x, T["tensor"]) and x.dim() == 2 and x.get_device() >= 0 and x.get_device() == T["device"](),
+                 "x to be a matrix on the current device")
+        (B, cols), dev, default, states, x_code = x.shape, x.get_device(), T["bf16"], "mx4", FORM_MX4
+        D = cols * 2          # an odd row's last code is zero
+        blocks = (D + MX_BLOCK - 1) // MX_BLOCK
+        x_stride = _packed(x, "x", "u8", cols, 16, dev)
+        x_s_stride = _packed(x_scales, "x_scales", "u8", blocks, 1, dev)
+        _require(x_scales.shape[0] == B, f"x_scales of {B} rows")
+        x_at = x_scales.data_ptr()
+    w_stride = _packed(w, "w", "u8", cols, 16, dev)
+    s_stride = _packed(w_scales, "w_scales", "u8", blocks, 4, dev)
+    V = w.shape[0]
+    _require(w_scales.shape[0] == V, f"w_scales of {V} rows")
+    out, code, y_stride = _logits_out(out, dtype, default, B, V, x.device, stream)
+    L, form = lib(), _STATES[states]
+    bias = _vector(bias, "bias", "f32", dev, (V,))
+    words = _vector(bitmask, "bitmask", "i32", dev, (B, (V + 31) // 32))
+    n = L.psc_head_mx_workspace(B, D, V, form)
+    ws = _new(n, "u8", x.device, stream)
+    _check(L.psc_head_logits_mx(x.data_ptr(), x_code, x_stride, x_at, x_s_stride, B, D, form, w.data_ptr(), w_stride,
+                                w_scales.data_ptr(), s_stride, V, bias, words, out.data_ptr(), code, y_stride,
+                                ws.data_ptr(), n, _stream_ptr(stream)))
     return out
 
 
