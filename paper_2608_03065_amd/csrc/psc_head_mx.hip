@@ -6,6 +6,8 @@
 // bfloat16 states the same 16 bytes are converted to bfloat16 times their power,
 // which holds them exactly, and go through four matrix instructions of 32
 // elements each, of which a lane has 8.  Sums are float32.
+#include <type_traits>
+
 #include "psc_head.hpp"
 #include "psc_mx.hpp"
 
@@ -19,14 +21,15 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kStepElems = kStep * 2;              // a line of codes
 constexpr int kStepScales = kStepElems / kMxBlock; // and its scales, in bytes
+constexpr int kPairScales = 2 * kStepScales;       // those of two lines are loaded at once
+constexpr int kScaleRows = 256;                    // the states' are held in tiles of so many rows: [tiles][pairs of lines][rows][16]
 constexpr int kWideStep = kStepElems * 2;          // the same elements in bfloat16
 constexpr uint32_t kOne = 127;                     // the scale of 1
 
 struct MxArgs : HeadBase {
     const void *x;                // states: codes or bfloat16, zeros from D up to whole steps
     int64_t x_stride;             // in bytes
-    const uint8_t *x_scales;      // of codes, whole steps too
-    int64_t x_scales_stride;
+    const uint8_t *x_scales;      // of codes, whole pairs of steps, in tiles
     const uint8_t *w;
     int64_t w_stride;
     const uint8_t *w_scales;
@@ -35,6 +38,12 @@ struct MxArgs : HeadBase {
 };
 
 // ---------------------------------------------------------------- prepare
+
+// The byte of a state's scale.
+__host__ __device__ __forceinline__ int64_t scale_at(int32_t steps, int64_t row, int32_t block) {
+    const int64_t pairs = (steps + 1) / 2;
+    return ((row / kScaleRows * pairs + block / kPairScales) * kScaleRows + row % kScaleRows) * kPairScales + block % kPairScales;
+}
 
 // Workgroups 0 .. rows - 1: a row of states each, to codes, or to bfloat16, or
 // copied codes; the others a block of needed tokens each; all of them clear
@@ -46,7 +55,8 @@ __device__ __forceinline__ void prepare_row(const MxArgs &a, int64_t r, const vo
                                             const uint8_t *__restrict__ x_scales, int64_t x_scales_stride, uint8_t *__restrict__ q,
                                             uint8_t *__restrict__ scales) {
     const int32_t padded = a.steps * kStepElems, blocks = (a.D + kMxBlock - 1) / kMxBlock;
-    uint8_t *const to = q + r * a.x_stride, *const to_scales = scales + r * a.x_scales_stride;
+    uint8_t *const to = q + r * a.x_stride;
+    const auto put_scale = [&](int32_t block, uint32_t scale) { scales[scale_at(a.steps, r, block)] = (uint8_t)scale; };
     for (int32_t d = threadIdx.x * kVec; d < padded; d += kPrepareBlock * kVec) {
         if constexpr (kFrom == From::kMx) {
             const uint8_t *const from = static_cast<const uint8_t *>(x) + r * x_stride;
@@ -54,7 +64,7 @@ __device__ __forceinline__ void prepare_row(const MxArgs &a, int64_t r, const vo
             if (d < a.D) __builtin_memcpy(&codes, from + d / 2, 4);
             if (d + kVec > a.D) codes &= d < a.D ? ~(~0u << (4 * (a.D - d))) : 0u;
             __builtin_memcpy(to + d / 2, &codes, 4);
-            if (threadIdx.x % 4 == 0) to_scales[d / kMxBlock] = d / kMxBlock < blocks ? x_scales[r * x_scales_stride + d / kMxBlock] : 0;
+            if (threadIdx.x % 4 == 0) put_scale(d / kMxBlock, d / kMxBlock < blocks ? x_scales[r * x_scales_stride + d / kMxBlock] : 0);
         } else {
             float v[kVec];
             load_eight<kFrom == From::kBf16>(static_cast<const char *>(x) + r * x_stride * (kFrom == From::kBf16 ? 2 : 4), d, a.D, v);
@@ -62,7 +72,7 @@ __device__ __forceinline__ void prepare_row(const MxArgs &a, int64_t r, const vo
                 uint32_t scale;
                 const uint32_t codes = to_mx4(v, scale);
                 __builtin_memcpy(to + d / 2, &codes, 4);
-                if (threadIdx.x % 4 == 0) to_scales[d / kMxBlock] = (uint8_t)scale;
+                if (threadIdx.x % 4 == 0) put_scale(d / kMxBlock, scale);
             } else {
                 store_eight<true>(to, d, padded, v);
             }
@@ -139,9 +149,11 @@ struct Extras {
 
 // ---------------------------------------------------------------- products
 
+// Of the scales, byte kByte.
+template <int kByte>
 __device__ __forceinline__ f32x4 product(const u32x4 &w, uint32_t w_scale, const u32x4 &x, uint32_t x_scale, const f32x4 &sum) {
     const i32x8 a = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0}, b = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, sum, 4, 4, 0, (int)w_scale, 0, (int)x_scale);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, sum, 4, 4, kByte, (int)w_scale, kByte, (int)x_scale);
 }
 
 __device__ __forceinline__ f32x4 product(const bf16x8 &w, const bf16x8 &x, const f32x4 &sum) {
@@ -171,8 +183,9 @@ __device__ __forceinline__ void load_word_to_lds(u32x4 from, uint32_t offset, ui
 
 // One workgroup computes kM states by kN tokens over a part of D.  Steps of 256
 // elements of all its rows go straight from memory into one of kStages buffers
-// in LDS, kStages - 1 steps ahead: a line of codes of every token and 8 bytes
-// of its scales, and of every state the same or four lines of bfloat16.  A
+// in LDS, kStages - 1 steps ahead: a line of codes of every token, and of every
+// state the same or four lines of bfloat16; with every second step, 16 bytes of
+// scales of each row of codes, those of both.  A
 // row's 16-byte chunk c lies at place c ^ (row & 7) of its line, and of a state in
 // bfloat16 at c ^ (row & 15), so that the 16 rows that a matrix instruction reads
 // at one chunk fall into different banks; since a load puts lane l's chunk at
@@ -187,12 +200,14 @@ __device__ __forceinline__ void small_mx_body(const MxArgs &a, bool gather_only)
     constexpr int kLoadsW = kN * kStep / 1024 / kWaves;
     static_assert(kLoadsW * kWaves * 1024 == kN * kStep, "every wavefront loads as much");
     constexpr int kX1024 = kM * kXStep / 1024, kLoadsX = (kX1024 + kWaves - 1) / kWaves;
-    constexpr int kRowsPerWord = 32, kS256 = kN / kRowsPerWord, kLoadsS = (kS256 + kWaves - 1) / kWaves;
-    constexpr int kT256 = kMx ? (kM + kRowsPerWord - 1) / kRowsPerWord : 0, kLoadsT = (kT256 + kWaves - 1) / kWaves;
-    constexpr int kLoads = kLoadsW + kLoadsX + kLoadsS + kLoadsT;
-    static_assert((kStages - 2) * kLoads < 64, "the counter's range");
-    constexpr int kAtX = kN * kStep, kAtS = kAtX + kX1024 * 1024, kAtT = kAtS + kS256 * 256, kStage = kAtT + kT256 * 256;
-    constexpr int kRest = kStages * kStage;       // where loads of nothing go
+    constexpr int kRowsS = kN + (kMx ? kM : 0), kS1024 = (kRowsS + kWave - 1) / kWave, kLoadsS = (kS1024 + kWaves - 1) / kWaves;
+    static_assert(kN % kWave == 0, "a load has the scales of tokens, or of states");
+    constexpr int kLoads = kLoadsW + kLoadsX;
+    static_assert(kStages == 3 || kStages == 4, "what is waited for");
+    static_assert(2 * kLoads + kLoadsS < 64, "the counter's range");
+    constexpr int kAtX = kN * kStep, kStage = kAtX + kX1024 * 1024;
+    constexpr int kGroups = kStages == 3 ? 2 : 3, kAtS = kStages * kStage;       // pairs of steps whose scales are held
+    constexpr int kRest = kAtS + kGroups * kS1024 * 1024;                       // where loads of nothing go
     __shared__ __align__(1024) uint8_t lds[kRest + 1024];
     __shared__ int32_t s_ids[kN];
     __shared__ uint32_t s_arrived;
@@ -227,7 +242,8 @@ __device__ __forceinline__ void small_mx_body(const MxArgs &a, bool gather_only)
     }
     const int32_t split = (int32_t)blockIdx.x / tiles, tile = (int32_t)blockIdx.x - split * tiles;
     const int32_t m0 = tile % a.m_tiles * kM, n0 = tile / a.m_tiles * kN;
-    const int32_t first = a.steps * split / plan.splits, steps = a.steps * (split + 1) / plan.splits;
+    const int32_t pairs = (a.steps + 1) / 2;          // a part is whole pairs of steps
+    const int32_t first = pairs * split / plan.splits * 2, steps = min(a.steps, pairs * (split + 1) / plan.splits * 2);
 
     if (plan.gather) {
         // token n0 + i of the needed ones: its block by bisection of the sums before each
@@ -251,9 +267,10 @@ __device__ __forceinline__ void small_mx_body(const MxArgs &a, bool gather_only)
     const u32x4 rw = rows_from(a.w + (int64_t)w_row * a.w_stride, code_bytes(a, w_row));
     const u32x4 rs = rows_from(a.w_scales + (int64_t)w_row * a.w_scales_stride, scale_bytes(a, w_row));
     const u32x4 rx = rows_from(static_cast<const char *>(a.x) + (int64_t)m0 * a.x_stride, (int64_t)(a.B - m0 - 1) * a.x_stride + (int64_t)a.steps * kXStep);
-    const u32x4 rt = kMx ? rows_from(a.x_scales + (int64_t)m0 * a.x_scales_stride, (int64_t)(a.B - m0) * a.x_scales_stride) : rs;
+    // from the tile's first pair on, its rows from m0 on
+    const u32x4 rt = kMx ? rows_from(a.x_scales + scale_at(a.steps, m0, 0), (int64_t)pairs * kScaleRows * kPairScales - m0 % kScaleRows * kPairScales) : rs;
     // offsets of the lane's loads; past the last step, and for rows that there are not, they read nothing
-    uint32_t from_w[kLoadsW], from_x[kLoadsX], from_s[kLoadsS], from_t[kLoadsT ? kLoadsT : 1];
+    uint32_t from_w[kLoadsW], from_x[kLoadsX], from_s[kLoadsS];
     const auto token = [&](int row, int64_t stride) {
         if (!plan.gather) return (uint32_t)row * (uint32_t)stride;
         return s_ids[row] >= 0 ? (uint32_t)s_ids[row] * (uint32_t)stride : kNowhere;
@@ -272,34 +289,27 @@ __device__ __forceinline__ void small_mx_body(const MxArgs &a, bool gather_only)
     }
 #pragma unroll
     for (int i = 0; i < kLoadsS; i++) {
-        const int row = (i * kWaves + wave) * kRowsPerWord + lane / 2;
-        const uint32_t at = row < kN ? token(row, a.w_scales_stride) : kNowhere;
-        from_s[i] = at == kNowhere ? at : at + (lane & 1) * 4;
+        const int row = (i * kWaves + wave) * kWave + lane;
+        if (row < kN) from_s[i] = token(row, a.w_scales_stride);
+        else from_s[i] = row < kRowsS ? (uint32_t)(row - kN) * kPairScales : kNowhere;
     }
-#pragma unroll
-    for (int i = 0; i < kLoadsT; i++) {
-        const int row = (i * kWaves + wave) * kRowsPerWord + lane / 2;
-        from_t[i] = row < kM && m0 + row < a.B ? (uint32_t)row * (uint32_t)a.x_scales_stride + (lane & 1) * 4 : kNowhere;
-    }
-    const auto fetch = [&](int32_t step) {
+    const auto fetch = [&](int32_t step, bool even) {
         const uint32_t base = lds_byte(lds), to = base + (uint32_t)(step % kStages) * kStage;
-        const auto off = [&](uint32_t from, uint32_t bytes) { return step < steps && from != kNowhere ? from + (uint32_t)step * bytes : kNowhere; };
+        const auto off = [&](uint32_t from, uint32_t bytes) { return step < steps && from != kNowhere ? from + bytes : kNowhere; };
+        if (even)
 #pragma unroll
-        for (int i = 0; i < kLoadsW; i++) load_to_lds(rw, off(from_w[i], kStep), to + (uint32_t)(i * kWaves + wave) * 1024u);
+            for (int i = 0; i < kLoadsS; i++) {
+                const int n = i * kWaves + wave;
+                const bool states = n * kWave >= kN;
+                load_to_lds(states ? rt : rs, off(from_s[i], (uint32_t)(step / 2) * (states ? kScaleRows * kPairScales : kPairScales)),
+                            n < kS1024 ? base + kAtS + (uint32_t)(step / 2 % kGroups * kS1024 + n) * 1024u : base + kRest);
+            }
+#pragma unroll
+        for (int i = 0; i < kLoadsW; i++) load_to_lds(rw, off(from_w[i], (uint32_t)step * kStep), to + (uint32_t)(i * kWaves + wave) * 1024u);
 #pragma unroll
         for (int i = 0; i < kLoadsX; i++) {
             const int n = i * kWaves + wave;
-            load_to_lds(rx, off(from_x[i], kXStep), n < kX1024 ? to + kAtX + (uint32_t)n * 1024u : base + kRest);
-        }
-#pragma unroll
-        for (int i = 0; i < kLoadsS; i++) {
-            const int n = i * kWaves + wave;
-            load_word_to_lds(rs, off(from_s[i], kStepScales), n < kS256 ? to + kAtS + (uint32_t)n * 256u : base + kRest);
-        }
-#pragma unroll
-        for (int i = 0; i < kLoadsT; i++) {
-            const int n = i * kWaves + wave;
-            load_word_to_lds(rt, off(from_t[i], kStepScales), n < kT256 ? to + kAtT + (uint32_t)n * 256u : base + kRest);
+            load_to_lds(rx, off(from_x[i], (uint32_t)step * kXStep), n < kX1024 ? to + kAtX + (uint32_t)n * 1024u : base + kRest);
         }
     };
     f32x4 acc[kTn][kTm] = {};
@@ -308,12 +318,10 @@ __device__ __forceinline__ void small_mx_body(const MxArgs &a, bool gather_only)
     Extras<kTn, kTm, kPlain> extras;
     if (!plan.gather && plan.splits == 1) extras.load(a, v0, m0, b0 - m0);
 #pragma unroll
-    for (int s = 0; s < kStages - 1; s++) fetch(first + s);
+    for (int s = 0; s < kStages - 1; s++) fetch(first + s, s % 2 == 0);
     if (fill) fill_forbidden<kBf16, 1>(a, blockIdx.x, gridDim.x);
-    for (int32_t step = first; step < steps; step++) {
-        wait_and_meet<(kStages - 2) * kLoads>();   // the step has landed, and its predecessor's buffer is free
-        fetch(step + kStages - 1);
-        const uint8_t *const at = lds + step % kStages * kStage;
+    const auto turn = [&](int32_t step, bool even) {
+        const uint8_t *const at = lds + step % kStages * kStage, *const scales = lds + kAtS + step / 2 % kGroups * kS1024 * 1024 + (even ? 0 : kStepScales);
         const int left = a.w_blocks - step * kStepScales - quad;       // of the lane's first block: blocks up to the row's end
 #pragma unroll
         for (int k = 0; k < kStepElems / 128; k++) {
@@ -323,7 +331,7 @@ __device__ __forceinline__ void small_mx_body(const MxArgs &a, bool gather_only)
             for (int i = 0; i < kTn; i++) {
                 const int row = (wn * kTn + i) * 16 + r16;
                 fw[i] = *reinterpret_cast<const u32x4 *>(at + row * kStep + (((k * 4 + quad) ^ (row & 7)) * kChunk));
-                const uint32_t word = *reinterpret_cast<const uint32_t *>(at + kAtS + row * kStepScales + k * 4);
+                const uint32_t word = *reinterpret_cast<const uint32_t *>(scales + row * kPairScales + k * 4);
                 sw[i] = left > k * 4 ? (word >> (8 * quad)) & 255u : kOne;
             }
             if constexpr (kMx) {
@@ -333,12 +341,12 @@ __device__ __forceinline__ void small_mx_body(const MxArgs &a, bool gather_only)
                 for (int j = 0; j < kTm; j++) {
                     const int row = (wm * kTm + j) * 16 + r16;
                     fx[j] = *reinterpret_cast<const u32x4 *>(at + kAtX + row * kStep + (((k * 4 + quad) ^ (row & 7)) * kChunk));
-                    sx[j] = *reinterpret_cast<const uint32_t *>(at + kAtT + row * kStepScales + k * 4) >> (8 * quad);
+                    sx[j] = *reinterpret_cast<const uint32_t *>(scales + (kN + row) * kPairScales + k * 4) >> (8 * quad);
                 }
 #pragma unroll
                 for (int i = 0; i < kTn; i++)
 #pragma unroll
-                    for (int j = 0; j < kTm; j++) acc[i][j] = product(fw[i], sw[i], fx[j], sx[j], acc[i][j]);
+                    for (int j = 0; j < kTm; j++) acc[i][j] = product<0>(fw[i], sw[i], fx[j], sx[j], acc[i][j]);
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
@@ -357,6 +365,16 @@ __device__ __forceinline__ void small_mx_body(const MxArgs &a, bool gather_only)
                 }
             }
         }
+    };
+    // of the loads after the step's own: kStages - 2 steps of them, of which scales come with the even ones
+    for (int32_t step = first; step < steps; step += 2) {
+        wait_and_meet<(kStages - 2) * kLoads + (kStages == 4 ? kLoadsS : 0)>();   // the step has landed, and its predecessor's buffer is free
+        fetch(step + kStages - 1, kStages == 3);
+        turn(step, true);
+        if (step + 1 == steps) break;
+        wait_and_meet<(kStages - 2) * kLoads + kLoadsS>();
+        fetch(step + kStages, kStages == 4);
+        turn(step + 1, false);
     }
     if (plan.splits > 1) {
         // The sums go to memory at device scope, which every XCD sees alike, and
@@ -445,6 +463,317 @@ small_mx_kernel(const MxArgs a, bool gather_only) {
     small_mx_body<kM, kN, kWavesM, kWavesN, kStages, kMx, kBf16, kPlain>(a, gather_only);
 }
 
+// ---------------------------------------------------------------- many rows
+
+// 256 states by kN tokens a tile, 4 wavefronts of 128 states by kN / 2 tokens, one
+// on each SIMD, a workgroup per compute unit that goes through tiles until none
+// are left, its loads running ahead into the next tile.  128 by 128 of a
+// wavefront, because a smaller share is bound by reading LDS.
+//
+// LDS holds two lines of every state, two of every token's codes, and their
+// scales.  A line of codes is 256 elements: one line of a state in 4 bits, four
+// of one in bfloat16.  A line of states is multiplied in two halves.  While one
+// is, the operands of the next are read; between the two, when the line has been
+// read by all wavefronts, the line after the next is fetched into its place.
+//
+// Of 4-bit states lane quad q takes block 2 q + k of the line's eight in half k, so
+// that its scales of both halves are two bytes in a row, of which the matrix
+// instruction picks one.  Of bfloat16 a half is 32 elements, one block of each
+// token: a lane has 8 of the block's codes, 4 bytes, and converts them beside the
+// matrix instructions, which leave the time.
+//
+// XCDs take workgroups in turn; ids are dealt so that the tiles of one block of
+// tokens (all blocks of states) run on one XCD and share its L2.
+template <int kN, bool kMx, bool kBf16, bool kPlain>
+__device__ __forceinline__ void wide_mx_body(const MxArgs &a) {
+    constexpr int kM = 256, kWavesM = 2, kWavesN = 2, kWaves = 4;
+    constexpr int kSubs = kMx ? 1 : 4;                 // lines of a state per line of codes
+    constexpr int kLoadsW = kN * kChunks / (kWaves * kWave), kLoadsX = kM * kChunks / (kWaves * kWave);
+    static_assert(kLoadsW * kWaves * kWave == kN * kChunks && kN % 64 == 0, "every wavefront loads as much");
+    constexpr int kRowsS = kN + (kMx ? kM : 0), kS1024 = kRowsS / kWave, kLoadsS = kS1024 / kWaves;
+    static_assert(kLoadsS * kWaves * kWave == kRowsS && kN % kWave == 0, "a load has the scales of tokens, or of states");
+    constexpr int kTm = kM / kWavesM / 16, kTn = kN / kWavesN / 16, kPairs = kTn / 2;
+    constexpr int kScales = kRowsS * kPairScales;
+    static_assert(kM == kScaleRows, "a tile of states is one of scales");
+    constexpr int kStores = kBf16 ? kPairs * kTm : kTn * kTm;      // of a whole tile
+    __shared__ __align__(1024) uint8_t lds_w[2 * kN * kStep], lds_x[2 * kM * kStep], lds_s[2 * kScales];
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int wm = wave % kWavesM, wn = wave / kWavesM;
+    if (!kPlain && a.counts) {
+        int32_t count[kShare];
+        if (lane_value(needed_upto(a, lane, count), kWave - 1) <= a.gather_most) {
+            fill_forbidden<kBf16, 4>(a, blockIdx.x, gridDim.x);      // the product was the small kernel's
+            return;
+        }
+    }
+    const int32_t n_tiles = (a.V + kN - 1) / kN, tiles = n_tiles * a.m_tiles, whole = n_tiles / 8 * 8 * a.m_tiles;
+    const auto corner = [&](int32_t id, int32_t &m0, int32_t &n0) {
+        n0 = (id < whole ? id / 8 / a.m_tiles * 8 + id % 8 : id / a.m_tiles) * kN;
+        m0 = (id < whole ? id / 8 % a.m_tiles : id % a.m_tiles) * kM;
+    };
+    // What is loaded next of the codes and of the states.  Past the last tile nothing is read, and the number of loads
+    // stays the same.
+    const uint32_t turn_w = kWaves * 8 * (uint32_t)a.w_stride, turn_x = kWaves * 8 * (uint32_t)a.x_stride;
+    const int32_t x_lines = a.steps * kSubs;
+    int32_t id_w = blockIdx.x, id_x = blockIdx.x, step_w = 0, line_x = 0, to_w = 0, to_x = 0, to_s = 0;
+    u32x4 rw, rs, rx, rt;
+    const auto point_w = [&]() {
+        int32_t m0 = 0, n0 = 0;
+        const bool some = id_w < tiles;
+        if (some) corner(id_w, m0, n0);
+        rw = rows_from(a.w + (int64_t)n0 * a.w_stride, some ? code_bytes(a, n0) : 0);
+        rs = rows_from(a.w_scales + (int64_t)n0 * a.w_scales_stride, some ? scale_bytes(a, n0) : 0);
+        if (kMx) rt = rows_from(a.x_scales + scale_at(a.steps, m0, 0), some ? (int64_t)((a.steps + 1) / 2) * kScaleRows * kPairScales : 0);
+    };
+    const auto point_x = [&]() {
+        int32_t m0 = 0, n0 = 0;
+        const bool some = id_x < tiles;
+        if (some) corner(id_x, m0, n0);
+        rx = rows_from(static_cast<const char *>(a.x) + (int64_t)m0 * a.x_stride, some ? (int64_t)(a.B - m0 - 1) * a.x_stride + (int64_t)x_lines * kStep : 0);
+    };
+    // a sum of scalars that the compiler keeps as one, in place of sums per lane that outlive the loop
+    const auto uniform = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); };
+    const int row8 = wave * 8 + lane / 8;
+    const uint32_t chunk = ((lane & 7) ^ (row8 & 7)) * kChunk;
+    const uint32_t base_w = (uint32_t)row8 * (uint32_t)a.w_stride + chunk, base_x = (uint32_t)row8 * (uint32_t)a.x_stride + chunk;
+    // with every second line of codes the scales of both: 64 rows a load, tokens first, then states
+    const auto fetch_s = [&]() {
+        if (step_w % 2) return;
+        const uint32_t pair = (uint32_t)step_w / 2;
+#pragma unroll
+        for (int i = 0; i < kLoadsS; i++) {
+            const int n = i * kWaves + wave;
+            const uint32_t row = (uint32_t)(n * kWave + lane);
+            const uint32_t to = lds_byte(lds_s) + (uint32_t)(to_s * kScales + n * 1024);
+            if (kMx && n * kWave >= kN) load_to_lds(rt, row * kPairScales + uniform((pair * kScaleRows - kN) * kPairScales), to);
+            else load_to_lds(rs, row * (uint32_t)a.w_scales_stride + uniform(pair * kPairScales), to);
+        }
+        to_s ^= 1;
+    };
+    const auto fetch_w = [&]() {
+#pragma unroll
+        for (int i = 0; i < kLoadsW; i++)
+            load_to_lds(rw, base_w + uniform(i * turn_w + (uint32_t)step_w * kStep), lds_byte(lds_w) + (uint32_t)(to_w * kN + (i * kWaves + wave) * 8) * kStep);
+        to_w ^= 1;
+        if (++step_w == a.steps) {
+            step_w = 0;
+            id_w += (int32_t)gridDim.x;
+            point_w();
+        }
+    };
+    const auto fetch_x = [&]() {
+#pragma unroll
+        for (int i = 0; i < kLoadsX; i++)
+            load_to_lds(rx, base_x + uniform(i * turn_x + (uint32_t)line_x * kStep), lds_byte(lds_x) + (uint32_t)(to_x * kM + (i * kWaves + wave) * 8) * kStep);
+        to_x ^= 1;
+        if (++line_x == x_lines) {
+            line_x = 0;
+            id_x += (int32_t)gridDim.x;
+            point_x();
+        }
+    };
+    // What is read next: half k of line `sub` of the states' of step `step_r`.
+    const int r16 = lane % 16, quad = lane / 16;
+    int32_t step_r = 0, sub_r = 0, at_w = 0, at_x = 0, at_s = 0;
+    u32x4 fx[2][kTm], fw[kMx ? 2 : 1][kMx ? kTn : 1];
+    uint32_t codes[kMx ? 1 : 2][kMx ? 1 : kTn], sw[2][kTn], sx[2][kMx ? kTm : 1];
+    const auto read = [&](auto half, int32_t sub, bool scales) {
+        constexpr int k = decltype(half)::value;
+        const int place = ((kMx ? quad * 2 + k : k * 4 + quad) ^ (r16 & 7)) * kChunk;
+        const uint8_t *const px = lds_x + (at_x * kM + wm * kTm * 16 + r16) * kStep + place;
+        const uint8_t *const pw = lds_w + (at_w * kN + wn * kTn * 16 + r16) * kStep + (kMx ? place : ((sub * 2 + k) ^ (r16 & 7)) * kChunk + quad * 4);
+        if (scales) {
+            const int left = a.w_blocks - step_r * kStepScales;       // blocks up to the row's end
+            const int first = kMx ? quad * 2 : sub * 2;               // of the two blocks whose scales are read
+            const uint8_t *const ps = lds_s + at_s * kScales + (wn * kTn * 16 + r16) * kPairScales + step_r % 2 * kStepScales + first;
+#pragma unroll
+            for (int i = 0; i < kTn; i++) sw[1][i] = *reinterpret_cast<const uint16_t *>(ps + i * 16 * kPairScales);
+            if constexpr (kMx) {
+                const uint8_t *const pt = ps + (kN + (wm * kTm - wn * kTn) * 16) * kPairScales;
+#pragma unroll
+                for (int j = 0; j < kTm; j++) sx[1][j] = *reinterpret_cast<const uint16_t *>(pt + j * 16 * kPairScales);
+            }
+            if (left < kStepScales) {
+                const uint32_t keep = (first < left ? 255u : 0u) | (first + 1 < left ? 255u << 8 : 0u);
+#pragma unroll
+                for (int i = 0; i < kTn; i++) sw[1][i] = (sw[1][i] & keep) | ((kOne | kOne << 8) & ~keep);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kTm; j++) fx[k][j] = *reinterpret_cast<const u32x4 *>(px + j * 16 * kStep);
+#pragma unroll
+        for (int i = 0; i < kTn; i++) {
+            if constexpr (kMx) fw[k][i] = *reinterpret_cast<const u32x4 *>(pw + i * 16 * kStep);
+            else codes[k][i] = *reinterpret_cast<const uint32_t *>(pw + i * 16 * kStep);
+        }
+    };
+    f32x4 acc[kTn][kTm] = {};
+    const auto multiply = [&](auto half) {
+        constexpr int k = decltype(half)::value;
+#pragma unroll
+        for (int i = 0; i < kTn; i++) {
+            bf16x8 w;
+            if constexpr (!kMx) w = widened(codes[k][i], mx_power(k ? sw[0][i] >> 8 : sw[0][i] & 255u));
+#pragma unroll
+            for (int j = 0; j < kTm; j++) {
+                if constexpr (kMx) acc[i][j] = product<k>(fw[k][i], sw[0][i], fx[k][j], sx[0][j], acc[i][j]);
+                else acc[i][j] = product(w, __builtin_bit_cast(bf16x8, fx[k][j]), acc[i][j]);
+            }
+        }
+        // the next operands' reads between the products
+        constexpr int kReads = 2 * kTn + (kMx ? 2 * kTm : kTm), kProducts = kTn * kTm, kEach = kProducts / kReads;
+#pragma unroll
+        for (int n = 0; n < kReads; n++) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
+        }
+    };
+    const auto renew = [&]() {
+#pragma unroll
+        for (int i = 0; i < kTn; i++) sw[0][i] = sw[1][i];
+        if constexpr (kMx)
+#pragma unroll
+            for (int j = 0; j < kTm; j++) sx[0][j] = sx[1][j];
+    };
+    constexpr std::integral_constant<int, 0> kFirst;
+    constexpr std::integral_constant<int, 1> kSecond;
+    point_w();
+    point_x();
+    fetch_s();
+    fetch_w();
+    fetch_x();
+    if (kMx) {
+        fetch_s();
+        fetch_w();
+    }
+    fetch_x();
+    wait_and_meet<0>();
+    read(kFirst, 0, true);
+    renew();
+    bool stored = false;       // stores of a whole tile were the last accesses
+    for (int32_t id = blockIdx.x; id < tiles; id += (int32_t)gridDim.x) {
+#pragma clang loop unroll(disable)
+        for (int32_t line = 0; line < x_lines; line++) {
+            read(kSecond, sub_r, false);
+            multiply(kFirst);
+            __builtin_amdgcn_sched_barrier(0);
+            // The next line has landed: all but what was issued after it, the stores of the tile before, or codes.
+            // And this one has been read by all.
+            if (line == 0 && stored) wait_and_meet<(kStores < 63 ? kStores : 63)>();
+            else if (!kMx && sub_r == 1) wait_and_meet<kLoadsW>();
+            else wait_and_meet<0>();
+            __builtin_amdgcn_sched_barrier(0);
+            if (kMx) {
+                fetch_s();
+                fetch_w();
+                fetch_x();
+            } else {
+                if (sub_r == 0) fetch_s();
+                fetch_x();
+                if (sub_r == 0) fetch_w();
+            }
+            at_x ^= 1;
+            if (kSubs > 1) sub_r = (sub_r + 1) % kSubs;
+            if (sub_r == 0) {
+                at_w ^= 1;
+                if (++step_r == a.steps) step_r = 0;
+                if (step_r % 2 == 0) at_s ^= 1;
+            }
+            read(kFirst, sub_r, true);
+            multiply(kSecond);
+            __builtin_amdgcn_sched_barrier(0);
+            renew();
+        }
+        int32_t m0, n0;
+        corner(id, m0, n0);
+        const int32_t v0 = n0 + wn * kTn * 16;       // the wavefront's first token
+        stored = m0 + kM <= a.B && n0 + kN <= a.V;
+        if (stored) {
+            // Whole tiles.  A lane has four consecutive tokens of every block:
+            // 16 bytes of float32.  Of bfloat16 it gets eight: of two blocks
+            // of 16 tokens, lanes 16 apart swap halves.  Either way a store
+            // writes 64 bytes of every state's row.
+            using T = typename Logit<kBf16>::type;
+            const int32_t mine = kBf16 ? (quad & 1) * 16 + (quad >> 1) * 8 : quad * 4;
+            T *to[kTm];
+            const uint32_t *words[kTm];
+#pragma unroll
+            for (int j = 0; j < kTm; j++) {
+                const int32_t b = m0 + (wm * kTm + j) * 16 + r16;
+                to[j] = static_cast<T *>(a.y) + (int64_t)b * a.y_stride + v0 + mine;
+                if (!kPlain && a.bitmask) words[j] = a.bitmask + (int64_t)b * a.W + (v0 >> 5);
+            }
+#pragma unroll
+            for (int p = 0; p < kPairs; p++) {
+                float bias[2][4] = {};
+                uint32_t word[kTm];
+                if (!kPlain && a.bias)
+#pragma unroll
+                    for (int h = 0; h < 2; h++) __builtin_memcpy(bias[h], a.bias + v0 + (2 * p + h) * 16 + quad * 4, sizeof bias[h]);
+#pragma unroll
+                for (int j = 0; j < kTm; j++) word[j] = !kPlain && a.bitmask ? words[j][p] >> mine : ~0u;
+#pragma unroll
+                for (int j = 0; j < kTm; j++) {
+                    float y[2][4];
+#pragma unroll
+                    for (int h = 0; h < 2; h++)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) y[h][e] = kPlain ? acc[2 * p + h][j][e] : acc[2 * p + h][j][e] + bias[h][e];
+                    if constexpr (kBf16) {
+                        uint32_t o[2][2];
+#pragma unroll
+                        for (int h = 0; h < 2; h++)
+#pragma unroll
+                            for (int e = 0; e < 2; e++)
+                                o[h][e] = (uint32_t)to_bf16(y[h][2 * e]) | (uint32_t)to_bf16(y[h][2 * e + 1]) << 16;
+                        const auto s0 = __builtin_amdgcn_permlane16_swap(o[0][0], o[1][0], false, false);
+                        const auto s1 = __builtin_amdgcn_permlane16_swap(o[0][1], o[1][1], false, false);
+                        u32x4 t = {(uint32_t)s0[0], (uint32_t)s1[0], (uint32_t)s0[1], (uint32_t)s1[1]};
+                        if (!kPlain)
+#pragma unroll
+                            for (int e = 0; e < 4; e++) {
+                                const uint32_t lo = (uint32_t)((int32_t)(word[j] << (31 - 2 * e)) >> 31);
+                                const uint32_t hi = (uint32_t)((int32_t)(word[j] << (30 - 2 * e)) >> 31);
+                                const uint32_t keep = (lo & 0xFFFFu) | (hi & 0xFFFF0000u);
+                                t[e] = (t[e] & keep) | (0xFF80FF80u & ~keep);
+                            }
+                        __builtin_memcpy(to[j] + p * 32, &t, sizeof t);
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < 2; h++) {
+                            if (!kPlain)
+#pragma unroll
+                                for (int e = 0; e < 4; e++) y[h][e] = (word[j] >> (h * 16 + e)) & 1 ? y[h][e] : kMinusInf;
+                            __builtin_memcpy(to[j] + p * 32 + h * 16, y[h], sizeof y[h]);
+                        }
+                    }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kTn; i++) {
+                const int32_t v = v0 + i * 16 + quad * 4, b = m0 + wm * kTm * 16 + r16;
+                Extras<1, kTm, kPlain> extras;
+                extras.load(a, v, m0, b - m0);
+                extras.template put<kBf16>(a, v, b, reinterpret_cast<const f32x4 (&)[1][kTm]>(acc[i]));
+            }
+            // no load of this branch is left for the compiler to wait for after the other, where a wait is one for all stores
+            __builtin_amdgcn_s_waitcnt(0x0F70);     // vmcnt(0)
+        }
+#pragma unroll
+        for (int i = 0; i < kTn; i++)
+#pragma unroll
+            for (int j = 0; j < kTm; j++) acc[i][j] = f32x4{};
+    }
+}
+
+// kPlain: neither a mask nor a bias.
+template <int kN, bool kMx, bool kBf16, bool kPlain>
+__global__ void __launch_bounds__(kWave * 4, 1)
+wide_mx_kernel(const MxArgs a) {
+    wide_mx_body<kN, kMx, kBf16, kPlain>(a);
+}
+
 // ---------------------------------------------------------------- host side
 
 template <int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kMx>
@@ -463,6 +792,24 @@ struct Small {
     }
 };
 
+template <int kN, bool kMx>
+void launch_wide(MxArgs a, bool bf16, hipStream_t s) {
+    a.m_tiles = up(a.B, 256);
+    const dim3 grid((uint32_t)std::min<int64_t>(kComputeUnits, (int64_t)a.m_tiles * up(a.V, kN))), block(kWave * 4);
+    const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
+    if (a.bitmask || a.bias) {
+        if (bf16) go(wide_mx_kernel<kN, kMx, true, false>);
+        else go(wide_mx_kernel<kN, kMx, false, false>);
+    } else {
+        if (bf16) go(wide_mx_kernel<kN, kMx, true, true>);
+        else go(wide_mx_kernel<kN, kMx, false, true>);
+    }
+}
+
+bool takes_wide(const MxArgs &a) {
+    return a.B > 128 && (int64_t)up(a.B, 256) * up(a.V, 256) >= kComputeUnits / 2;
+}
+
 constexpr int32_t kMostD = 131072;
 int32_t steps_of(int32_t D) { return up(D, kStepElems); }
 
@@ -470,15 +817,14 @@ int32_t steps_of(int32_t D) { return up(D, kStepElems); }
 // arrival counters, the partial sums; each from a multiple of 16 bytes on.
 struct Workspace {
     size_t scales, counts, ids, arrivals, partials, total;
-    int64_t x_stride, x_scales_stride;
+    int64_t x_stride;
     int32_t partials_most;
     Workspace(int32_t B, int32_t D, int32_t V, bool mx) {
         const auto whole = [](size_t n) { return (n + 15) / 16 * 16; };
         const int64_t blocks = up(V, kBlockTokens);
         x_stride = (int64_t)steps_of(D) * (mx ? kStep : kWideStep);
-        x_scales_stride = mx ? (int64_t)steps_of(D) * kStepScales : 0;
         scales = (size_t)B * (size_t)x_stride;
-        counts = scales + whole((size_t)B * (size_t)x_scales_stride);
+        counts = scales + (mx ? (size_t)scale_at(steps_of(D), (int64_t)up(B, kScaleRows) * kScaleRows, 0) : 0);
         ids = counts + whole(blocks <= kMostBlocks ? blocks * sizeof(int32_t) : 0);
         arrivals = ids + (blocks <= kMostBlocks ? blocks * kBlockTokens * sizeof(int32_t) : 0);
         partials = arrivals + kMostArrivals * sizeof(uint32_t);
@@ -519,16 +865,28 @@ void launch_prepare(const MxArgs &a, const States &x, int32_t rows, uint8_t *q, 
 
 template <bool kMx>
 psc_status head_mx(const char *what, MxArgs &a, const States &x, bool bf16, uint8_t *q, uint8_t *scales, int32_t *counts, int32_t *ids, bool direct, hipStream_t s) {
+    const auto prepare = [&](bool needed) {
+        if (!needed) return PSC_OK;
+        launch_prepare<kMx>(a, x, direct ? 0 : a.B, q, scales, counts, ids, s);
+        return launched_op(what);      // the product would go by whatever the workspace holds
+    };
     const auto run = [&](auto small) {
         small.shape(a, false);
-        if (!direct || a.counts || a.splits > 1) {
-            launch_prepare<kMx>(a, x, direct ? 0 : a.B, q, scales, counts, ids, s);
-            // the product would go by whatever the workspace holds
-            if (psc_status st = launched_op(what)) return st;
-        }
+        if (psc_status st = prepare(!direct || a.counts || a.splits > 1)) return st;
         small.launch(a, bf16, false, s);
         return launched_op(what);
     };
+    if (takes_wide(a)) {
+        if (psc_status st = prepare(!direct || a.counts)) return st;
+        if (a.counts) {
+            using Gather = std::conditional_t<kMx, Small<64, 128, 1, 4, 3, true>, Small<64, 128, 1, 8, 3, false>>;
+            MxArgs few = a;
+            Gather::shape(few, true);
+            Gather::launch(few, bf16, true, s);
+        }
+        launch_wide<256, kMx>(a, bf16, s);
+        return launched_op(what);
+    }
     if constexpr (kMx) {
         if (a.B <= 32) return run(Small<32, 64, 1, 4, 4, true>{});
         if (a.B <= 64) return run(Small<64, 128, 1, 4, 3, true>{});
@@ -582,7 +940,6 @@ extern "C" psc_status psc_head_logits_mx(const void *x, psc_form x_form, int64_t
     a.x = at;
     a.x_stride = ws.x_stride;
     a.x_scales = at + ws.scales;
-    a.x_scales_stride = ws.x_scales_stride;
     // States in bfloat16 that are whole steps at 16-byte addresses are read where they are.
     const bool direct = !mx && x_form == PSC_FORM_BF16 && D % kStepElems == 0 && aligned_to(x, 16) && x_stride % 8 == 0 && (x_stride >= D || B == 1) &&
                         x_stride <= (1 << 22);
@@ -614,7 +971,7 @@ extern "C" psc_status psc_head_logits_mx(const void *x, psc_form x_form, int64_t
         a.blocks = up(V, kBlockTokens);
         a.counts = counts = reinterpret_cast<int32_t *>(at + ws.counts);
         a.ids = ids = reinterpret_cast<int32_t *>(at + ws.ids);
-        a.gather_most = V / 2;
+        a.gather_most = takes_wide(a) ? V / 4 : V / 2;
     }
     const States given{x, x_form, x_stride, x_scales, x_scales_stride};
     uint8_t *const scales = at + ws.scales;
