@@ -465,16 +465,17 @@ small_mx_kernel(const MxArgs a, bool gather_only) {
 
 // ---------------------------------------------------------------- many rows
 
-// 256 states by kN tokens a tile, 4 wavefronts of 128 states by kN / 2 tokens, one
+// 256 states by kN tokens a tile, 8 wavefronts of 64 states by kN / 2 tokens, two
 // on each SIMD, a workgroup per compute unit that goes through tiles until none
-// are left, its loads running ahead into the next tile.  128 by 128 of a
-// wavefront, because a smaller share is bound by reading LDS.
+// are left, its loads running ahead into the next tile.  Two, because matrix
+// instructions of one alone come 24 cycles apart, of two 16.
 //
 // LDS holds two lines of every state, two of every token's codes, and their
 // scales.  A line of codes is 256 elements: one line of a state in 4 bits, four
 // of one in bfloat16.  A line of states is multiplied in two halves.  While one
-// is, the operands of the next are read; between the two, when the line has been
-// read by all wavefronts, the line after the next is fetched into its place.
+// is, the operands of the next are read, weights into the place of those that
+// have been multiplied; between the two, when the line has been read by all
+// wavefronts, the line after the next is fetched into its place.
 //
 // Of 4-bit states lane quad q takes block 2 q + k of the line's eight in half k, so
 // that its scales of both halves are two bytes in a row, of which the matrix
@@ -486,12 +487,12 @@ small_mx_kernel(const MxArgs a, bool gather_only) {
 // tokens (all blocks of states) run on one XCD and share its L2.
 template <int kN, bool kMx, bool kBf16, bool kPlain>
 __device__ __forceinline__ void wide_mx_body(const MxArgs &a) {
-    constexpr int kM = 256, kWavesM = 2, kWavesN = 2, kWaves = 4;
+    constexpr int kM = 256, kWavesM = 4, kWavesN = 2, kWaves = 8;
     constexpr int kSubs = kMx ? 1 : 4;                 // lines of a state per line of codes
     constexpr int kLoadsW = kN * kChunks / (kWaves * kWave), kLoadsX = kM * kChunks / (kWaves * kWave);
     static_assert(kLoadsW * kWaves * kWave == kN * kChunks && kN % 64 == 0, "every wavefront loads as much");
-    constexpr int kRowsS = kN + (kMx ? kM : 0), kS1024 = kRowsS / kWave, kLoadsS = kS1024 / kWaves;
-    static_assert(kLoadsS * kWaves * kWave == kRowsS && kN % kWave == 0, "a load has the scales of tokens, or of states");
+    constexpr int kRowsS = kN + (kMx ? kM : 0), kS1024 = kRowsS / kWave;
+    static_assert(kS1024 <= kWaves && kN % kWave == 0, "a load has the scales of tokens, or of states");
     constexpr int kTm = kM / kWavesM / 16, kTn = kN / kWavesN / 16, kPairs = kTn / 2;
     constexpr int kScales = kRowsS * kPairScales;
     static_assert(kM == kScaleRows, "a tile of states is one of scales");
@@ -533,24 +534,28 @@ __device__ __forceinline__ void wide_mx_body(const MxArgs &a) {
     };
     // a sum of scalars that the compiler keeps as one, in place of sums per lane that outlive the loop
     const auto uniform = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); };
-    const int row8 = wave * 8 + lane / 8;
-    const uint32_t chunk = ((lane & 7) ^ (row8 & 7)) * kChunk;
-    const uint32_t base_w = (uint32_t)row8 * (uint32_t)a.w_stride + chunk, base_x = (uint32_t)row8 * (uint32_t)a.x_stride + chunk;
+    // The lane, anew: what is worked out of it then is not kept in registers beside the sums, which would not fit.
+    const auto this_lane = [&]() {
+        int32_t l = threadIdx.x % kWave;
+        asm volatile("" : "+v"(l));
+        return l;
+    };
+    // of the lane's row and chunk in a load of eight rows
+    const auto base = [&](int64_t stride) {
+        const int l = this_lane(), row8 = wave * 8 + l / 8;
+        return (uint32_t)row8 * (uint32_t)stride + ((l & 7) ^ (row8 & 7)) * kChunk;
+    };
     // with every second line of codes the scales of both: 64 rows a load, tokens first, then states
     const auto fetch_s = [&]() {
         if (step_w % 2) return;
         const uint32_t pair = (uint32_t)step_w / 2;
-#pragma unroll
-        for (int i = 0; i < kLoadsS; i++) {
-            const int n = i * kWaves + wave;
-            const uint32_t row = (uint32_t)(n * kWave + lane);
-            const uint32_t to = lds_byte(lds_s) + (uint32_t)(to_s * kScales + n * 1024);
-            if (kMx && n * kWave >= kN) load_to_lds(rt, row * kPairScales + uniform((pair * kScaleRows - kN) * kPairScales), to);
-            else load_to_lds(rs, row * (uint32_t)a.w_scales_stride + uniform(pair * kPairScales), to);
-        }
+        const uint32_t row = (uint32_t)(wave * kWave + this_lane()), to = lds_byte(lds_s) + (uint32_t)(to_s * kScales + wave * 1024);
+        if (kMx && wave * kWave >= kN) load_to_lds(rt, row * kPairScales + uniform((pair * kScaleRows - kN) * kPairScales), to);
+        else if (wave < kS1024) load_to_lds(rs, row * (uint32_t)a.w_scales_stride + uniform(pair * kPairScales), to);
         to_s ^= 1;
     };
     const auto fetch_w = [&]() {
+        const uint32_t base_w = base(a.w_stride);
 #pragma unroll
         for (int i = 0; i < kLoadsW; i++)
             load_to_lds(rw, base_w + uniform(i * turn_w + (uint32_t)step_w * kStep), lds_byte(lds_w) + (uint32_t)(to_w * kN + (i * kWaves + wave) * 8) * kStep);
@@ -562,6 +567,7 @@ __device__ __forceinline__ void wide_mx_body(const MxArgs &a) {
         }
     };
     const auto fetch_x = [&]() {
+        const uint32_t base_x = base(a.x_stride);
 #pragma unroll
         for (int i = 0; i < kLoadsX; i++)
             load_to_lds(rx, base_x + uniform(i * turn_x + (uint32_t)line_x * kStep), lds_byte(lds_x) + (uint32_t)(to_x * kM + (i * kWaves + wave) * 8) * kStep);
@@ -573,67 +579,65 @@ __device__ __forceinline__ void wide_mx_body(const MxArgs &a) {
         }
     };
     // What is read next: half k of line `sub` of the states' of step `step_r`.
-    const int r16 = lane % 16, quad = lane / 16;
     int32_t step_r = 0, sub_r = 0, at_w = 0, at_x = 0, at_s = 0;
-    u32x4 fx[2][kTm], fw[kMx ? 2 : 1][kMx ? kTn : 1];
-    uint32_t codes[kMx ? 1 : 2][kMx ? 1 : kTn], sw[2][kTn], sx[2][kMx ? kTm : 1];
-    const auto read = [&](auto half, int32_t sub, bool scales) {
-        constexpr int k = decltype(half)::value;
+    u32x4 fx[2][kTm], fw[kMx ? kTn : 1];
+    uint32_t codes[kMx ? 1 : kTn], sw[kTn], sx[2][kMx ? kTm : 1];
+    const uint8_t *px, *pw, *ps;
+    const auto look = [&](int k) {
+        const int l = this_lane(), r16 = l % 16, quad = l / 16;
         const int place = ((kMx ? quad * 2 + k : k * 4 + quad) ^ (r16 & 7)) * kChunk;
-        const uint8_t *const px = lds_x + (at_x * kM + wm * kTm * 16 + r16) * kStep + place;
-        const uint8_t *const pw = lds_w + (at_w * kN + wn * kTn * 16 + r16) * kStep + (kMx ? place : ((sub * 2 + k) ^ (r16 & 7)) * kChunk + quad * 4);
-        if (scales) {
-            const int left = a.w_blocks - step_r * kStepScales;       // blocks up to the row's end
-            const int first = kMx ? quad * 2 : sub * 2;               // of the two blocks whose scales are read
-            const uint8_t *const ps = lds_s + at_s * kScales + (wn * kTn * 16 + r16) * kPairScales + step_r % 2 * kStepScales + first;
+        px = lds_x + (at_x * kM + wm * kTm * 16 + r16) * kStep + place;
+        pw = lds_w + (at_w * kN + wn * kTn * 16 + r16) * kStep + (kMx ? place : ((sub_r * 2 + k) ^ (r16 & 7)) * kChunk + quad * 4);
+    };
+    const auto read_w = [&](int i) {
+        if constexpr (kMx) fw[i] = *reinterpret_cast<const u32x4 *>(pw + i * 16 * kStep);
+        else codes[i] = *reinterpret_cast<const uint32_t *>(pw + i * 16 * kStep);
+    };
+    const auto read_x = [&](int k, int j) { fx[k][j] = *reinterpret_cast<const u32x4 *>(px + j * 16 * kStep); };
+    // the scales of both halves of a line
+    const auto look_s = [&]() {
+        const int l = this_lane(), r16 = l % 16, quad = l / 16;
+        ps = lds_s + at_s * kScales + (wn * kTn * 16 + r16) * kPairScales + step_r % 2 * kStepScales + (kMx ? quad * 2 : sub_r * 2);
+    };
+    const auto read_s = [&](int i) { sw[i] = *reinterpret_cast<const uint16_t *>(ps + i * 16 * kPairScales); };
+    const auto read_t = [&]() {
+        if constexpr (kMx)
 #pragma unroll
-            for (int i = 0; i < kTn; i++) sw[1][i] = *reinterpret_cast<const uint16_t *>(ps + i * 16 * kPairScales);
-            if constexpr (kMx) {
-                const uint8_t *const pt = ps + (kN + (wm * kTm - wn * kTn) * 16) * kPairScales;
+            for (int j = 0; j < kTm; j++) sx[1][j] = *reinterpret_cast<const uint16_t *>(ps + (kN + (wm * kTm - wn * kTn + j) * 16) * kPairScales);
+    };
+    // and what is done when all of them are read: a scale past the row's end becomes that of 1
+    const auto renew = [&]() {
+        const int left = a.w_blocks - step_r * kStepScales;       // blocks up to the row's end
+        if (left < kStepScales) {
+            const int first = kMx ? this_lane() / 16 * 2 : sub_r * 2;
+            const uint32_t keep = (first < left ? 255u : 0u) | (first + 1 < left ? 255u << 8 : 0u);
 #pragma unroll
-                for (int j = 0; j < kTm; j++) sx[1][j] = *reinterpret_cast<const uint16_t *>(pt + j * 16 * kPairScales);
-            }
-            if (left < kStepScales) {
-                const uint32_t keep = (first < left ? 255u : 0u) | (first + 1 < left ? 255u << 8 : 0u);
-#pragma unroll
-                for (int i = 0; i < kTn; i++) sw[1][i] = (sw[1][i] & keep) | ((kOne | kOne << 8) & ~keep);
-            }
+            for (int i = 0; i < kTn; i++) sw[i] = (sw[i] & keep) | ((kOne | kOne << 8) & ~keep);
         }
+        if constexpr (kMx)
 #pragma unroll
-        for (int j = 0; j < kTm; j++) fx[k][j] = *reinterpret_cast<const u32x4 *>(px + j * 16 * kStep);
-#pragma unroll
-        for (int i = 0; i < kTn; i++) {
-            if constexpr (kMx) fw[k][i] = *reinterpret_cast<const u32x4 *>(pw + i * 16 * kStep);
-            else codes[k][i] = *reinterpret_cast<const uint32_t *>(pw + i * 16 * kStep);
-        }
+            for (int j = 0; j < kTm; j++) sx[0][j] = sx[1][j];
     };
     f32x4 acc[kTn][kTm] = {};
-    const auto multiply = [&](auto half) {
+    // Half k, a block of 16 tokens after the other, and after each of them what `then` does with its number.  The
+    // products are pinned to their place: the compiler would take them along over the branches that follow.
+    const auto multiply = [&](auto half, auto &&then) {
         constexpr int k = decltype(half)::value;
 #pragma unroll
         for (int i = 0; i < kTn; i++) {
             bf16x8 w;
-            if constexpr (!kMx) w = widened(codes[k][i], mx_power(k ? sw[0][i] >> 8 : sw[0][i] & 255u));
+            if constexpr (!kMx) w = widened(codes[i], mx_power(k ? sw[i] >> 8 : sw[i] & 255u));
 #pragma unroll
             for (int j = 0; j < kTm; j++) {
-                if constexpr (kMx) acc[i][j] = product<k>(fw[k][i], sw[0][i], fx[k][j], sx[0][j], acc[i][j]);
+                if constexpr (kMx) acc[i][j] = product<k>(fw[i], sw[i], fx[k][j], sx[0][j], acc[i][j]);
                 else acc[i][j] = product(w, __builtin_bit_cast(bf16x8, fx[k][j]), acc[i][j]);
             }
+#pragma unroll
+            for (int j = 0; j < kTm; j++) asm volatile("" : "+v"(acc[i][j]));
+            __builtin_amdgcn_sched_barrier(0);
+            then(i);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        // the next operands' reads between the products
-        constexpr int kReads = 2 * kTn + (kMx ? 2 * kTm : kTm), kProducts = kTn * kTm, kEach = kProducts / kReads;
-#pragma unroll
-        for (int n = 0; n < kReads; n++) {
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
-        }
-    };
-    const auto renew = [&]() {
-#pragma unroll
-        for (int i = 0; i < kTn; i++) sw[0][i] = sw[1][i];
-        if constexpr (kMx)
-#pragma unroll
-            for (int j = 0; j < kTm; j++) sx[0][j] = sx[1][j];
     };
     constexpr std::integral_constant<int, 0> kFirst;
     constexpr std::integral_constant<int, 1> kSecond;
@@ -648,45 +652,63 @@ __device__ __forceinline__ void wide_mx_body(const MxArgs &a) {
     }
     fetch_x();
     wait_and_meet<0>();
-    read(kFirst, 0, true);
+    look(0);
+#pragma unroll
+    for (int i = 0; i < kTn; i++) read_w(i);
+#pragma unroll
+    for (int j = 0; j < kTm; j++) read_x(0, j);
+    look_s();
+#pragma unroll
+    for (int i = 0; i < kTn; i++) read_s(i);
+    read_t();
     renew();
     bool stored = false;       // stores of a whole tile were the last accesses
     for (int32_t id = blockIdx.x; id < tiles; id += (int32_t)gridDim.x) {
 #pragma clang loop unroll(disable)
         for (int32_t line = 0; line < x_lines; line++) {
-            read(kSecond, sub_r, false);
-            multiply(kFirst);
-            __builtin_amdgcn_sched_barrier(0);
+            multiply(kFirst, [&](int i) {
+                if (i == 0) look(1);
+                if (i == 1) read_w(0);
+                if (i > 0) read_w(i);
+                if (i < kTm) read_x(1, i);
+            });
             // The next line has landed: all but what was issued after it, the stores of the tile before, or codes.
             // And this one has been read by all.
             if (line == 0 && stored) wait_and_meet<(kStores < 63 ? kStores : 63)>();
             else if (!kMx && sub_r == 1) wait_and_meet<kLoadsW>();
             else wait_and_meet<0>();
             __builtin_amdgcn_sched_barrier(0);
-            if (kMx) {
-                fetch_s();
-                fetch_w();
-                fetch_x();
-            } else {
-                if (sub_r == 0) fetch_s();
-                fetch_x();
-                if (sub_r == 0) fetch_w();
-            }
-            at_x ^= 1;
-            if (kSubs > 1) sub_r = (sub_r + 1) % kSubs;
-            if (sub_r == 0) {
-                at_w ^= 1;
-                if (++step_r == a.steps) step_r = 0;
-                if (step_r % 2 == 0) at_s ^= 1;
-            }
-            read(kFirst, sub_r, true);
-            multiply(kSecond);
-            __builtin_amdgcn_sched_barrier(0);
+            multiply(kSecond, [&](int i) {
+                if (i == 0) {
+                    if (kMx || sub_r == 0) fetch_s();
+                    fetch_x();
+                } else if (i == 1) {
+                    if (kMx || sub_r == 0) fetch_w();
+                    at_x ^= 1;
+                    if (kSubs > 1) sub_r = (sub_r + 1) % kSubs;
+                    if (sub_r == 0) {
+                        at_w ^= 1;
+                        if (++step_r == a.steps) step_r = 0;
+                        if (step_r % 2 == 0) at_s ^= 1;
+                    }
+                    look(0);
+                    look_s();
+                    read_t();
+                    read_w(0);
+                    read_s(0);
+                }
+                if (i > 0) {
+                    read_w(i);
+                    read_s(i);
+                    if (i <= kTm) read_x(0, i - 1);
+                }
+            });
             renew();
         }
         int32_t m0, n0;
         corner(id, m0, n0);
         const int32_t v0 = n0 + wn * kTn * 16;       // the wavefront's first token
+        const int l = this_lane(), r16 = l % 16, quad = l / 16;
         stored = m0 + kM <= a.B && n0 + kN <= a.V;
         if (stored) {
             // Whole tiles.  A lane has four consecutive tokens of every block:
@@ -769,7 +791,7 @@ __device__ __forceinline__ void wide_mx_body(const MxArgs &a) {
 
 // kPlain: neither a mask nor a bias.
 template <int kN, bool kMx, bool kBf16, bool kPlain>
-__global__ void __launch_bounds__(kWave * 4, 1)
+__global__ void __launch_bounds__(kWave * 8, 2)
 wide_mx_kernel(const MxArgs a) {
     wide_mx_body<kN, kMx, kBf16, kPlain>(a);
 }
@@ -795,7 +817,7 @@ struct Small {
 template <int kN, bool kMx>
 void launch_wide(MxArgs a, bool bf16, hipStream_t s) {
     a.m_tiles = up(a.B, 256);
-    const dim3 grid((uint32_t)std::min<int64_t>(kComputeUnits, (int64_t)a.m_tiles * up(a.V, kN))), block(kWave * 4);
+    const dim3 grid((uint32_t)std::min<int64_t>(kComputeUnits, (int64_t)a.m_tiles * up(a.V, kN))), block(kWave * 8);
     const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
     if (a.bitmask || a.bias) {
         if (bf16) go(wide_mx_kernel<kN, kMx, true, false>);
