@@ -494,6 +494,7 @@ __device__ __forceinline__ void wide_mx_body(const MxArgs &a) {
     constexpr int kRowsS = kN + (kMx ? kM : 0), kS1024 = kRowsS / kWave;
     static_assert(kS1024 <= kWaves && kN % kWave == 0, "a load has the scales of tokens, or of states");
     constexpr int kTm = kM / kWavesM / 16, kTn = kN / kWavesN / 16, kPairs = kTn / 2;
+    static_assert(kTn == 2 * kTm && kLoadsX == kTm && kLoadsW == kTm, "the reads and loads that go with a block's products");
     constexpr int kScales = kRowsS * kPairScales;
     static_assert(kM == kScaleRows, "a tile of states is one of scales");
     constexpr int kStores = kBf16 ? kPairs * kTm : kTn * kTm;      // of a whole tile
@@ -554,11 +555,14 @@ __device__ __forceinline__ void wide_mx_body(const MxArgs &a) {
         else if (wave < kS1024) load_to_lds(rs, row * (uint32_t)a.w_scales_stride + uniform(pair * kPairScales), to);
         to_s ^= 1;
     };
-    const auto fetch_w = [&]() {
-        const uint32_t base_w = base(a.w_stride);
-#pragma unroll
-        for (int i = 0; i < kLoadsW; i++)
-            load_to_lds(rw, base_w + uniform(i * turn_w + (uint32_t)step_w * kStep), lds_byte(lds_w) + (uint32_t)(to_w * kN + (i * kWaves + wave) * 8) * kStep);
+    // Load i of a line; `base` is the lane's place in the first one.
+    const auto fetch_w = [&](uint32_t base, int i) {
+        load_to_lds(rw, base + uniform(i * turn_w + (uint32_t)step_w * kStep), lds_byte(lds_w) + (uint32_t)(to_w * kN + (i * kWaves + wave) * 8) * kStep);
+    };
+    const auto fetch_x = [&](uint32_t base, int i) {
+        load_to_lds(rx, base + uniform(i * turn_x + (uint32_t)line_x * kStep), lds_byte(lds_x) + (uint32_t)(to_x * kM + (i * kWaves + wave) * 8) * kStep);
+    };
+    const auto fetched_w = [&]() {
         to_w ^= 1;
         if (++step_w == a.steps) {
             step_w = 0;
@@ -566,11 +570,7 @@ __device__ __forceinline__ void wide_mx_body(const MxArgs &a) {
             point_w();
         }
     };
-    const auto fetch_x = [&]() {
-        const uint32_t base_x = base(a.x_stride);
-#pragma unroll
-        for (int i = 0; i < kLoadsX; i++)
-            load_to_lds(rx, base_x + uniform(i * turn_x + (uint32_t)line_x * kStep), lds_byte(lds_x) + (uint32_t)(to_x * kM + (i * kWaves + wave) * 8) * kStep);
+    const auto fetched_x = [&]() {
         to_x ^= 1;
         if (++line_x == x_lines) {
             line_x = 0;
@@ -580,8 +580,8 @@ __device__ __forceinline__ void wide_mx_body(const MxArgs &a) {
     };
     // What is read next: half k of line `sub` of the states' of step `step_r`.
     int32_t step_r = 0, sub_r = 0, at_w = 0, at_x = 0, at_s = 0;
-    u32x4 fx[2][kTm], fw[kMx ? kTn : 1];
-    uint32_t codes[kMx ? 1 : kTn], sw[kTn], sx[2][kMx ? kTm : 1];
+    u32x4 fx[2][kTm], fw[2][kMx ? kTn : 1];
+    uint32_t codes[2][kMx ? 1 : kTn], sw[kTn], sx[2][kMx ? kTm : 1];
     const uint8_t *px, *pw, *ps;
     const auto look = [&](int k) {
         const int l = this_lane(), r16 = l % 16, quad = l / 16;
@@ -589,9 +589,9 @@ __device__ __forceinline__ void wide_mx_body(const MxArgs &a) {
         px = lds_x + (at_x * kM + wm * kTm * 16 + r16) * kStep + place;
         pw = lds_w + (at_w * kN + wn * kTn * 16 + r16) * kStep + (kMx ? place : ((sub_r * 2 + k) ^ (r16 & 7)) * kChunk + quad * 4);
     };
-    const auto read_w = [&](int i) {
-        if constexpr (kMx) fw[i] = *reinterpret_cast<const u32x4 *>(pw + i * 16 * kStep);
-        else codes[i] = *reinterpret_cast<const uint32_t *>(pw + i * 16 * kStep);
+    const auto read_w = [&](int k, int i) {
+        if constexpr (kMx) fw[k][i] = *reinterpret_cast<const u32x4 *>(pw + i * 16 * kStep);
+        else codes[k][i] = *reinterpret_cast<const uint32_t *>(pw + i * 16 * kStep);
     };
     const auto read_x = [&](int k, int j) { fx[k][j] = *reinterpret_cast<const u32x4 *>(px + j * 16 * kStep); };
     // the scales of both halves of a line
@@ -605,37 +605,60 @@ __device__ __forceinline__ void wide_mx_body(const MxArgs &a) {
 #pragma unroll
             for (int j = 0; j < kTm; j++) sx[1][j] = *reinterpret_cast<const uint16_t *>(ps + (kN + (wm * kTm - wn * kTn + j) * 16) * kPairScales);
     };
-    // and what is done when all of them are read: a scale past the row's end becomes that of 1
-    const auto renew = [&]() {
+    // A block past the row's end counts with a power of 2^-127, whatever its scale: it is multiplied by zeros.  For
+    // 4-bit states the bytes that count of the lane's two; for bfloat16 the bits of each half's power.
+    uint32_t inside[2];
+    const auto look_inside = [&]() {
         const int left = a.w_blocks - step_r * kStepScales;       // blocks up to the row's end
-        if (left < kStepScales) {
-            const int first = kMx ? this_lane() / 16 * 2 : sub_r * 2;
-            const uint32_t keep = (first < left ? 255u : 0u) | (first + 1 < left ? 255u << 8 : 0u);
-#pragma unroll
-            for (int i = 0; i < kTn; i++) sw[i] = (sw[i] & keep) | ((kOne | kOne << 8) & ~keep);
+        if constexpr (kMx) {
+            inside[1] = 0xFFFFu;
+            if (left < kStepScales) {
+                const int first = this_lane() / 16 * 2;
+                inside[1] = (first < left ? 0xFFu : 0u) | (first + 1 < left ? 0xFF00u : 0u);
+            }
+        } else {
+            inside[0] = sub_r * 2 < left ? 0x7F800000u : 0u;
+            inside[1] = sub_r * 2 + 1 < left ? 0x7F800000u : 0u;
         }
-        if constexpr (kMx)
+    };
+    const auto renew = [&]() {
+        if constexpr (kMx) {
 #pragma unroll
             for (int j = 0; j < kTm; j++) sx[0][j] = sx[1][j];
+#pragma unroll
+            for (int i = 0; i < kTn; i++) sw[i] &= inside[1];
+        }
     };
     f32x4 acc[kTn][kTm] = {};
-    // Half k, a block of 16 tokens after the other, and after each of them what `then` does with its number.  The
-    // products are pinned to their place: the compiler would take them along over the branches that follow.
-    const auto multiply = [&](auto half, auto &&then) {
+    bf16x8 w[2];
+    const auto convert = [&](int k, int i) {
+        if constexpr (!kMx) {
+            const uint32_t power = (k ? sw[i] << 15 : sw[i] << 23) & inside[k];
+            w[i % 2] = widened(codes[k][i], __builtin_bit_cast(float, power));
+        }
+    };
+    // Half k, a block of 16 tokens after the other, the next one's weights converted meanwhile; with each of them,
+    // what `with` does with its number.  The products are pinned to their place: the compiler would take them along
+    // over the branches that follow.
+    const auto multiply = [&](auto half, auto &&with) {
         constexpr int k = decltype(half)::value;
 #pragma unroll
         for (int i = 0; i < kTn; i++) {
-            bf16x8 w;
-            if constexpr (!kMx) w = widened(codes[i], mx_power(k ? sw[i] >> 8 : sw[i] & 255u));
+            with(i);
 #pragma unroll
             for (int j = 0; j < kTm; j++) {
-                if constexpr (kMx) acc[i][j] = product<k>(fw[i], sw[i], fx[k][j], sx[0][j], acc[i][j]);
-                else acc[i][j] = product(w, __builtin_bit_cast(bf16x8, fx[k][j]), acc[i][j]);
+                if constexpr (kMx) acc[i][j] = product<k>(fw[k][i], sw[i], fx[k][j], sx[0][j], acc[i][j]);
+                else acc[i][j] = product(w[i % 2], __builtin_bit_cast(bf16x8, fx[k][j]), acc[i][j]);
+            }
+            if (i + 1 < kTn) convert(k, i + 1);
+#pragma unroll
+            for (int j = 0; j < kTm; j++) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             }
 #pragma unroll
             for (int j = 0; j < kTm; j++) asm volatile("" : "+v"(acc[i][j]));
-            __builtin_amdgcn_sched_barrier(0);
-            then(i);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -643,47 +666,57 @@ __device__ __forceinline__ void wide_mx_body(const MxArgs &a) {
     constexpr std::integral_constant<int, 1> kSecond;
     point_w();
     point_x();
-    fetch_s();
-    fetch_w();
-    fetch_x();
-    if (kMx) {
-        fetch_s();
-        fetch_w();
+#pragma unroll
+    for (int n = 0; n < 2; n++) {
+        if (kMx || n == 0) {
+            fetch_s();
+#pragma unroll
+            for (int i = 0; i < kLoadsW; i++) fetch_w(base(a.w_stride), i);
+            fetched_w();
+        }
+#pragma unroll
+        for (int i = 0; i < kLoadsX; i++) fetch_x(base(a.x_stride), i);
+        fetched_x();
     }
-    fetch_x();
     wait_and_meet<0>();
     look(0);
+    look_s();
+    look_inside();
 #pragma unroll
-    for (int i = 0; i < kTn; i++) read_w(i);
+    for (int i = 0; i < kTn; i++) {
+        read_w(0, i);
+        read_s(i);
+    }
 #pragma unroll
     for (int j = 0; j < kTm; j++) read_x(0, j);
-    look_s();
-#pragma unroll
-    for (int i = 0; i < kTn; i++) read_s(i);
     read_t();
     renew();
+    convert(0, 0);
     bool stored = false;       // stores of a whole tile were the last accesses
     for (int32_t id = blockIdx.x; id < tiles; id += (int32_t)gridDim.x) {
 #pragma clang loop unroll(disable)
         for (int32_t line = 0; line < x_lines; line++) {
             multiply(kFirst, [&](int i) {
+                // read before the last blocks, so that nothing is waited for at the barrier
                 if (i == 0) look(1);
-                if (i == 1) read_w(0);
-                if (i > 0) read_w(i);
-                if (i < kTm) read_x(1, i);
+                if (i < kTm) {
+                    read_x(1, i);
+                    read_w(1, 2 * i);
+                    read_w(1, 2 * i + 1);
+                }
             });
+            convert(1, 0);
             // The next line has landed: all but what was issued after it, the stores of the tile before, or codes.
             // And this one has been read by all.
             if (line == 0 && stored) wait_and_meet<(kStores < 63 ? kStores : 63)>();
             else if (!kMx && sub_r == 1) wait_and_meet<kLoadsW>();
             else wait_and_meet<0>();
             __builtin_amdgcn_sched_barrier(0);
+            const bool codes_too = kMx || sub_r == 0;
+            const uint32_t base_x = base(a.x_stride), base_w = base(a.w_stride);
             multiply(kSecond, [&](int i) {
                 if (i == 0) {
-                    if (kMx || sub_r == 0) fetch_s();
-                    fetch_x();
-                } else if (i == 1) {
-                    if (kMx || sub_r == 0) fetch_w();
+                    if (codes_too) fetch_s();
                     at_x ^= 1;
                     if (kSubs > 1) sub_r = (sub_r + 1) % kSubs;
                     if (sub_r == 0) {
@@ -693,17 +726,25 @@ __device__ __forceinline__ void wide_mx_body(const MxArgs &a) {
                     }
                     look(0);
                     look_s();
-                    read_t();
-                    read_w(0);
-                    read_s(0);
                 }
+                if (i < kLoadsX) fetch_x(base_x, i);
+                if (i >= kLoadsX && codes_too) fetch_w(base_w, i - kLoadsX);
                 if (i > 0) {
-                    read_w(i);
-                    read_s(i);
-                    if (i <= kTm) read_x(0, i - 1);
+                    read_s(i - 1);
+                    if (i <= kTm) {
+                        read_x(0, i - 1);
+                        read_w(0, 2 * i - 2);
+                        read_w(0, 2 * i - 1);
+                    }
                 }
+                if (i == kTm) read_t();
             });
+            read_s(kTn - 1);
+            fetched_x();
+            if (codes_too) fetched_w();
+            look_inside();
             renew();
+            convert(0, 0);
         }
         int32_t m0, n0;
         corner(id, m0, n0);
