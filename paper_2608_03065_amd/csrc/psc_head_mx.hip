@@ -494,7 +494,7 @@ __device__ __forceinline__ void wide_mx_body(const MxArgs &a) {
     constexpr int kRowsS = kN + (kMx ? kM : 0), kS1024 = kRowsS / kWave;
     static_assert(kS1024 <= kWaves && kN % kWave == 0, "a load has the scales of tokens, or of states");
     constexpr int kTm = kM / kWavesM / 16, kTn = kN / kWavesN / 16, kPairs = kTn / 2;
-    static_assert(kTn == 2 * kTm && kLoadsX == kTm && kLoadsW == kTm, "the reads and loads that go with a block's products");
+    static_assert(kTn % 2 == 0 && kTm < kTn && kLoadsX + kLoadsW <= kTn, "the reads and loads that go with a block's products");
     constexpr int kScales = kRowsS * kPairScales;
     static_assert(kM == kScaleRows, "a tile of states is one of scales");
     constexpr int kStores = kBf16 ? kPairs * kTm : kTn * kTm;      // of a whole tile
@@ -699,8 +699,8 @@ __device__ __forceinline__ void wide_mx_body(const MxArgs &a) {
             multiply(kFirst, [&](int i) {
                 // read before the last blocks, so that nothing is waited for at the barrier
                 if (i == 0) look(1);
-                if (i < kTm) {
-                    read_x(1, i);
+                if (i < kTm) read_x(1, i);
+                if (i < kTn / 2) {
                     read_w(1, 2 * i);
                     read_w(1, 2 * i + 1);
                 }
@@ -728,11 +728,11 @@ __device__ __forceinline__ void wide_mx_body(const MxArgs &a) {
                     look_s();
                 }
                 if (i < kLoadsX) fetch_x(base_x, i);
-                if (i >= kLoadsX && codes_too) fetch_w(base_w, i - kLoadsX);
+                if (i >= kLoadsX && i < kLoadsX + kLoadsW && codes_too) fetch_w(base_w, i - kLoadsX);
                 if (i > 0) {
                     read_s(i - 1);
-                    if (i <= kTm) {
-                        read_x(0, i - 1);
+                    if (i <= kTm) read_x(0, i - 1);
+                    if (i <= kTn / 2) {
                         read_w(0, 2 * i - 2);
                         read_w(0, 2 * i - 1);
                     }
@@ -946,6 +946,14 @@ psc_status head_mx(const char *what, MxArgs &a, const States &x, bool bf16, uint
             MxArgs few = a;
             Gather::shape(few, true);
             Gather::launch(few, bf16, true, s);
+        }
+        if constexpr (!kMx) {
+            const int64_t rounds256 = up((int64_t)up(a.B, 256) * up(a.V, 256), kComputeUnits),
+                          rounds320 = up((int64_t)up(a.B, 256) * up(a.V, 320), kComputeUnits);
+            if (rounds320 * 320 < rounds256 * 256) {
+                launch_wide<320, false>(a, bf16, s);
+                return launched_op(what);
+            }
         }
         launch_wide<256, kMx>(a, bf16, s);
         return launched_op(what);
