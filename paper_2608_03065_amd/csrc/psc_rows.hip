@@ -3,6 +3,7 @@
 // root-mean-square norm with the residual's addition whose result goes to any
 // of the forms (psc_add_rms_norm).
 #include <algorithm>
+#include <type_traits>
 
 #include "psc_mx.hpp"
 
@@ -54,7 +55,7 @@ struct LookupArgs {
 };
 
 // A thread takes eight elements of a row; a row of no table's is zeros.
-template <bool kMx, bool kBf16>
+template <bool kMx, bool kBf16, bool kStream>
 __global__ void __launch_bounds__(kBlock)
 lookup_kernel(const LookupArgs a, Divisor eights, uint32_t units) {
     const uint32_t u = blockIdx.x * kBlock + threadIdx.x;
@@ -79,7 +80,18 @@ lookup_kernel(const LookupArgs a, Divisor eights, uint32_t units) {
             for (int e = 0; e < kVec; e++) v[e] = (float)t[e] * scale;
         }
     }
-    store_eight<kBf16>(static_cast<char *>(a.out) + at * a.out_stride * (kBf16 ? 2 : 4), (int64_t)k * kVec, a.D, v);
+    char *const out = static_cast<char *>(a.out) + at * a.out_stride * (kBf16 ? 2 : 4);
+    if constexpr (kStream) {
+        constexpr int kStores = kBf16 ? 1 : 2;
+        u32x4 t[kStores];
+#pragma unroll
+        for (int e = 0; e < kVec; e++) {
+            if constexpr (kBf16) t[0][e / 2] = e % 2 ? t[0][e / 2] | (uint32_t)to_bf16(v[e]) << 16 : to_bf16(v[e]);
+            else t[e / 4][e % 4] = __builtin_bit_cast(uint32_t, v[e]);
+        }
+#pragma unroll
+        for (int i = 0; i < kStores; i++) __builtin_nontemporal_store(t[i], reinterpret_cast<u32x4 *>(out) + (int64_t)k * kStores + i);
+    } else store_eight<kBf16>(out, (int64_t)k * kVec, a.D, v);
 }
 
 // ---------------------------------------------------------------- the norm
@@ -92,9 +104,8 @@ struct NormArgs {
     int64_t x_stride, residual_stride, out_stride, scales_stride, n_rows;
     int32_t D, padded;            // padded: elements of the result's row that are written
     float eps;
+    bool x_bf16;
 };
-
-constexpr int kTurns = 4;         // vectors of a thread that stay in registers
 
 // Sum or maximum over a row's threads, the same in all of them.
 template <int kThreads, class T, class Op>
@@ -110,57 +121,83 @@ __device__ __forceinline__ T row_all(T v, T none, const Op &op, T *s_part) {
     return v;
 }
 
-// kThreads threads take a row.  A row of up to kTurns vectors a thread is read
-// once and stays in registers; of a longer one the sum is read again from
-// the residual, or x where there is none.
-template <psc_form kTo, bool kXBf16, int kResidual, int kThreads, bool kHeld>
+// kThreads threads take a row, eight elements a thread at a time.  A row of up to
+// kTurns times that is read once and stays in registers, up to twice its gain too; of a
+// longer one (kTurns 0) the sum is read again from the residual, or x where there
+// is none.  kResidual: none, float32, bfloat16.
+template <psc_form kTo, int kResidual, int kThreads, int kTurns>
 __global__ void __launch_bounds__(kThreads > kBlock ? kThreads : kBlock)
 norm_kernel(const NormArgs a) {
     constexpr int kRows = kThreads < kBlock ? kBlock / kThreads : 1;      // rows of a workgroup
     constexpr int kParts = kThreads / kWave;
+    constexpr bool kHeld = kTurns > 0, kGains = kTurns == 1 || kTurns == 2, kRBf16 = kResidual == 2;
     __shared__ float s_sum[kParts], s_again[kParts];
     __shared__ uint32_t s_most[kParts];
     const int t = threadIdx.x % kThreads;
     const int64_t r = (int64_t)blockIdx.x * kRows + threadIdx.x / kThreads;
     if (r >= a.n_rows) return;            // whole wavefronts, and where there are barriers, whole workgroups
-    const char *const x = static_cast<const char *>(a.x) + r * a.x_stride * (kXBf16 ? 2 : 4);
-    constexpr bool kRBf16 = kResidual == 2;
+    const char *const x = static_cast<const char *>(a.x) + r * a.x_stride * (a.x_bf16 ? 2 : 4);
     char *const residual = kResidual ? static_cast<char *>(a.residual) + r * a.residual_stride * (kRBf16 ? 2 : 4) : nullptr;
-
-    // the residual's sum is rounded to its own type before anything is made of it
-    const auto take = [&](int64_t d, float (&v)[kVec], bool first) {
-        if constexpr (kResidual == 0) load_eight<kXBf16>(x, d, a.D, v);
-        else if (!first) load_eight<kRBf16>(residual, d, a.D, v);
-        else {
-            float y[kVec];
-            load_eight<kXBf16>(x, d, a.D, y);
-            load_eight<kRBf16>(residual, d, a.D, v);
-#pragma unroll
-            for (int k = 0; k < kVec; k++) {
-                v[k] += y[k];
-                if constexpr (kRBf16) v[k] = from_bf16(to_bf16(v[k]));
-            }
-            store_eight<kRBf16>(residual, d, a.D, v);
-        }
+    const auto load_x = [&](int64_t d, float (&v)[kVec]) {
+        if (a.x_bf16) load_eight<true>(x, d, a.D, v);
+        else load_eight<false>(x, d, a.D, v);
     };
-    float held[kHeld ? kTurns : 1][kVec], sum = 0;
+    const auto load_gain = [&](int64_t d, float (&g)[kVec]) {
+        if (a.gain) load_eight<false>(a.gain, d, a.D, g);
+        else
+#pragma unroll
+            for (int k = 0; k < kVec; k++) g[k] = 1.0f;
+    };
+    // the residual's sum is rounded to its own type before anything is made of it
+    const auto add = [&](int64_t d, float (&v)[kVec], const float (&y)[kVec]) {
+#pragma unroll
+        for (int k = 0; k < kVec; k++) {
+            v[k] += y[k];
+            if constexpr (kRBf16) v[k] = from_bf16(to_bf16(v[k]));
+        }
+        store_eight<kRBf16>(residual, d, a.D, v);
+    };
+    float held[kHeld ? kTurns : 1][kVec], gains[kGains ? kTurns : 1][kVec];
+    if constexpr (kHeld) {
+        float y[kTurns][kVec];
+#pragma unroll
+        for (int i = 0; i < kTurns; i++) {
+            const int64_t d = ((int64_t)i * kThreads + t) * kVec;
+            load_x(d, kResidual ? y[i] : held[i]);
+            if constexpr (kResidual != 0) load_eight<kRBf16>(residual, d, a.D, held[i]);
+            if constexpr (kGains) load_gain(d, gains[i]);
+        }
+        if constexpr (kResidual != 0)
+#pragma unroll
+            for (int i = 0; i < kTurns; i++) add(((int64_t)i * kThreads + t) * kVec, held[i], y[i]);
+    }
+    // f(first element, the sum there, its gain) for all of the thread's
     const auto each = [&](auto &&f, bool first) {
         if constexpr (kHeld) {
 #pragma unroll
             for (int i = 0; i < kTurns; i++) {
                 const int64_t d = ((int64_t)i * kThreads + t) * kVec;
-                if (first) take(d, held[i], true);
+                if (!kGains && !first) load_gain(d, gains[0]);
+                f(d, held[i], gains[kGains ? i : 0]);
             }
-#pragma unroll
-            for (int i = 0; i < kTurns; i++) f(((int64_t)i * kThreads + t) * kVec, held[i]);
         } else {
             for (int64_t d = (int64_t)t * kVec; d < a.padded; d += kThreads * kVec) {
-                take(d, held[0], first);
-                f(d, held[0]);
+                if constexpr (kResidual == 0) load_x(d, held[0]);
+                else {
+                    load_eight<kRBf16>(residual, d, a.D, held[0]);
+                    if (first) {
+                        float y[kVec];
+                        load_x(d, y);
+                        add(d, held[0], y);
+                    }
+                }
+                if (!first) load_gain(d, gains[0]);
+                f(d, held[0], gains[0]);
             }
         }
     };
-    each([&](int64_t, float (&v)[kVec]) {
+    float sum = 0;
+    each([&](int64_t, const float (&v)[kVec], const float (&)[kVec]) {
 #pragma unroll
         for (int k = 0; k < kVec; k++) sum = __builtin_fmaf(v[k], v[k], sum);
     }, true);
@@ -172,35 +209,33 @@ norm_kernel(const NormArgs a) {
         by = sum < 1 ? 0x1p80f : 0x1p-80f;
         eps = eps * by * by;
         sum = 0;
-        each([&](int64_t, float (&v)[kVec]) {
+        each([&](int64_t, const float (&v)[kVec], const float (&)[kVec]) {
 #pragma unroll
             for (int k = 0; k < kVec; k++) sum = __builtin_fmaf(v[k] * by, v[k] * by, sum);
         }, false);
         sum = row_all<kThreads>(sum, 0.0f, kAdd, s_again);
     }
     const float inverse = 1.0f / __builtin_sqrtf(sum / (float)a.D + eps);
-    const auto scaled = [&](int64_t d, const float (&v)[kVec], float (&y)[kVec]) {
-        float g[kVec];
-        if (a.gain) load_eight<false>(a.gain, d, a.D, g);
+    const auto norm = [&](const float (&v)[kVec], const float (&g)[kVec], float (&y)[kVec]) {
 #pragma unroll
-        for (int k = 0; k < kVec; k++) y[k] = v[k] * by * inverse * (a.gain ? g[k] : 1.0f);
+        for (int k = 0; k < kVec; k++) y[k] = v[k] * by * inverse * g[k];
     };
     if constexpr (kTo == PSC_FORM_F32 || kTo == PSC_FORM_BF16) {
         constexpr bool kBf16 = kTo == PSC_FORM_BF16;
         char *const out = static_cast<char *>(a.out) + r * a.out_stride * (kBf16 ? 2 : 4);
-        each([&](int64_t d, float (&v)[kVec]) {
+        each([&](int64_t d, const float (&v)[kVec], const float (&g)[kVec]) {
             if (d >= a.padded) return;
             float y[kVec];
-            scaled(d, v, y);
+            norm(v, g, y);
             store_eight<kBf16>(out, d, a.D, y);
         }, false);
     } else if constexpr (kTo == PSC_FORM_MX4) {
         uint8_t *const out = static_cast<uint8_t *>(a.out) + r * a.out_stride;
         uint8_t *const scales = static_cast<uint8_t *>(a.scales) + r * a.scales_stride;
-        each([&](int64_t d, float (&v)[kVec]) {
+        each([&](int64_t d, const float (&v)[kVec], const float (&g)[kVec]) {
             if (d >= a.padded) return;            // whole blocks
             float y[kVec];
-            scaled(d, v, y);
+            norm(v, g, y);
             if (d + kVec > a.D)
 #pragma unroll
                 for (int k = 0; k < kVec; k++) y[k] = d + k < a.D ? y[k] : 0.0f;      // 0 times an infinite factor is none
@@ -211,10 +246,10 @@ norm_kernel(const NormArgs a) {
         }, false);
     } else {
         uint32_t most = 0;            // of the absolute values' bits: a NaN's are above an infinity's
-        each([&](int64_t d, float (&v)[kVec]) {
+        each([&](int64_t d, const float (&v)[kVec], const float (&g)[kVec]) {
             if (d >= a.D) return;
             float y[kVec];
-            scaled(d, v, y);
+            norm(v, g, y);
 #pragma unroll
             for (int k = 0; k < kVec; k++)
                 if (d + k < a.D) most = max(most, __builtin_bit_cast(uint32_t, y[k]) & 0x7FFFFFFFu);
@@ -224,14 +259,21 @@ norm_kernel(const NormArgs a) {
         const float scale = finite ? __builtin_bit_cast(float, most) / 127.0f : __builtin_nanf("");
         if (t == 0) static_cast<float *>(a.scales)[r] = scale;
         int8_t *const out = static_cast<int8_t *>(a.out) + r * a.out_stride;
-        each([&](int64_t d, float (&v)[kVec]) {
+        // Quotients by the scale's reciprocal and one correction by the remainder, which is exact, a division's
+        // result in three operations for its ten; a scale whose reciprocal or remainders leave the range divides.
+        const bool divides = !(scale > 0x1p-100f);
+        const float reciprocal = 1.0f / scale;
+        each([&](int64_t d, const float (&v)[kVec], const float (&g)[kVec]) {
             if (d >= a.padded) return;
             float y[kVec];
-            scaled(d, v, y);
+            norm(v, g, y);
             uint64_t codes = 0;
 #pragma unroll
             for (int k = 0; k < kVec; k++) {
-                const float f = scale > 0 && d + k < a.D ? __builtin_rintf(y[k] / scale) : 0.0f;
+                const float near = y[k] * reciprocal;
+                float f = __builtin_fmaf(__builtin_fmaf(-near, scale, y[k]), reciprocal, near);
+                if (divides) f = scale > 0 ? y[k] / scale : 0.0f;
+                f = d + k < a.D ? __builtin_rintf(f) : 0.0f;
                 codes |= (uint64_t)(uint8_t)(int8_t)(int)fminf(fmaxf(f, -127.0f), 127.0f) << (8 * k);
             }
             __builtin_memcpy(out + d, &codes, sizeof codes);
@@ -271,18 +313,16 @@ psc_status check_i8(const char *what, const void *q, int64_t q_stride, const voi
     return PSC_OK;
 }
 
-template <psc_form kTo, bool kXBf16, int kResidual>
+template <psc_form kTo, int kResidual>
 void launch_norm(const NormArgs &all, hipStream_t s) {
-    // Threads of a row: the fewest that hold it.
     NormArgs a = all;
-    const int64_t vectors = (a.padded + kVec - 1) / kVec;
     const auto go = [&](auto kernel, int threads, int rows) {
-        for (int64_t r = 0; r < all.n_rows;) {
-            const int64_t n = std::min<int64_t>(all.n_rows - r, (((int64_t)1 << 32) / threads - 1) * rows);
+        for (int64_t left = all.n_rows; left > 0;) {
+            const int64_t n = std::min<int64_t>(left, (((int64_t)1 << 32) / threads - 1) * rows);
             a.n_rows = n;
             hipLaunchKernelGGL(kernel, dim3((uint32_t)((n + rows - 1) / rows)), dim3(threads), 0, s, a);
-            r += n;
-            a.x = static_cast<const char *>(a.x) + n * a.x_stride * (kXBf16 ? 2 : 4);
+            left -= n;
+            a.x = static_cast<const char *>(a.x) + n * a.x_stride * (a.x_bf16 ? 2 : 4);
             if (kResidual) a.residual = static_cast<char *>(a.residual) + n * a.residual_stride * (kResidual == 2 ? 2 : 4);
             constexpr int kSize = kTo == PSC_FORM_F32 ? 4 : kTo == PSC_FORM_BF16 ? 2 : 1;
             a.out = static_cast<char *>(a.out) + n * a.out_stride * kSize;
@@ -290,23 +330,22 @@ void launch_norm(const NormArgs &all, hipStream_t s) {
             if (kTo == PSC_FORM_MX4) a.scales = static_cast<char *>(a.scales) + n * a.scales_stride;
         }
     };
-    if (vectors <= kWave * 2) go(norm_kernel<kTo, kXBf16, kResidual, 64, true>, kBlock, kBlock / 64);
-    else if (vectors <= 256 * kTurns) go(norm_kernel<kTo, kXBf16, kResidual, 256, true>, 256, 1);
-    else if (vectors <= 1024 * kTurns) go(norm_kernel<kTo, kXBf16, kResidual, 1024, true>, 1024, 1);
-    else go(norm_kernel<kTo, kXBf16, kResidual, 1024, false>, 1024, 1);
+    // Threads of a row: a wavefront where it holds the row in two turns, else the fewest that hold it.
+    const int64_t vectors = (a.padded + kVec - 1) / kVec;
+    if (vectors <= 64 * 2) go(norm_kernel<kTo, kResidual, 64, 2>, kBlock, kBlock / 64);
+    else if (vectors <= 256) go(norm_kernel<kTo, kResidual, 256, 1>, 256, 1);
+    else if (vectors <= 256 * 2) go(norm_kernel<kTo, kResidual, 256, 2>, 256, 1);
+    else if (vectors <= 256 * 4) go(norm_kernel<kTo, kResidual, 256, 4>, 256, 1);
+    else if (vectors <= 1024 * 2) go(norm_kernel<kTo, kResidual, 1024, 2>, 1024, 1);
+    else if (vectors <= 1024 * 4) go(norm_kernel<kTo, kResidual, 1024, 4>, 1024, 1);
+    else go(norm_kernel<kTo, kResidual, 1024, 0>, 1024, 1);
 }
 
 template <psc_form kTo>
-void launch_norm(const NormArgs &a, bool x_bf16, int residual, hipStream_t s) {
-    if (x_bf16) {
-        if (residual == 0) launch_norm<kTo, true, 0>(a, s);
-        else if (residual == 1) launch_norm<kTo, true, 1>(a, s);
-        else launch_norm<kTo, true, 2>(a, s);
-    } else {
-        if (residual == 0) launch_norm<kTo, false, 0>(a, s);
-        else if (residual == 1) launch_norm<kTo, false, 1>(a, s);
-        else launch_norm<kTo, false, 2>(a, s);
-    }
+void launch_norm(const NormArgs &a, int residual, hipStream_t s) {
+    if (residual == 0) launch_norm<kTo, 0>(a, s);
+    else if (residual == 1) launch_norm<kTo, 1>(a, s);
+    else launch_norm<kTo, 2>(a, s);
 }
 
 }  // namespace
@@ -352,16 +391,23 @@ extern "C" psc_status psc_lookup_rows(psc_form form, const void *q, int64_t q_st
     if (n_rows > 0)        // of a table without rows nothing is read
         if (psc_status st = form == PSC_FORM_MX4 ? check_mx(what, q, q_stride, scales, scales_stride, D) : check_i8(what, q, q_stride, scales, D)) return st;
     const int64_t eights = (D + kVec - 1) / kVec;
+    const bool streams = D % kVec == 0 && aligned_to(out, 16) && (n == 1 || out_stride * size_of(dtype) % 16 == 0);
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     by_launches(n, eights, [&](int64_t r, uint32_t units) {
         const LookupArgs a{q, scales, q_stride, scales_stride, n_rows, ids, out, out_stride, r, D};
         const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid_of(units), dim3(kBlock), 0, s, a, Divisor((uint32_t)eights), units); };
+        const auto of = [&](auto mx, auto bf16) {
+            if (streams) go(lookup_kernel<mx, bf16, true>);
+            else go(lookup_kernel<mx, bf16, false>);
+        };
+        constexpr std::true_type yes;
+        constexpr std::false_type no;
         if (form == PSC_FORM_MX4) {
-            if (dtype == PSC_BF16) go(lookup_kernel<true, true>);
-            else go(lookup_kernel<true, false>);
+            if (dtype == PSC_BF16) of(yes, yes);
+            else of(yes, no);
         } else {
-            if (dtype == PSC_BF16) go(lookup_kernel<false, true>);
-            else go(lookup_kernel<false, false>);
+            if (dtype == PSC_BF16) of(no, yes);
+            else of(no, no);
         }
     });
     return launched_op(what);
@@ -383,7 +429,7 @@ extern "C" psc_status psc_add_rms_norm(const void *x, psc_dtype x_dtype, int64_t
     if (residual && ((n_rows > 1 && residual_stride < D) || !aligned_to(residual, size_of(residual_dtype))))
         return refuse(what, "rows of the residual overlap, or it is off its elements' alignment");
     if (!aligned_to(gain, 4)) return refuse(what, "gain off its elements' alignment");
-    NormArgs a{x, residual, gain, out, scales, x_stride, residual_stride, out_stride, scales_stride, n_rows, D, D, eps};
+    NormArgs a{x, residual, gain, out, scales, x_stride, residual_stride, out_stride, scales_stride, n_rows, D, D, eps, x_dtype == PSC_BF16};
     if (to == PSC_FORM_MX4) {
         if (psc_status st = check_mx(what, out, out_stride, scales, scales_stride, D)) return st;
         a.padded = (int32_t)whole(D, kMxBlock);
@@ -395,13 +441,12 @@ extern "C" psc_status psc_add_rms_norm(const void *x, psc_dtype x_dtype, int64_t
         if ((n_rows > 1 && out_stride < D) || !aligned_to(out, size)) return refuse(what, "rows of out overlap, or it is off its elements' alignment");
     }
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    const bool x_bf16 = x_dtype == PSC_BF16;
     const int kind = !residual ? 0 : residual_dtype == PSC_BF16 ? 2 : 1;
     switch (to) {
-        case PSC_FORM_F32: launch_norm<PSC_FORM_F32>(a, x_bf16, kind, s); break;
-        case PSC_FORM_BF16: launch_norm<PSC_FORM_BF16>(a, x_bf16, kind, s); break;
-        case PSC_FORM_I8: launch_norm<PSC_FORM_I8>(a, x_bf16, kind, s); break;
-        default: launch_norm<PSC_FORM_MX4>(a, x_bf16, kind, s); break;
+        case PSC_FORM_F32: launch_norm<PSC_FORM_F32>(a, kind, s); break;
+        case PSC_FORM_BF16: launch_norm<PSC_FORM_BF16>(a, kind, s); break;
+        case PSC_FORM_I8: launch_norm<PSC_FORM_I8>(a, kind, s); break;
+        default: launch_norm<PSC_FORM_MX4>(a, kind, s); break;
     }
     return launched_op(what);
 }

@@ -771,25 +771,46 @@ def _logits_out(out, dtype, default, B: int, V: int, device, stream):
     T = _T or _torch_types()
     if out is not None:
         _require(dtype is None or dtype == out.dtype, "dtype to be that of out")
-        return (out, *_rows(out, "out", device.index, (B, V)))
+        code, stride = _rows(out, "out", device.index, (B, V))
+        return out, code, stride
     code = T["codes"].get(default if dtype is None else dtype)
     if code is None:
         _require(False, f"float32 or bfloat16 logits, not {dtype}")
     return _new((B, V), ("f32", "bf16")[code], device, stream), code, V
 
 
-def _packed(t, name: str, dtype: str, cols: int, align: int, dev: int) -> int:
-    """The row stride of t, a matrix of bytes of `dtype` with `cols` adjacent columns and rows that start at multiples
-    of `align` bytes."""
+def _matrix(t, name: str) -> None:
     T = _T or _torch_types()
-    if not (isinstance(t, T["tensor"]) and t.dtype is T[dtype] and t.dim() == 2 and t.shape[1] == cols and cols > 0):
-        _require(False, f"{name} to be a matrix of {T[dtype]} with {cols} columns")
-    whole = (cols + align - 1) // align * align
-    stride = t.stride(0) if t.shape[0] > 1 else whole
-    _require(t.get_device() == dev and (cols == 1 or t.stride(1) == 1) and stride >= whole and stride % align == 0
-             and t.data_ptr() % align == 0,
-             f"{name} on device {dev}, with adjacent elements and rows that start at multiples of {align} bytes")
-    return stride
+    if not (isinstance(t, T["tensor"]) and t.dim() == 2):
+        _require(False, f"{name} to be a matrix")
+
+
+def _wide(t, cols: int):
+    """The first `cols` columns of t."""
+    return t if t.shape[1] == cols else t.narrow(1, 0, cols)
+
+
+def _packed(t, name: str, dtype: str, cols: int, align: int, dev: int | None = None, rows: int | None = None):
+    """(row stride, rows, device index) of t, a matrix of bytes of `dtype` on the current device with `cols` adjacent
+    columns and rows that start at multiples of `align` bytes."""
+    T = _T or _torch_types()
+    if type(t) is T["tensor"] and t.dtype is T[dtype] and t.dim() == 2:      # no message is put together on the common path
+        (n, wide), (apart, step), at = t.shape, t.stride(), t.get_device()
+        if n <= 1:
+            apart = (cols + align - 1) // align * align
+        if (wide == cols > 0 and step == 1 and apart % align == 0 and apart >= cols and t.data_ptr() % align == 0
+                and at >= 0 and at == (T["device"]() if dev is None else dev) and (rows is None or n == rows)):
+            return apart, n, at
+    _require(isinstance(t, T["tensor"]) and t.dtype is T[dtype] and t.dim() == 2 and t.shape[1] == cols and cols > 0,
+             f"{name} to be a matrix of {T[dtype]} with {cols} columns")
+    n = t.shape[0]
+    _require(rows is None or n == rows, f"{name} of {rows} rows, not {n}")
+    apart = t.stride(0) if n > 1 else (cols + align - 1) // align * align
+    at = t.get_device()
+    _require(at >= 0 and at == (T["device"]() if dev is None else dev), f"{name} on the current device")
+    _require((cols == 1 or t.stride(1) == 1) and apart >= cols and apart % align == 0 and t.data_ptr() % align == 0,
+             f"{name} with adjacent elements and rows that start at multiples of {align} bytes")
+    return apart, n, at
 
 
 def head_logits(x, w, w_scales, dtype=None, bias=None, bitmask=None, out=None, stream=None, x_scales=None):
@@ -804,9 +825,8 @@ def head_logits(x, w, w_scales, dtype=None, bias=None, bitmask=None, out=None, s
         x_code, x_stride = _rows(x, "x")
         default = x.dtype
     else:
-        _require(isinstance(x, T["tensor"]) and x.dim() == 2 and x.get_device() >= 0 and x.get_device() == T["device"](),
-                 "x to be a matrix on the current device")
-        x_stride, default = _packed(x, "x", "i8", x.shape[1], 16, x.get_device()), T["bf16"]
+        _matrix(x, "x")
+        x_stride, default = _packed(x, "x", "i8", x.shape[1], 16)[0], T["bf16"]
     B, D = x.shape
     dev = x.get_device()
     if not (isinstance(w, T["tensor"]) and w.dtype is T["i8"] and w.dim() == 2 and w.shape[1] == D and D > 0):
@@ -847,7 +867,7 @@ def quantize_mx(x, stream=None):
     q, scales = _new((n, q_stride), "u8", x.device, stream), _new((n, s_stride), "u8", x.device, stream)
     _check(lib().psc_quantize_mx(x.data_ptr(), code, stride, n, D, q.data_ptr(), q_stride, scales.data_ptr(), s_stride,
                                  _stream_ptr(stream)))
-    return q[:, :(D + 1) // 2], scales[:, :blocks]
+    return _wide(q, (D + 1) // 2), _wide(scales, blocks)
 
 
 def lookup_rows(q, scales, ids=None, D=None, dtype=None, out=None, stream=None):
@@ -857,15 +877,18 @@ def lookup_rows(q, scales, ids=None, D=None, dtype=None, out=None, stream=None):
     A row whose id is outside the table is zeros.  `out`: where to write them;
     else a new tensor of `dtype`, bfloat16 by default."""
     T = _T or _torch_types()
-    _require(isinstance(q, T["tensor"]) and q.dim() == 2 and q.dtype in (T["i8"], T["u8"]) and q.get_device() >= 0
-             and q.get_device() == T["device"](), "q to be an int8 or uint8 matrix on the current device")
-    (rows, cols), dev, mx = q.shape, q.get_device(), q.dtype is T["u8"]
+    _matrix(q, "q")
+    mx, cols = q.dtype is T["u8"], q.shape[1]
     if D is None:
         D = cols * 2 if mx else cols
-    _require(cols == ((D + 1) // 2 if mx else D), f"q of rows of {D} elements")
+    if D == 0:
+        q_stride, rows, dev = 0, q.shape[0], q.get_device()
+    else:
+        q_stride, rows, dev = _packed(q, "q", "u8" if mx else "i8", (D + 1) // 2 if mx else D, 16)
     n = rows
     if ids is not None:
-        _require(isinstance(ids, T["tensor"]) and ids.dim() == 1, "ids to be a vector")
+        if not (isinstance(ids, T["tensor"]) and ids.dim() == 1):
+            _require(False, "ids to be a vector")
         n = ids.shape[0]
     if out is None:
         code, out_stride = T["codes"].get(T["bf16"] if dtype is None else dtype), D
@@ -877,11 +900,9 @@ def lookup_rows(q, scales, ids=None, D=None, dtype=None, out=None, stream=None):
         code, out_stride = _rows(out, "out", dev, (n, D))
     if D == 0 or n == 0:
         return out
-    at_ids = _vector(ids, "ids", "i32", dev, (n,))
-    q_stride, s_stride = _packed(q, "q", "u8" if mx else "i8", cols, 16, dev), 0
+    at_ids, s_stride = _vector(ids, "ids", "i32", dev, (n,)), 0
     if mx:
-        s_stride = _packed(scales, "scales", "u8", (D + MX_BLOCK - 1) // MX_BLOCK, 4, dev)
-        _require(scales.shape[0] == rows, f"scales of {rows} rows")
+        s_stride = _packed(scales, "scales", "u8", (D + MX_BLOCK - 1) // MX_BLOCK, 4, dev, rows)[0]
         at = scales.data_ptr()
     else:
         at = _vector(scales, "scales", "f32", dev, (rows,))
@@ -911,12 +932,12 @@ def add_rms_norm(x, gain=None, residual=None, eps=1e-6, to=None, stream=None):
     if to == "i8":
         form, o_stride = FORM_I8, (D + 15) // 16 * 16
         out, scales = _new((n, o_stride), "i8", x.device, stream), _new(n, "f32", x.device, stream)
-        got = out[:, :D], scales
+        got = _wide(out, D), scales
     elif to == "mx4":
         blocks = (D + MX_BLOCK - 1) // MX_BLOCK
         form, o_stride, s_stride = FORM_MX4, blocks * 16, (blocks + 15) // 16 * 16
         out, scales = _new((n, o_stride), "u8", x.device, stream), _new((n, s_stride), "u8", x.device, stream)
-        got = out[:, :(D + 1) // 2], scales[:, :blocks]
+        got = _wide(out, (D + 1) // 2), _wide(scales, blocks)
     else:
         form, o_stride = T["codes"].get(x.dtype if to is None else to), D
         if form is None:
@@ -939,28 +960,26 @@ def head_logits_mx(x, w, w_scales, states="bf16", x_scales=None, dtype=None, bia
     as they are.  `out`: where to write the logits; else a new tensor of
     `dtype`, by default that of x, of states in 4 bits bfloat16."""
     T = _T or _torch_types()
-    _require(states in _STATES, 'states: "bf16" or "mx4"')
+    form = _STATES.get(states)
+    if form is None:
+        _require(False, 'states: "bf16" or "mx4"')
     x_at, x_s_stride = None, 0
     if x_scales is None:
         x_code, x_stride = _rows(x, "x")
         (B, D), dev, default = x.shape, x.get_device(), x.dtype
         cols, blocks = (D + 1) // 2, (D + MX_BLOCK - 1) // MX_BLOCK
     else:
-        _require(isinstance(x, T["tensor"]) and x.dim() == 2 and x.get_device() >= 0 and x.get_device() == T["device"](),
-                 "x to be a matrix on the current device")
-        (B, cols), dev, default, states, x_code = x.shape, x.get_device(), T["bf16"], "mx4", FORM_MX4
+        _matrix(x, "x")
+        cols, default, form, x_code = x.shape[1], T["bf16"], FORM_MX4, FORM_MX4
         D = cols * 2          # an odd row's last code is zero
         blocks = (D + MX_BLOCK - 1) // MX_BLOCK
-        x_stride = _packed(x, "x", "u8", cols, 16, dev)
-        x_s_stride = _packed(x_scales, "x_scales", "u8", blocks, 1, dev)
-        _require(x_scales.shape[0] == B, f"x_scales of {B} rows")
+        x_stride, B, dev = _packed(x, "x", "u8", cols, 16)
+        x_s_stride = _packed(x_scales, "x_scales", "u8", blocks, 1, dev, B)[0]
         x_at = x_scales.data_ptr()
-    w_stride = _packed(w, "w", "u8", cols, 16, dev)
-    s_stride = _packed(w_scales, "w_scales", "u8", blocks, 4, dev)
-    V = w.shape[0]
-    _require(w_scales.shape[0] == V, f"w_scales of {V} rows")
+    w_stride, V, _ = _packed(w, "w", "u8", cols, 16, dev)
+    s_stride = _packed(w_scales, "w_scales", "u8", blocks, 4, dev, V)[0]
     out, code, y_stride = _logits_out(out, dtype, default, B, V, x.device, stream)
-    L, form = lib(), _STATES[states]
+    L = lib()
     bias = _vector(bias, "bias", "f32", dev, (V,))
     words = _vector(bitmask, "bitmask", "i32", dev, (B, (V + 31) // 32))
     n = L.psc_head_mx_workspace(B, D, V, form)
