@@ -942,7 +942,7 @@ psc_status head_mx(const char *what, MxArgs &a, const States &x, bool bf16, uint
     if (takes_wide(a)) {
         if (psc_status st = prepare(!direct || a.counts)) return st;
         if (a.counts) {
-            using Gather = std::conditional_t<kMx, Small<64, 128, 1, 4, 3, true>, Small<64, 128, 1, 8, 3, false>>;
+            using Gather = std::conditional_t<kMx, Small<64, 128, 2, 4, 3, true>, Small<64, 128, 1, 8, 3, false>>;
             MxArgs few = a;
             Gather::shape(few, true);
             Gather::launch(few, bf16, true, s);
@@ -960,11 +960,11 @@ psc_status head_mx(const char *what, MxArgs &a, const States &x, bool bf16, uint
     }
     if constexpr (kMx) {
         if (a.B <= 32) return run(Small<32, 64, 1, 4, 4, true>{});
-        if (a.B <= 64) return run(Small<64, 128, 1, 4, 3, true>{});
+        if (a.B <= 64) return run(Small<64, 128, 2, 4, 3, true>{});
         return run(Small<128, 128, 2, 4, 3, true>{});
     } else {
-        if (a.B <= 16) return run(Small<16, 64, 1, 4, 4, false>{});
-        if (a.B <= 32) return run(Small<32, 64, 1, 4, 3, false>{});
+        if (a.B <= 16) return run(Small<16, 64, 1, 4, 3, false>{});
+        if (a.B <= 32) return run(Small<32, 128, 1, 8, 3, false>{});
         return run(Small<64, 128, 1, 8, 3, false>{});
     }
 }
