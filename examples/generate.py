@@ -14,7 +14,14 @@ Each step of B streams, on one HIP stream and without a copy to the host:
 The model is a stand-in with random weights, hidden = decay * hidden +
 embedding[token], since the text's form comes from the grammar.
 
-  python examples/generate.py --workload json --batch 4 --tokens 48
+With --weights mx4 the output projection and the embedding share one table in
+4 bits, and a norm stands before the projection, whose states are in 4 bits too:
+
+  psc.lookup_rows              the last token's embedding out of the table
+  psc.add_rms_norm             its addition to the hidden state, the norm, and the result in 4 bits
+  psc.head_logits_mx           these states -> logits by the table's weights
+
+  python examples/generate.py --workload json --batch 4 --tokens 48 [--weights mx4]
 """
 import argparse
 import os
@@ -32,14 +39,20 @@ class Generator:
     """B streams of at most `cap` tokens under clf's grammar, from a seed."""
 
     def __init__(self, clf, eos_id, B, cap, D=1024, k=50, temperature=1.0, top_p=0.95, min_p=0.02, repetition=1.1,
-                 presence=0.2, frequency=0.1, eos_bias=2.0, seed=0):
+                 presence=0.2, frequency=0.1, eos_bias=2.0, seed=0, weights="i8"):
         dev = clf.device
         self.g = torch.Generator(dev).manual_seed(seed)
         self.clf, self.k = clf, k
         self.states = psc.DecodeStates(clf, B, 4096, dev)
+        self.tied = weights == "mx4"
         self.embedding = torch.randn(clf.V, D, generator=self.g, device=dev)
-        # once: the output projection's weights in 8 bits, a scale per token
-        self.weights, self.scales = psc.quantize_rows(torch.randn(clf.V, D, generator=self.g, device=dev) / D ** 0.5)
+        if self.tied:
+            # once: the table in 4 bits, a power of two per 32 elements
+            self.weights, self.scales = psc.quantize_mx(self.embedding / D ** 0.5)
+            self.gain, self.last = torch.ones(D, device=dev), torch.zeros(B, D, dtype=torch.bfloat16, device=dev)
+        else:
+            # once: the output projection's weights in 8 bits, a scale per token
+            self.weights, self.scales = psc.quantize_rows(torch.randn(clf.V, D, generator=self.g, device=dev) / D ** 0.5)
         self.hidden = torch.randn(B, D, generator=self.g, device=dev)
         self.history = torch.zeros(B, cap, dtype=torch.int32, device=dev)
         self.lens = torch.zeros(B, dtype=torch.int32, device=dev)
@@ -54,13 +67,20 @@ class Generator:
     def step(self):
         """One token per stream; returns (tokens, log-probabilities, masks), token -1 for a stream that is done."""
         masks = self.states.compute_masks().masked_fill_(self.done[:, None], 0)
-        logits = psc.head_logits(self.hidden.to(torch.bfloat16), self.weights, self.scales, bitmask=masks)
+        if self.tied:
+            state, powers = psc.add_rms_norm(self.last, self.gain, residual=self.hidden.mul_(0.8), to="mx4")
+            logits = psc.head_logits_mx(state, self.weights, self.scales, x_scales=powers, bitmask=masks)
+        else:
+            logits = psc.head_logits(self.hidden.to(torch.bfloat16), self.weights, self.scales, bitmask=masks)
         psc.penalize(logits, self.history, self.lens, bitmask=masks, **self.penalties)
         self.noise.exponential_(generator=self.g)
         tokens, logprobs, _, _ = psc.sample(logits, self.k, bitmask=masks, noise=self.noise, **self.draw)
         psc.append_tokens(self.history, self.lens, tokens)
         self.done |= self.states.advance(tokens) != psc.ADV_OK
-        self.hidden.mul_(0.8).add_(self.embedding[tokens.clamp(min=0)])
+        if self.tied:
+            self.last = psc.lookup_rows(self.weights, self.scales, tokens)
+        else:
+            self.hidden.mul_(0.8).add_(self.embedding[tokens.clamp(min=0)])
         return tokens, logprobs, masks
 
 
@@ -71,10 +91,12 @@ def main():
     ap.add_argument("--tokens", type=int, default=48)
     ap.add_argument("--hidden", type=int, default=1024)
     ap.add_argument("--seed", type=int, default=0)
+    ap.add_argument("--weights", default="i8", choices=("i8", "mx4"))
     args = ap.parse_args()
     wl = configs.get(args.workload)
     clf = psc.Classifier(wl.grammar, wl.vocab).bind("cuda:0")
-    gen = Generator(clf, wl.vocab.eos_id, args.batch, args.tokens, D=args.hidden, seed=args.seed)
+    gen = Generator(clf, wl.vocab.eos_id, args.batch, args.tokens, D=args.hidden, seed=args.seed,
+                    weights=args.weights)
     start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     score = torch.zeros(args.batch, device="cuda:0")
     for n in range(args.tokens):

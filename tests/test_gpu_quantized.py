@@ -371,7 +371,8 @@ def test_head_logits_mx_that_are_not_numbers(B, states):
         if states == "mx4":
             y[2] = np.nan
         else:
-            y[2] = np.where(w[:, 0] == 0, np.nan, np.inf * np.sign(w[:, 0]))
+            with np.errstate(invalid="ignore"):
+                y[2] = np.where(w[:, 0] == 0, np.nan, np.inf * np.sign(w[:, 0]))
             y[2, [7, 599]] = np.nan
     xv[~np.isfinite(xv)] = 0
     close(psc.head_logits_mx(x.to(DEV), q, s, states=states, dtype=torch.float32), y, head_bound(xv, w, 0, states))
