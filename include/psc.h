@@ -598,7 +598,7 @@ typedef enum {
  * psc_quantize_rows and psc_add_rms_norm write them, q_stride bytes apart) with
  * their scales.  Values of -128 count as they are; what lies between D and
  * q_stride does not matter.  The same workspace, refusals and errors. */
-psc_status psc_head_logits_i8(const int8_t *q, int64_t q_stride, const float *scales, int32_t B, int32_t D,
+psc_status psc_head_logits_quantized(const int8_t *q, int64_t q_stride, const float *scales, int32_t B, int32_t D,
                               const int8_t *w, int64_t w_stride, const float *w_scales, int32_t V,
                               const float *bias, const uint32_t *bitmask, void *logits, psc_dtype dtype,
                               int64_t stride, void *workspace, size_t workspace_bytes, void *stream);
@@ -631,7 +631,7 @@ psc_status psc_quantize_mx(const void *x, psc_dtype dtype, int64_t x_stride, int
  *  form    PSC_FORM_I8: q as psc_quantize_rows writes it, scales float32 [n_rows]
  *          (scales_stride is not used); the product with the scale is float32,
  *          rounded once to `dtype`.  PSC_FORM_MX4: as psc_quantize_mx writes it;
- *          every value is exact in bfloat16 and float32.
+ *          every value is exact in bfloat16 and float32, past their range infinite.
  *  out     [n] rows, out_stride elements apart (>= D).
  * n, n_rows < 2^31, D <= 2^30; n == 0 or D == 0 is a no-op.  Errors:
  * PSC_E_INVALID_ARG, PSC_E_DEVICE.
@@ -646,14 +646,14 @@ psc_status psc_lookup_rows(psc_form form, const void *q, int64_t q_stride, const
  *   y = h / sqrt(mean_d h[d]^2 + eps) * gain[d]
  * in float32, squares past its range included.  Without a residual (NULL) h is x.
  *  x         [n_rows] rows of D, x_stride elements apart.
- *  residual  rows residual_stride elements apart (>= D), changed in place; not x.
+ *  residual  rows residual_stride elements apart (>= D), changed in place.
  *  gain      float32 [D], or NULL for 1.
  *  to, out   PSC_FORM_F32, PSC_FORM_BF16: y rounded to it, rows out_stride elements
  *            apart (>= D).  PSC_FORM_I8: y quantised as by psc_quantize_rows, `scales`
  *            float32 [n_rows].  PSC_FORM_MX4: as by psc_quantize_mx, `scales` bytes
  *            scales_stride apart.  For these two out_stride is in bytes, a multiple
  *            of 16, at a 16-byte address; y is not rounded before it is quantised.
- * eps >= 0.  A row with a NaN becomes NaN; one with an infinity has NaN there and
+ * What is written overlaps nothing else.  eps >= 0.  A row with a NaN becomes NaN; one with an infinity has NaN there and
  * zeros elsewhere (8 bits: scale NaN).  n_rows < 2^31, D <= 2^30; n_rows == 0 or D == 0
  * is a no-op.  Errors: PSC_E_INVALID_ARG, PSC_E_DEVICE.
  */
@@ -668,8 +668,9 @@ psc_status psc_add_rms_norm(const void *x, psc_dtype x_dtype, int64_t x_stride, 
  * where w' are the weights' values and x' the states, in bfloat16 (`states`
  * PSC_FORM_BF16: float32 states are rounded to it) or in 4 bits as by
  * psc_quantize_mx (PSC_FORM_MX4); -inf where `bitmask` forbids v.  Products are exact,
- * sums and the bias float32, the result is rounded once to `dtype`.  A
- * weight's row with a scale of 255 gives NaN.
+ * sums and the bias float32, the result is rounded once to `dtype`; the same
+ * call gives the same bits.  A weight's row with a scale of 255 gives NaN; numbers
+ * below 2^-126 may count as 0.
  *  x          [B] rows of D: x_form PSC_FORM_F32 or PSC_FORM_BF16, x_stride elements
  *             apart (x_scales is not used); or PSC_FORM_MX4, for `states` of that form,
  *             codes x_stride bytes apart (a multiple of 16, at a 16-byte address,

@@ -900,11 +900,11 @@ extern "C" psc_status psc_head_logits(const void *x, psc_dtype x_dtype, int64_t 
                        workspace_bytes, stream);
 }
 
-extern "C" psc_status psc_head_logits_i8(const int8_t *q, int64_t q_stride, const float *scales, int32_t B, int32_t D,
+extern "C" psc_status psc_head_logits_quantized(const int8_t *q, int64_t q_stride, const float *scales, int32_t B, int32_t D,
                                          const int8_t *w, int64_t w_stride, const float *w_scales, int32_t V,
                                          const float *bias, const uint32_t *bitmask, void *logits, psc_dtype dtype,
                                          int64_t stride, void *workspace, size_t workspace_bytes, void *stream) {
-    const char *what = "psc_head_logits_i8";
+    const char *what = "psc_head_logits_quantized";
     if (psc_status st = check_rows(what, logits, dtype, stride, B, V)) return st;
     if (!scales && B > 0 && V > 0) return refuse(what, "null pointer");
     return head_logits(what, {q, PSC_F32, q_stride, scales}, B, D, w, w_stride, w_scales, V, bias, bitmask, logits, dtype, stride, workspace,

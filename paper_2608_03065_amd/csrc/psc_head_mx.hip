@@ -5,7 +5,30 @@
 // 32 of them: a block, 16 bytes of codes, with the block's power of two.  For
 // bfloat16 states the same 16 bytes are converted to bfloat16 times their power,
 // which holds them exactly, and go through four matrix instructions of 32
-// elements each, of which a lane has 8.  Sums are float32.
+// elements each, of which a lane has 8.  Sums are float32: of 4-bit states what an
+// instruction adds up is exact, of bfloat16 products exact and the sum rounded.
+// (The same instruction takes states in 8-bit floating point, whose sums it cuts
+// off near 2^-13 of the largest product: no form of states here.)
+//
+// A call launches prepare_mx_kernel (the states to what is multiplied, and under a
+// mask the list of tokens that any row allows) unless the states can be read
+// where they are, there is no mask, and D is not split; then the product:
+// small_mx_kernel for up to 128 rows and where the large tiles would be few
+// (takes_wide), wide_mx_kernel for the others.  Where the mask leaves few tokens,
+// the product is taken of the listed tokens' weights only (small_mx_kernel,
+// `gather`; beside wide_mx_kernel in a launch of its own).  Where there are too few
+// tiles for the GPU, D is split over workgroups, and the last one of a tile to end
+// adds their sums in the order of the parts: the same call gives the same bits.
+//
+// Few rows are bound by the weights' bytes, each read once: 1 x 128,256 x 4,096
+// takes 50 us, 5.6 TB/s, where a large copy reaches 4.7; 64 x 128,256 x 4,096 66 us of
+// states in 4 bits, 4.5 TB/s, but 118 of bfloat16, whose lines are three times the
+// weights' bytes on their way from L2 to LDS.  Many rows: 2,048 x 128,256 x 4,096
+// takes 587 us in 4 bits, 3.7 P operations a second (the library's product of that
+// size without scales' variety, a mask or a bias 820), 256 x 151,936 x 4,096 of
+// bfloat16 271.  Their matrix instructions alone would take 228 and 160; the rest is
+// about equally the waits for what is read from LDS, for the lines from L2, and
+// the stores of the logits, which all compute units write at once.
 #include <type_traits>
 
 #include "psc_head.hpp"
@@ -869,6 +892,10 @@ void launch_wide(MxArgs a, bool bf16, hipStream_t s) {
     }
 }
 
+// wide_mx_kernel's calls: above 128 rows, unless its tiles would leave most compute units idle.  us by wide_mx_kernel and by
+// small_mx_kernel, times 128,256 x 4,096: states in 4 bits 96 rows 83 and 86, 128 89 and 88, 160 91 and 151; bfloat16 96
+// rows 213 and 212, 128 225 and 223, 160 229 and 317.  256 x 40,000 x 4,096 (157 tiles) 44 and 62, 111 and 138;
+// 256 x 24,000 (94 tiles) 39 and 41, 106 and 83.
 bool takes_wide(const MxArgs &a) {
     return a.B > 128 && (int64_t)up(a.B, 256) * up(a.V, 256) >= kComputeUnits / 2;
 }
@@ -939,6 +966,8 @@ psc_status head_mx(const char *what, MxArgs &a, const States &x, bool bf16, uint
         small.launch(a, bf16, false, s);
         return launched_op(what);
     };
+    // Of bfloat16 states the width whose rounds of tiles over the compute units end first: 256 x 151,936 x 4,096 takes 314 us
+    // in 3 rounds of 256, 278 in 2 of 320.  Sums and operands in 4 bits of 320 would not fit the registers.
     if (takes_wide(a)) {
         if (psc_status st = prepare(!direct || a.counts)) return st;
         if (a.counts) {
@@ -958,6 +987,10 @@ psc_status head_mx(const char *what, MxArgs &a, const States &x, bool bf16, uint
         launch_wide<256, kMx>(a, bf16, s);
         return launched_op(what);
     }
+    // The tiles grow with the rows.  us of states in 4 bits by tiles of 64 x 64 and 64 x 128, the latter by wavefronts of 64
+    // and of 32 states: 64 x 128,256 x 4,096 72, 66, 66; 64 x 151,665 x 2,048 under masks 61, 54, 51.  Of bfloat16: 1 x 128,256 x
+    // 4,096 by 16 x 64, three steps in LDS, three workgroups a compute unit 50, four steps 55; 32 rows by 32 x 64 82, by
+    // 32 x 128 of eight wavefronts 74; 64 rows by 64 x 64 of four 163, by 64 x 128 of eight 118.
     if constexpr (kMx) {
         if (a.B <= 32) return run(Small<32, 64, 1, 4, 4, true>{});
         if (a.B <= 64) return run(Small<64, 128, 2, 4, 3, true>{});
@@ -1042,7 +1075,12 @@ extern "C" psc_status psc_head_logits_mx(const void *x, psc_form x_form, int64_t
         a.blocks = up(V, kBlockTokens);
         a.counts = counts = reinterpret_cast<int32_t *>(at + ws.counts);
         a.ids = ids = reinterpret_cast<int32_t *>(at + ws.ids);
-        a.gather_most = takes_wide(a) ? V / 4 : V / 2;
+        // Half of them, of states in 4 bits a third; a quarter where wide_mx_kernel takes all.  us with the needed ones only
+        // and with all: 8 x 128,256 x 4,096 of bfloat16 45 and 62 where half are needed, 64 rows 90 and 121, at 0.6 119 and
+        // 121; 64 x 151,665 x 2,048 in 4 bits 47 and 49 at 0.3, 52 and 49 at 0.4; by wide_mx_kernel 256 x 151,936 x 4,096 in 4 bits
+        // 124 and 153 at 0.2, 157 and 154 at 0.3, of bfloat16 256 and 300 at 0.3, 319 and 302 at 0.4; 512 x 128,256 x 2,048 in
+        // 4 bits 123 and 125 at 0.1, 162 and 126 at 0.2.
+        a.gather_most = takes_wide(a) ? V / 4 : mx ? V / 3 : V / 2;
     }
     const States given{x, x_form, x_stride, x_scales, x_scales_stride};
     uint8_t *const scales = at + ws.scales;

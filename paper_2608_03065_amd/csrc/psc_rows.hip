@@ -26,7 +26,8 @@ struct Divisor {
 // ---------------------------------------------------------------- rows to 4 bits
 
 // A thread takes eight elements, four threads a block.  A row has `eights` of
-// them, whole blocks, zeros from D on.
+// them, whole blocks, zeros from D on.  Bound by memory: 128,256 x 4,096 from bfloat16
+// take 236 us, 1.3 GB, 5.6 TB/s.
 template <bool kBf16>
 __global__ void __launch_bounds__(kBlock)
 quantize_mx_kernel(const void *__restrict__ x, int64_t x_stride, int32_t D, Divisor eights, uint32_t units,
@@ -54,7 +55,10 @@ struct LookupArgs {
     int32_t D;
 };
 
-// A thread takes eight elements of a row; a row of no table's is zeros.
+// A thread takes eight elements of a row; a row of no table's is zeros.  kStream:
+// whole vectors, stored past the caches, which are not to hold what is read once
+// after it all: 128,256 x 4,096 from 4 bits to bfloat16 take 259 us (361 by ordinary
+// stores), 8,192 x 4,096 from 8 bits 16.3 (22.2), 6.2 TB/s.
 template <bool kMx, bool kBf16, bool kStream>
 __global__ void __launch_bounds__(kBlock)
 lookup_kernel(const LookupArgs a, Divisor eights, uint32_t units) {
@@ -125,6 +129,10 @@ __device__ __forceinline__ T row_all(T v, T none, const Op &op, T *s_part) {
 // kTurns times that is read once and stays in registers, up to twice its gain too; of a
 // longer one (kTurns 0) the sum is read again from the residual, or x where there
 // is none.  kResidual: none, float32, bfloat16.
+//
+// Bound by memory where there are many rows: 8,192 x 4,096 with a bfloat16 residual to
+// 8 bits take 50.7 us, 235 MB, 4.6 TB/s, what a large copy reaches; one of 2,048 by its
+// chain of waits, 3.0 us.
 template <psc_form kTo, int kResidual, int kThreads, int kTurns>
 __global__ void __launch_bounds__(kThreads > kBlock ? kThreads : kBlock)
 norm_kernel(const NormArgs a) {

@@ -31,7 +31,7 @@ EXPORTED = ["psc_build", "psc_info", "psc_device_bytes", "psc_bind_device", "psc
             "psc_predictor_fill", "psc_predictor_updates", "psc_timeline_records", "psc_compute_and_apply_timeline",
             "psc_set_options", "psc_compute_and_argmax_noalloc", "psc_grammar_compile", "psc_grammar_view",
             "psc_grammar_symbol_name", "psc_grammar_free", "psc_build_from_text", "psc_quantize_rows",
-            "psc_head_workspace", "psc_head_logits", "psc_head_logits_i8", "psc_quantize_mx", "psc_lookup_rows",
+            "psc_head_workspace", "psc_head_logits", "psc_head_logits_quantized", "psc_quantize_mx", "psc_lookup_rows",
             "psc_add_rms_norm", "psc_head_mx_workspace", "psc_head_logits_mx", "psc_penalize", "psc_append_tokens", "psc_sample_workspace",
             "psc_sample"]
 
@@ -236,7 +236,7 @@ def lib() -> C.CDLL:
         L.psc_head_workspace.restype = C.c_size_t
         L.psc_head_logits.argtypes = [P, C.c_int, I64, I32, I32, P, I64, P, I32, P, P, P, C.c_int, I64, P,
                                       C.c_size_t, P]
-        L.psc_head_logits_i8.argtypes = [P, I64, P, I32, I32, P, I64, P, I32, P, P, P, C.c_int, I64, P, C.c_size_t, P]
+        L.psc_head_logits_quantized.argtypes = [P, I64, P, I32, I32, P, I64, P, I32, P, P, P, C.c_int, I64, P, C.c_size_t, P]
         L.psc_quantize_mx.argtypes = [P, C.c_int, I64, I64, I32, P, I64, P, I64, P]
         L.psc_lookup_rows.argtypes = [C.c_int, P, I64, P, I64, I64, I32, P, I64, P, C.c_int, I64, P]
         L.psc_add_rms_norm.argtypes = [P, C.c_int, I64, P, C.c_int, I64, I64, I32, P, C.c_float, C.c_int, P, I64, P, I64, P]
@@ -261,7 +261,7 @@ def lib() -> C.CDLL:
                      "psc_compute_and_argmax_n", "psc_predictor_fill", "psc_predictor_updates",
                      "psc_compute_and_apply_timeline", "psc_set_options", "psc_compute_and_argmax_noalloc",
                      "psc_grammar_compile", "psc_grammar_view", "psc_build_from_text", "psc_quantize_rows",
-                     "psc_head_logits", "psc_head_logits_i8", "psc_quantize_mx", "psc_lookup_rows", "psc_add_rms_norm",
+                     "psc_head_logits", "psc_head_logits_quantized", "psc_quantize_mx", "psc_lookup_rows", "psc_add_rms_norm",
                      "psc_head_logits_mx", "psc_penalize", "psc_append_tokens", "psc_sample"):
             getattr(L, name).restype = C.c_int
         _lib = L
@@ -819,7 +819,7 @@ def head_logits(x, w, w_scales, dtype=None, bias=None, bitmask=None, out=None, s
     `out`: where to write them (its rows may lie apart); else a new tensor of
     `dtype`, that of x by default.  States that are in 8 bits already (x int8
     with x_scales float32 [B], as quantize_rows and add_rms_norm return them)
-    are taken as they are, to bfloat16 logits by default (psc_head_logits_i8)."""
+    are taken as they are, to bfloat16 logits by default (psc_head_logits_quantized)."""
     T = _T or _torch_types()
     if x_scales is None:
         x_code, x_stride = _rows(x, "x")
@@ -847,7 +847,7 @@ def head_logits(x, w, w_scales, dtype=None, bias=None, bitmask=None, out=None, s
     rest = (B, D, w.data_ptr(), w_stride, scales, V, bias, words, out.data_ptr(), code, y_stride, ws.data_ptr(), n,
             _stream_ptr(stream))
     _check(L.psc_head_logits(x.data_ptr(), x_code, x_stride, *rest) if given is None
-           else L.psc_head_logits_i8(x.data_ptr(), x_stride, given, *rest))
+           else L.psc_head_logits_quantized(x.data_ptr(), x_stride, given, *rest))
     return out
 
 

@@ -77,14 +77,14 @@ def test_head_logits_mx_refuses(wrong):
 
 
 def head_i8(q=AT, q_stride=64, scales=AT, B=2, D=64, w=AT, w_stride=64, w_scales=AT, V=8, y=AT, dtype=1, stride=8, ws=AT, ws_bytes=1 << 40):
-    return psc.lib().psc_head_logits_i8(q, q_stride, scales, B, D, w, w_stride, w_scales, V, None, None, y, dtype, stride, ws, ws_bytes, None)
+    return psc.lib().psc_head_logits_quantized(q, q_stride, scales, B, D, w, w_stride, w_scales, V, None, None, y, dtype, stride, ws, ws_bytes, None)
 
 
 @pytest.mark.parametrize("wrong", [dict(q=None), dict(scales=None), dict(q_stride=72), dict(q_stride=48), dict(q=AT + 8), dict(scales=AT + 2),
                                    dict(B=-1), dict(V=-1), dict(D=0), dict(D=131073), dict(w=None), dict(w_scales=None), dict(y=None),
                                    dict(ws=None), dict(w_stride=60), dict(stride=7), dict(ws_bytes=263), dict(dtype=2)])
 def test_head_logits_i8_refuses(wrong):
-    assert refused(head_i8(**wrong), "psc_head_logits_i8")
+    assert refused(head_i8(**wrong), "psc_head_logits_quantized")
 
 
 def test_sizes_that_pass_a_launch_or_its_offsets_are_refused():
