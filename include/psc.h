@@ -682,7 +682,7 @@ psc_status psc_add_rms_norm(const void *x, psc_dtype x_dtype, int64_t x_stride, 
  *             at a 4-byte address; the same goes for them.
  *  bias       float32 [V] or NULL.
  *  workspace  psc_head_mx_workspace(B, D, V, states) bytes, 16-byte aligned.
- * 1 <= D <= 131,072, V <= 2^26, ceil(B / 64) * ceil(V / 512) < 2^24.  B == 0 or V == 0 is
+ * 1 <= D <= 131,072, V <= 2^26, ceil(B / 64) * ceil(V / 512) < 2^23.  B == 0 or V == 0 is
  * a no-op.  Errors: PSC_E_INVALID_ARG, PSC_E_DEVICE.
  */
 size_t psc_head_mx_workspace(int32_t B, int32_t D, int32_t V, psc_form states);

@@ -5,10 +5,9 @@
 // 32 of them: a block, 16 bytes of codes, with the block's power of two.  For
 // bfloat16 states the same 16 bytes are converted to bfloat16 times their power,
 // which holds them exactly, and go through four matrix instructions of 32
-// elements each, of which a lane has 8.  Sums are float32: of 4-bit states what an
-// instruction adds up is exact, of bfloat16 products exact and the sum rounded.
-// (The same instruction takes states in 8-bit floating point, whose sums it cuts
-// off near 2^-13 of the largest product: no form of states here.)
+// elements each, of which a lane has 8.  Products are exact, sums float32.  (The
+// same instruction takes states in 8-bit floating point, whose sums it cuts off
+// near 2^-13 of the largest product: no form of states here.)
 //
 // A call launches prepare_mx_kernel (the states to what is multiplied, and under a
 // mask the list of tokens that any row allows) unless the states can be read
@@ -1022,7 +1021,8 @@ extern "C" psc_status psc_head_logits_mx(const void *x, psc_form x_form, int64_t
     if (D < 1 || D > kMostD) return refuse(what, "D outside [1, 131072]");
     if (V > kMostV) return refuse(what, "V > 2^26");
     if (B == 0 || V == 0) return PSC_OK;
-    if ((int64_t)up(B, 64) * up(V, 512) > kMostGrid) return refuse(what, "ceil(B / 64) * ceil(V / 512) >= 2^24");
+    // workgroups of 512 threads, where needed tokens are taken beside wide_mx_kernel
+    if ((int64_t)up(B, 64) * up(V, 512) > kMostGrid / 2) return refuse(what, "ceil(B / 64) * ceil(V / 512) >= 2^23");
     if (!x || !w || !w_scales || !workspace) return refuse(what, "null pointer");
     const int64_t blocks = up(D, kMxBlock);
     if (x_form == PSC_FORM_MX4) {

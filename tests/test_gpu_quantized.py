@@ -285,7 +285,8 @@ def state_values(x, states):
 HEADS = [(1, 64, 1), (1, 1, 33), (2, 17, 64), (3, 128, 65), (8, 200, 513), (15, 1024, 1000), (16, 130, 700), (17, 256, 513),
          (33, 96, 1537), (48, 640, 300), (64, 512, 2049), (65, 300, 777), (100, 1000, 4097), (128, 384, 515),
          (200, 129, 1025), (256, 256, 600), (257, 320, 1100), (300, 128, 5000), (520, 144, 257), (1, 8192, 513), (4, 5000, 100),
-         (60, 4096, 130), (300, 4096, 300), (3, 33, 40), (40, 2080, 90), (270, 1056, 33000), (600, 512, 20001)]
+         (60, 4096, 130), (300, 4096, 300), (3, 33, 40), (40, 2080, 90), (270, 1056, 33000), (600, 512, 20001),
+         (200, 520, 33000), (300, 33, 17000), (1025, 256, 6500), (140, 640, 40001)]
 FORMS = ["bf16", "mx4"]
 
 
@@ -461,6 +462,47 @@ def test_steps_in_a_graph_and_on_a_stream(how, B):
             assert torch.equal(tokens.cpu(), want[k])
         assert torch.equal(r.cpu(), residual)
         assert [t.tolist() for t in eager(side)[0]] == [t.tolist() for t in want]
+
+
+@pytest.mark.parametrize("states", FORMS)
+def test_two_streams_at_once(states):
+    """Calls whose tiles and parts go through workspaces, on two streams that overlap: as one after the other."""
+    calls = []
+    for B, D, V, shares in ((3, 4096, 1000, None), (40, 2048, 6000, (0.1,)), (150, 512, 33000, (0.02, 0.2)), (300, 768, 30000, None)):
+        x = torch.randn(B, D, generator=torch.Generator().manual_seed(B)).to(torch.bfloat16).to(DEV)
+        q, s, _ = weights(V, D, B)
+        kw = dict(states=states, dtype=torch.float32, bitmask=None if shares is None else mask(B, V, B, shares)[0])
+        calls.append((x, q, s, kw))
+    want = [psc.head_logits_mx(x, q, s, **kw) for x, q, s, kw in calls]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[psc.head_logits_mx(x, q, s, stream=stream, **kw) for stream in streams] for x, q, s, kw in calls * 5]
+    for stream in streams:
+        stream.synchronize()
+    assert all(torch.equal(t, w) for g, w in zip(got, want * 5) for t in g)
+
+
+def test_two_graphs_in_turn():
+    """Each graph's workspace is its own: replays in any order give what the eager calls gave."""
+    side, graphs = torch.cuda.Stream(), []
+    for B, D, V, states in ((2, 4096, 700, "bf16"), (70, 1024, 3000, "mx4")):
+        x = torch.randn(B, D, generator=torch.Generator().manual_seed(B)).to(torch.bfloat16).to(DEV)
+        q, s, _ = weights(V, D, B)
+        words, _ = mask(B, V, B, (0.1, 0.3))
+        run = lambda x=x, q=q, s=s, words=words, states=states: psc.head_logits_mx(x, q, s, states=states, bitmask=words)  # noqa: E731
+        want = run()
+        side.wait_stream(torch.cuda.current_stream())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            out = run()
+        graphs.append((graph, out, want, run))
+    for k in (0, 1, 1, 0, 0, 1):
+        graph, out, want, run = graphs[k]
+        out.fill_(0)
+        graph.replay()
+        assert torch.equal(run(), want)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
 
 
 def test_stream_argument():

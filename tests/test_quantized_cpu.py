@@ -91,11 +91,12 @@ def test_sizes_that_pass_a_launch_or_its_offsets_are_refused():
     V = (1 << 26) + 1
     assert psc.lib().psc_head_mx_workspace(2, 64, V, 1) == 0 and psc.lib().psc_head_mx_workspace(2, 64, 8, 0) == 0
     assert refused(head(V=V, stride=V), "psc_head_logits_mx") and b"2^26" in psc.lib().psc_last_error()
-    most = ((1 << 24) - 1) * 64
-    for B, V in ((most + 1, 8), (most // 2, 513), ((1 << 31) - 1, 1)):
-        assert refused(head(B=B, V=V, stride=V), "psc_head_logits_mx") and b"2^24" in psc.lib().psc_last_error()
-    # the last one that is taken gets as far as the workspace's check
-    assert refused(head(V=1 << 26, stride=1 << 26, ws_bytes=1), "psc_head_logits_mx") and b"workspace" in psc.lib().psc_last_error()
+    most = ((1 << 23) - 1) * 64
+    for B, V in ((most + 1, 8), (most // 2 + 64, 513), ((1 << 31) - 1, 1)):
+        assert refused(head(B=B, V=V, stride=V), "psc_head_logits_mx") and b"2^23" in psc.lib().psc_last_error()
+    # the last ones that are taken get as far as the workspace's check
+    for B, V in ((2, 1 << 26), (most, 512), (64 * 63, 1 << 26)):
+        assert refused(head(B=B, V=V, stride=V, ws_bytes=1), "psc_head_logits_mx") and b"workspace" in psc.lib().psc_last_error()
 
 
 def test_head_mx_workspace_holds_states():
