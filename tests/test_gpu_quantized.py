@@ -402,6 +402,32 @@ def test_head_logits_mx_twice_is_the_same(states):
             assert torch.equal(psc.head_logits_mx(x, q, s, states=states, dtype=torch.float32, **kw), first)
 
 
+@pytest.mark.parametrize("B,states,masked", [(2, "bf16", False), (40, "mx4", True), (200, "mx4", False), (140, "bf16", True)])
+def test_more_than_4_gib_of_weights(B, states, masked):
+    """Rows on both sides of byte 2^32 of the codes, by the projection and by their tokens."""
+    D, V = 16384, 530001
+    g = torch.Generator(DEV).manual_seed(B)
+    q = torch.randint(0, 256, (V, D // 2), generator=g, device=DEV, dtype=torch.uint8)
+    s = torch.randint(118, 130, (V, D // 32), generator=g, device=DEV, dtype=torch.uint8)
+    edge = 2 ** 32 // (D // 2)
+    at = torch.tensor([0, 1, 77, edge - 2, edge - 1, edge, edge + 1, V - 200, V - 2, V - 1], device=DEV)
+    w = values(host(q[at]), host(s[at]), D)
+    close(psc.lookup_rows(q, s, at.to(torch.int32)), w, 0)
+    x = torch.randn(B, D, generator=torch.Generator().manual_seed(B)).to(torch.bfloat16)
+    xv = state_values(x, states)
+    words = None
+    if masked:                                   # odd tokens and the last one
+        words = torch.full((B, (V + 31) // 32), 0x55555555 * 2 - 2 ** 32, dtype=torch.int32, device=DEV)
+        words[:, -1] |= 1 << (V - 1) % 32
+    got = psc.head_logits_mx(x.to(DEV), q, s, states=states, dtype=torch.float32, bitmask=words)
+    y = xv @ w.T
+    if masked:
+        even = host(at) % 2 == 0
+        even[-1] = False
+        y[:, even] = -np.inf
+    close(got[:, at], y, head_bound(xv, w, 0, states))
+
+
 # ---------------------------------------------------------------- together
 
 def step(x, residual, gain, table, out, words, how):
