@@ -576,7 +576,7 @@ psc_status psc_quantize_rows(const void *x, psc_dtype dtype, int64_t x_stride, i
  *             lies between D and w_stride does not matter.
  *  w_scales   float32 [V];  bias  float32 [V] or NULL.
  *  workspace  psc_head_workspace(B, D, V) bytes, 16-byte aligned.
- * 1 <= D <= 131,072 (up to there no sum can overflow), V <= 2^26, ceil(B / 64) *
+ * 1 <= D <= 131,072 (up to there no sum passes 32 bits), V <= 2^26, ceil(B / 64) *
  * ceil(V / 512) < 2^24.  B == 0 or V == 0 is a no-op.  Errors: PSC_E_INVALID_ARG,
  * PSC_E_DEVICE.
  */
@@ -596,8 +596,8 @@ typedef enum {
 
 /* psc_head_logits of states that are in 8 bits already: rows of q (as
  * psc_quantize_rows and psc_add_rms_norm write them, q_stride bytes apart) with
- * their scales.  Values of -128 count as they are; what lies between D and
- * q_stride does not matter.  The same workspace, refusals and errors. */
+ * their scales.  Values of -128 count as they are, at every D; what lies between D
+ * and q_stride does not matter.  The same workspace, refusals and errors. */
 psc_status psc_head_logits_quantized(const int8_t *q, int64_t q_stride, const float *scales, int32_t B, int32_t D,
                               const int8_t *w, int64_t w_stride, const float *w_scales, int32_t V,
                               const float *bias, const uint32_t *bitmask, void *logits, psc_dtype dtype,

@@ -141,7 +141,11 @@ prepare_kernel(const HeadArgs a, int32_t rows, const void *__restrict__ x, int64
     else needed_block(a, (int32_t)blockIdx.x - rows, counts, ids, shared);
 }
 
-// The same of states that are in 8 bits already: rows `first` .. are copied, zeros behind them.
+// |sum| <= 127 * 128 * D stays below 2^31 for every row but one of -128 alone, which is at 2^31 with weights of -128.
+constexpr int32_t kMostD = 131072;
+
+// The same of states that are in 8 bits already: rows `first` .. are copied, zeros behind them.  A row of kMostD times
+// -128 becomes one of -64 with twice its scale, the same numbers, whose sums fit 32 bits.
 __global__ void __launch_bounds__(kQuantBlock)
 copy_kernel(const HeadArgs a, int32_t first, int32_t rows, const int8_t *__restrict__ x, int64_t x_stride, const float *__restrict__ x_scales,
             int8_t *__restrict__ q, float *__restrict__ scales, int32_t *__restrict__ counts, int32_t *__restrict__ ids) {
@@ -153,6 +157,17 @@ copy_kernel(const HeadArgs a, int32_t first, int32_t rows, const int8_t *__restr
         return;
     }
     const int64_t r = (int64_t)first + blockIdx.x;
+    bool halves = false;
+    if (a.D == kMostD) {
+        uint32_t off = 0;
+        for (int32_t d = threadIdx.x * kChunk; d < kMostD; d += kQuantBlock * kChunk) {
+            uint32_t t[4];
+            __builtin_memcpy(t, x + r * x_stride + d, sizeof t);
+#pragma unroll
+            for (int k = 0; k < 4; k++) off |= t[k] ^ 0x80808080u;
+        }
+        halves = !__syncthreads_or(off != 0);
+    }
     for (int32_t d = threadIdx.x * kChunk; d < (int32_t)a.x_stride; d += kQuantBlock * kChunk) {
         uint32_t t[4] = {};
         if (d < a.D) __builtin_memcpy(t, x + r * x_stride + d, sizeof t);
@@ -160,10 +175,15 @@ copy_kernel(const HeadArgs a, int32_t first, int32_t rows, const int8_t *__restr
         for (int k = 0; k < 4; k++) {
             const int32_t left = a.D - d - 4 * k;
             if (left < 4) t[k] &= left > 0 ? ~(~0u << (8 * left)) : 0u;
+            if (halves) t[k] = 0xC0C0C0C0u;
         }
         __builtin_memcpy(q + r * a.x_stride + d, t, sizeof t);
     }
-    if (threadIdx.x == 0) scales[r] = x_scales[r];
+    if (threadIdx.x == 0) {
+        const float scale = x_scales[r], twice = 2 * scale;
+        // a scale whose double passes float32 makes every sum but 0 infinite as it is
+        scales[r] = halves && __builtin_isfinite(twice) ? twice : scale;
+    }
 }
 
 // ---------------------------------------------------------------- results
@@ -770,7 +790,6 @@ void launch_product(const HeadArgs &a, bool bf16, hipStream_t s) {
     else launch_wide<256, 3>(a, bf16, s);
 }
 
-constexpr int32_t kMostD = 131072;       // |sum| <= 127 * 128 * D stays below 2^31
 int32_t whole_steps(int32_t D) { return up(D, kStep) * kStep; }
 
 // The workspace: quantised states [B][whole_steps(D)], their scales, the needed

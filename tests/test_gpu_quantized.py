@@ -552,3 +552,41 @@ def test_empty_calls():
     assert psc.add_rms_norm(none, to="i8")[0].shape == (0, 200)
     assert psc.head_logits_mx(none, q, s).shape == (0, 90)
     assert psc.lookup_rows(q, s, torch.empty(0, dtype=torch.int32, device=DEV), D=200).shape == (0, 200)
+
+
+# ---------------------------------------------------------------- the ends of what the contract allows
+
+@pytest.mark.parametrize("B,V", [(3, 3), (24, 40), (50, 140), (100, 200), (140, 32600)])
+@pytest.mark.parametrize("share", [None, 0.05])
+def test_head_logits_of_quantized_states_at_the_end_of_32_bits(B, V, share):
+    """-128 in the states and the weights at the largest D: the sum is 2^31, the only one that passes 32 bits."""
+    D = 131072
+    x = torch.full((B, D), -128, dtype=torch.int8, device=DEV)
+    w = torch.full((V, D), -128, dtype=torch.int8, device=DEV)
+    w[V - 1], w[V // 2, 5] = 127, -127
+    x[1, D - 1], x[B - 1] = -127, 127
+    sums = np.full((B, V), 2.0 ** 31)
+    sums[:, V // 2] -= 128
+    sums[1] -= 128
+    sums[:, V - 1] = -127.0 * 128 * D
+    sums[1, V - 1] += 127
+    sums[B - 1] = -127.0 * 128 * D
+    sums[B - 1, V // 2] += 127
+    sums[B - 1, V - 1] = 127.0 ** 2 * D
+    g = torch.Generator().manual_seed(V)
+    xs, ws = torch.rand(B, generator=g) + 0.5, torch.rand(V, generator=g) / D
+    y = sums * xs.double().numpy()[:, None] * ws.double().numpy()
+    words, keep = (None, np.True_) if share is None else mask(B, V, V, (share,))
+    got = psc.head_logits(x, w, ws.to(DEV), x_scales=xs.to(DEV), dtype=torch.float32, bitmask=words)
+    close(got, np.where(keep, y, -np.inf), 8 * U * np.abs(y))
+
+
+def test_head_logits_of_quantized_states_of_the_largest_scales():
+    """Rows of -128 alone whose scale's double passes float32, or is none: a sum of 0 stays 0, the others keep their sign."""
+    D = 131072
+    x = torch.full((3, D), -128, dtype=torch.int8, device=DEV)
+    w = torch.full((3, D), -128, dtype=torch.int8, device=DEV)
+    w[1], w[2, ::2], w[2, 1::2] = 127, 1, -1
+    xs = torch.tensor([1.5 * 2.0 ** 127, math.inf, math.nan], device=DEV)
+    got = psc.head_logits(x, w, torch.ones(3, device=DEV), x_scales=xs, dtype=torch.float32)
+    close(got, np.array([[np.inf, -np.inf, 0], [np.inf, -np.inf, np.nan], [np.nan] * 3]), 0)
