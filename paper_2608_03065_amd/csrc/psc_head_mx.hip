@@ -203,6 +203,14 @@ __device__ __forceinline__ void load_word_to_lds(u32x4 from, uint32_t offset, ui
                  : "memory", "m0");
 }
 
+// A row's codes past D in its last block, in LDS, to zeros: its scale could make them infinite in bfloat16, and these
+// no zeros of the states' take out.  `line` holds the row's last step.
+__device__ __forceinline__ void clear_behind(const MxArgs &a, uint8_t *line, int row) {
+    const int block = a.w_blocks - 1 - (a.steps - 1) * kStepScales, n = a.D % kMxBlock;
+    uint32_t *const at = reinterpret_cast<uint32_t *>(line + ((block ^ (row & 7)) * kChunk));
+    for (int e = n / kVec; e < kMxBlock / kVec; e++) at[e] &= ~(~0u << (4 * max(n - e * kVec, 0)));
+}
+
 // One workgroup computes kM states by kN tokens over a part of D.  Steps of 256
 // elements of all its rows go straight from memory into one of kStages buffers
 // in LDS, kStages - 1 steps ahead: a line of codes of every token, and of every
@@ -211,7 +219,7 @@ __device__ __forceinline__ void load_word_to_lds(u32x4 from, uint32_t offset, ui
 // row's 16-byte chunk c lies at place c ^ (row & 7) of its line, and of a state in
 // bfloat16 at c ^ (row & 15), so that the 16 rows that a matrix instruction reads
 // at one chunk fall into different banks; since a load puts lane l's chunk at
-// place l, the lane fetches the chunk that belongs there.  Codes past a row's D
+// place l, the lane fetches the chunk that belongs there.  Blocks past a row's D
 // elements are multiplied by the states' zeros, and by a scale of 1.
 template <int kM, int kN, int kWavesM, int kWavesN, int kStages, bool kMx, bool kBf16, bool kPlain>
 __device__ __forceinline__ void small_mx_body(const MxArgs &a, bool gather_only) {
@@ -388,14 +396,21 @@ __device__ __forceinline__ void small_mx_body(const MxArgs &a, bool gather_only)
             }
         }
     };
+    const auto settle = [&](int32_t step) {
+        if (kMx || a.D % kMxBlock == 0 || step + 1 != a.steps) return;
+        for (int row = threadIdx.x; row < kN; row += kWaves * kWave) clear_behind(a, lds + step % kStages * kStage + row * kStep, row);
+        wait_and_meet<63>();
+    };
     // of the loads after the step's own: kStages - 2 steps of them, of which scales come with the even ones
     for (int32_t step = first; step < steps; step += 2) {
         wait_and_meet<(kStages - 2) * kLoads + (kStages == 4 ? kLoadsS : 0)>();   // the step has landed, and its predecessor's buffer is free
         fetch(step + kStages - 1, kStages == 3);
+        settle(step);
         turn(step, true);
         if (step + 1 == steps) break;
         wait_and_meet<(kStages - 2) * kLoads + kLoadsS>();
         fetch(step + kStages, kStages == 4);
+        settle(step + 1);
         turn(step + 1, false);
     }
     if (plan.splits > 1) {
@@ -701,6 +716,14 @@ __device__ __forceinline__ void wide_mx_body(const MxArgs &a) {
         fetched_x();
     }
     wait_and_meet<0>();
+    const bool ragged = !kMx && a.D % kMxBlock != 0;
+    const auto settle = [&](int buffer) {
+        if ((int)threadIdx.x < kN) clear_behind(a, lds_w + (buffer * kN + (int)threadIdx.x) * kStep, threadIdx.x);
+    };
+    if (ragged && a.steps == 1) {
+        settle(0);
+        wait_and_meet<0>();
+    }
     look(0);
     look_s();
     look_inside();
@@ -733,6 +756,8 @@ __device__ __forceinline__ void wide_mx_body(const MxArgs &a) {
             if (line == 0 && stored) wait_and_meet<(kStores < 63 ? kStores : 63)>();
             else if (!kMx && sub_r == 1) wait_and_meet<kLoadsW>();
             else wait_and_meet<0>();
+            // The next line of codes, which is first read after the next barrier.
+            if (ragged && sub_r == 2 && (step_r + 1 == a.steps ? 1 : step_r + 2) == a.steps) settle(at_w ^ 1);
             __builtin_amdgcn_sched_barrier(0);
             const bool codes_too = kMx || sub_r == 0;
             const uint32_t base_x = base(a.x_stride), base_w = base(a.w_stride);

@@ -590,3 +590,26 @@ def test_head_logits_of_quantized_states_of_the_largest_scales():
     xs = torch.tensor([1.5 * 2.0 ** 127, math.inf, math.nan], device=DEV)
     got = psc.head_logits(x, w, torch.ones(3, device=DEV), x_scales=xs, dtype=torch.float32)
     close(got, np.array([[np.inf, -np.inf, 0], [np.inf, -np.inf, np.nan], [np.nan] * 3]), 0)
+
+
+@pytest.mark.parametrize("B,D,V", [(1, 33, 40), (3, 7, 5), (20, 1000, 300), (50, 300, 130), (100, 2049, 200), (200, 129, 33000), (200, 500, 70000),
+                                   (300, 95, 50000), (300, 300, 70000)])
+@pytest.mark.parametrize("share", [None, 0.02])
+@pytest.mark.parametrize("states", FORMS)
+def test_head_logits_mx_of_the_largest_scales(B, D, V, share, states):
+    """Scales up to 254, of which bfloat16 holds 4 at most times 2^125, 3 times 2^126 and 1.5 times 2^127: weights up to there
+    are taken as they are, and any code behind the row's D does not matter."""
+    q, s, _ = weights(V, D, D, low=240, high=255)
+    blocks = s.shape[1]
+    whole = torch.as_strided(q, (V, blocks * 16), q.stride())
+    codes = torch.stack((whole & 15, whole >> 4), -1).view(V, -1)
+    inside = torch.arange(blocks * 32, device=DEV) < D
+    most = torch.where(s == 254, 3, torch.where(s == 253, 5, 7)).repeat_interleave(32, 1)      # a code's place in the list
+    codes = torch.where(inside, codes // 8 * 8 + torch.minimum(codes % 8, most), codes)
+    whole.copy_(codes[:, ::2] + 16 * codes[:, 1::2])
+    w = values(host(q), host(s), D)
+    x = (torch.randn(B, D, generator=torch.Generator().manual_seed(B)) * 2.0 ** -20).to(torch.bfloat16)
+    xv = state_values(x, states)
+    words, keep = (None, np.True_) if share is None else mask(B, V, V, (share,))
+    got = psc.head_logits_mx(x.to(DEV), q, s, states=states, dtype=torch.float32, bitmask=words)
+    close(got, np.where(keep, xv @ w.T, -np.inf), head_bound(xv, w, 0, states))
