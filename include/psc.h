@@ -670,7 +670,8 @@ psc_status psc_add_rms_norm(const void *x, psc_dtype x_dtype, int64_t x_stride, 
  * psc_quantize_mx (PSC_FORM_MX4); -inf where `bitmask` forbids v.  Products are exact,
  * sums and the bias float32, the result is rounded once to `dtype`; the same
  * call gives the same bits.  A weight's row with a scale of 255 gives NaN; numbers
- * below 2^-126 may count as 0.
+ * below 2^-126 may count as 0; for states in bfloat16 weights of 2^128 and more,
+ * which scales of 253 and 254 can make, are infinite, as psc_lookup_rows has them.
  *  x          [B] rows of D: x_form PSC_FORM_F32 or PSC_FORM_BF16, x_stride elements
  *             apart (x_scales is not used); or PSC_FORM_MX4, for `states` of that form,
  *             codes x_stride bytes apart (a multiple of 16, at a 16-byte address,

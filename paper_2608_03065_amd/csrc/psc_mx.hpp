@@ -86,7 +86,8 @@ __device__ __forceinline__ uint32_t to_mx4(const float (&v)[kVec], uint32_t &sca
 // instructions take a power of two by (0 stands for 2^-127, an infinity for NaN).
 __device__ __forceinline__ float mx_power(uint32_t scale) { return __builtin_bit_cast(float, scale << 23); }
 
-// Eight codes as pairs of bfloat16, scaled: no rounding from 2^-133 on, the smallest bfloat16.
+// Eight codes as pairs of bfloat16, scaled: no rounding from 2^-133 on, the smallest bfloat16; from 2^128 on infinite (4 and 6
+// with a scale of 253, 2 and more with one of 254).
 __device__ __forceinline__ void from_mx4(uint32_t codes, float power, uint32_t (&out)[4]) {
     out[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, power, 0));
     out[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, power, 1));

@@ -613,3 +613,27 @@ def test_head_logits_mx_of_the_largest_scales(B, D, V, share, states):
     words, keep = (None, np.True_) if share is None else mask(B, V, V, (share,))
     got = psc.head_logits_mx(x.to(DEV), q, s, states=states, dtype=torch.float32, bitmask=words)
     close(got, np.where(keep, xv @ w.T, -np.inf), head_bound(xv, w, 0, states))
+
+
+@pytest.mark.parametrize("B", [1, 24, 50, 200])
+def test_head_logits_mx_of_weights_past_bfloat16(B):
+    """Of 2^128 and more: infinite where the states are bfloat16, as lookup_rows has them; as they are where both are in 4 bits."""
+    D, V = 64, 33000
+    q, s, w = weights(V, D, 2, low=252, high=255)
+    x = (torch.randn(B, D, generator=torch.Generator().manual_seed(B)) * 2.0 ** -20).to(torch.bfloat16)
+    x[0, 1::2] = 0
+    xv = state_values(x, "mx4")
+    got = psc.head_logits_mx(x.to(DEV), q, s, states="mx4", dtype=torch.float32)
+    close(got, xv @ w.T, head_bound(xv, w, 0, "mx4"))
+    with np.errstate(over="ignore"):
+        w = w.astype(np.float32).astype(np.float64)
+    xv, large = state_values(x, "bf16"), np.isinf(w)
+    rest = np.where(large, 0, w)
+    up = (np.maximum(xv, 0) @ np.maximum(np.where(large, np.sign(w), 0), 0).T + np.maximum(-xv, 0) @ np.maximum(-np.where(large, np.sign(w), 0), 0).T) > 0
+    down = (np.maximum(-xv, 0) @ np.maximum(np.where(large, np.sign(w), 0), 0).T + np.maximum(xv, 0) @ np.maximum(-np.where(large, np.sign(w), 0), 0).T) > 0
+    none = ((xv == 0).astype(float) @ large.T.astype(float)) > 0
+    y = np.where(up, np.inf, np.where(down, -np.inf, xv @ rest.T))
+    y[none | (up & down)] = np.nan
+    assert np.isnan(y).any() and np.isinf(y).any() and np.isfinite(y).any()
+    got = psc.head_logits_mx(x.to(DEV), q, s, dtype=torch.float32)
+    close(got, y, head_bound(xv, rest, 0, "bf16"))
