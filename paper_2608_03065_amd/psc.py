@@ -951,14 +951,16 @@ def add_rms_norm(x, gain=None, residual=None, eps=1e-6, to=None, stream=None):
 
 
 def head_logits_mx(x, w, w_scales, states="bf16", x_scales=None, dtype=None, bias=None, bitmask=None, out=None,
-                   stream=None):
+                   stream=None, D=None):
     """Logits [B, V] of hidden states x [B, D] by 4-bit weights w [V, ceil(D / 2)]
     with w_scales [V, ceil(D / 32)] (quantize_mx), forbidden tokens -inf
     (psc_head_logits_mx).  `states`: what the products take them in, "bf16", or
     "mx4", quantised as by quantize_mx.  States that are in 4 bits already (x
     uint8 with x_scales, as quantize_mx and add_rms_norm return them) are taken
-    as they are.  `out`: where to write the logits; else a new tensor of
-    `dtype`, by default that of x, of states in 4 bits bfloat16."""
+    as they are; D is that of their rows where it is odd (else their last code
+    counts too, a zero as the quantisers write it).  `out`: where to write the
+    logits; else a new tensor of `dtype`, by default that of x, of states in
+    4 bits bfloat16."""
     T = _T or _torch_types()
     form = _STATES.get(states)
     if form is None:
@@ -966,12 +968,17 @@ def head_logits_mx(x, w, w_scales, states="bf16", x_scales=None, dtype=None, bia
     x_at, x_s_stride = None, 0
     if x_scales is None:
         x_code, x_stride = _rows(x, "x")
+        if D is not None and D != x.shape[1]:
+            _require(False, f"x of {D} columns")
         (B, D), dev, default = x.shape, x.get_device(), x.dtype
         cols, blocks = (D + 1) // 2, (D + MX_BLOCK - 1) // MX_BLOCK
     else:
         _matrix(x, "x")
         cols, default, form, x_code = x.shape[1], T["bf16"], FORM_MX4, FORM_MX4
-        D = cols * 2          # an odd row's last code is zero
+        if D is None:
+            D = cols * 2
+        elif (D + 1) // 2 != cols:
+            _require(False, f"x of {(D + 1) // 2} columns for D = {D}")
         blocks = (D + MX_BLOCK - 1) // MX_BLOCK
         x_stride, B, dev = _packed(x, "x", "u8", cols, 16)
         x_s_stride = _packed(x_scales, "x_scales", "u8", blocks, 1, dev, B)[0]

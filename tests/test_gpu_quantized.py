@@ -637,3 +637,15 @@ def test_head_logits_mx_of_weights_past_bfloat16(B):
     assert np.isnan(y).any() and np.isinf(y).any() and np.isfinite(y).any()
     got = psc.head_logits_mx(x.to(DEV), q, s, dtype=torch.float32)
     close(got, y, head_bound(xv, rest, 0, "bf16"))
+
+
+@pytest.mark.parametrize("B,D,V", [(1, 1, 5), (5, 95, 300), (33, 2047, 70), (300, 319, 700)])
+def test_head_logits_mx_of_quantized_states_of_odd_rows(B, D, V):
+    """What lies behind an odd row's last code, in the same byte, does not matter where D is given."""
+    x = torch.randn(B, D, generator=torch.Generator().manual_seed(B)).to(torch.bfloat16).to(DEV)
+    q, s, _ = weights(V, D, 3)
+    q[:, -1] |= 0x70
+    xq, xs = psc.quantize_mx(x)
+    want = psc.head_logits_mx(x, q, s, states="mx4", dtype=torch.float32)
+    xq[:, -1] |= 0x70
+    assert torch.equal(psc.head_logits_mx(xq, q, s, x_scales=xs, D=D, dtype=torch.float32), want)

@@ -123,3 +123,13 @@ def test_the_binding_refuses_tensors_that_the_library_cannot_check():
                  lambda: psc.head_logits_mx(q, q, s, x_scales=s), lambda: psc.head_logits(q, q, s, x_scales=s)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_the_binding_refuses_a_d_that_is_not_the_states():
+    q, s = torch.zeros(8, 32, dtype=torch.uint8), torch.zeros(8, 4, dtype=torch.uint8)
+    for D in (0, 1, 62, 65, 128, -1):
+        with pytest.raises(ValueError, match="x of"):
+            psc.head_logits_mx(q, q, s, x_scales=s, D=D)
+    for D in (63, 64):                  # taken: what is refused is that they are host tensors
+        with pytest.raises(ValueError, match="device"):
+            psc.head_logits_mx(q, q, s, x_scales=s, D=D)
