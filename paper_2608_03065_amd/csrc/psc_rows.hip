@@ -211,10 +211,14 @@ norm_kernel(const NormArgs a) {
     }, true);
     sum = row_all<kThreads>(sum, 0.0f, kAdd, s_sum);
     // Squares past float32's range: the same of the numbers times 2^-80, or 2^80
-    // where eps is too small to hide it.
-    float by = 1, eps = a.eps;
+    // where eps is too small to hide it.  An element much smaller than the row's
+    // largest would lose bits to 2^-80: it goes with the quotient, all of it but the
+    // quarter that keeps that from the subnormal numbers.
+    float before = 1, after = 1, eps = a.eps;
     if (!(sum < __builtin_huge_valf()) || (sum < 0x1p-40f && eps < 0x1p-80f)) {
-        by = sum < 1 ? 0x1p80f : 0x1p-80f;
+        const float by = sum < 1 ? 0x1p80f : 0x1p-80f;
+        before = sum < 1 ? by : 0x1p-2f;
+        after = sum < 1 ? 1.0f : 0x1p-78f;
         eps = eps * by * by;
         sum = 0;
         each([&](int64_t, const float (&v)[kVec], const float (&)[kVec]) {
@@ -223,10 +227,10 @@ norm_kernel(const NormArgs a) {
         }, false);
         sum = row_all<kThreads>(sum, 0.0f, kAdd, s_again);
     }
-    const float inverse = 1.0f / __builtin_sqrtf(sum / (float)a.D + eps);
+    const float inverse = 1.0f / __builtin_sqrtf(sum / (float)a.D + eps) * after;
     const auto norm = [&](const float (&v)[kVec], const float (&g)[kVec], float (&y)[kVec]) {
 #pragma unroll
-        for (int k = 0; k < kVec; k++) y[k] = v[k] * by * inverse * g[k];
+        for (int k = 0; k < kVec; k++) y[k] = v[k] * before * inverse * g[k];
     };
     if constexpr (kTo == PSC_FORM_F32 || kTo == PSC_FORM_BF16) {
         constexpr bool kBf16 = kTo == PSC_FORM_BF16;

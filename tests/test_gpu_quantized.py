@@ -649,3 +649,14 @@ def test_head_logits_mx_of_quantized_states_of_odd_rows(B, D, V):
     want = psc.head_logits_mx(x, q, s, states="mx4", dtype=torch.float32)
     xq[:, -1] |= 0x70
     assert torch.equal(psc.head_logits_mx(xq, q, s, x_scales=xs, D=D, dtype=torch.float32), want)
+
+
+@pytest.mark.parametrize("D", [64, 3000, 20000, 50000])
+@pytest.mark.parametrize("large,small", [(2.0 ** 65, 2.0 ** -57), (2.0 ** 100, 2.0 ** -24), (2.0 ** 127, 1.0), (2.0 ** -70, 2.0 ** -140)])
+def test_add_rms_norm_of_small_elements_beside_large_ones(D, large, small):
+    """Squares past float32's range on either side do not cost a small element its bits.  Bound as where squares pass it."""
+    x = torch.randn(3, D, generator=torch.Generator().manual_seed(D)).mul_(small)
+    x[:, D // 2] = large
+    _, y = normed(x, None, None, 0.0)
+    got = psc.add_rms_norm(x.to(DEV), eps=0)
+    close(got, y, (norm_bound(D) + 4 * U) * np.abs(y) + 2.0 ** -148)
