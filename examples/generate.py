@@ -45,12 +45,13 @@ class Generator:
         self.clf, self.k = clf, k
         self.states = psc.DecodeStates(clf, B, 4096, dev)
         self.tied = weights == "mx4"
-        self.embedding = torch.randn(clf.V, D, generator=self.g, device=dev)
+        embedding = torch.randn(clf.V, D, generator=self.g, device=dev)
         if self.tied:
             # once: the table in 4 bits, a power of two per 32 elements
-            self.weights, self.scales = psc.quantize_mx(self.embedding / D ** 0.5)
+            self.weights, self.scales = psc.quantize_mx(embedding / D ** 0.5)
             self.gain, self.last = torch.ones(D, device=dev), torch.zeros(B, D, dtype=torch.bfloat16, device=dev)
         else:
+            self.embedding = embedding
             # once: the output projection's weights in 8 bits, a scale per token
             self.weights, self.scales = psc.quantize_rows(torch.randn(clf.V, D, generator=self.g, device=dev) / D ** 0.5)
         self.hidden = torch.randn(B, D, generator=self.g, device=dev)

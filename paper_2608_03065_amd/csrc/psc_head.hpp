@@ -56,7 +56,7 @@ struct Plan {
     int32_t columns, tiles, splits;
 };
 
-// What is read is the wavefront's; `total` as needed_total gives it.
+// What is read is the wavefront's; `total` is the last lane's needed_upto.
 template <int kM, int kN>
 __device__ __forceinline__ Plan plan_of(const HeadBase &a, int32_t total) {
     Plan p{false, a.V, (a.V + kN - 1) / kN, a.splits};
@@ -177,6 +177,7 @@ __device__ __forceinline__ u32x4 rows_from(const void *p, int64_t bytes) {
     const uintptr_t at = reinterpret_cast<uintptr_t>(p);
     return u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, (uint32_t)min(max(bytes, (int64_t)0), (int64_t)kMostBytes), 0x00020000u};
 }
+
 // ---------------------------------------------------------------- host side
 
 constexpr int32_t kComputeUnits = 256;

@@ -197,12 +197,6 @@ __device__ __forceinline__ int64_t scale_bytes(const MxArgs &a, int32_t row) {
     return (int64_t)(a.V - row - 1) * a.w_scales_stride + (a.w_blocks + 3) / 4 * 4;
 }
 
-// 4 bytes per lane from the resource straight to LDS, as load_to_lds does with 16.
-__device__ __forceinline__ void load_word_to_lds(u32x4 from, uint32_t offset, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(offset), "s"(from)
-                 : "memory", "m0");
-}
-
 // A row's codes past D in its last block, in LDS, to zeros: its scale could make them infinite in bfloat16, and these
 // no zeros of the states' take out.  `line` holds the row's last step.
 __device__ __forceinline__ void clear_behind(const MxArgs &a, uint8_t *line, int row) {

@@ -16,9 +16,6 @@ constexpr int kMxBlock = 32;       // elements of a scale
 constexpr int kMxNaN = 255;        // the scale of a block with an infinity or a NaN
 constexpr int kVec = 8;            // elements that a thread takes at once
 
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
 // Elements d .. d + 7 of a row of D, zeros from D on.
 template <bool kBf16>
 __device__ __forceinline__ void load_eight(const void *row, int64_t d, int64_t D, float (&v)[kVec]) {

@@ -1,5 +1,6 @@
 // What the device files of the operators around a step's logits share
-// (psc_head.hip, psc_penalize.hip, psc_sample.hip).  Not part of the public ABI.
+// (psc_head.hip, psc_head_mx.hip, psc_rows.hip, psc_penalize.hip, psc_sample.hip).
+// Not part of the public ABI.
 #pragma once
 
 #include <hip/hip_runtime.h>
