@@ -660,3 +660,15 @@ def test_add_rms_norm_of_small_elements_beside_large_ones(D, large, small):
     _, y = normed(x, None, None, 0.0)
     got = psc.add_rms_norm(x.to(DEV), eps=0)
     close(got, y, (norm_bound(D) + 4 * U) * np.abs(y) + 2.0 ** -148)
+
+
+@pytest.mark.parametrize("B,D,V", [(1, 256, 70), (24, 97, 300), (50, 300, 130), (200, 160, 33000)])
+@pytest.mark.parametrize("states", FORMS)
+def test_head_logits_mx_of_the_smallest_scales(B, D, V, states):
+    """Scales from 0 on, of states near float32's end; a weight below 2^-126 may count as 0."""
+    q, s, w = weights(V, D, D, low=0, high=24)
+    x = (torch.randn(B, D, generator=torch.Generator().manual_seed(B)) * 2.0 ** 123).to(torch.bfloat16)
+    xv = state_values(x, states)
+    got = psc.head_logits_mx(x.to(DEV), q, s, states=states, dtype=torch.float32)
+    small = np.abs(xv) @ np.where(np.abs(w) < 2.0 ** -126, np.abs(w), 0).T
+    close(got, xv @ w.T, head_bound(xv, w, 0, states) + small)
