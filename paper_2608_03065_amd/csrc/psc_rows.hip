@@ -210,12 +210,12 @@ norm_kernel(const NormArgs a) {
         for (int k = 0; k < kVec; k++) sum = __builtin_fmaf(v[k], v[k], sum);
     }, true);
     sum = row_all<kThreads>(sum, 0.0f, kAdd, s_sum);
-    // Squares past float32's range: the same of the numbers times 2^-80, or 2^80
-    // where eps is too small to hide it.  An element much smaller than the row's
-    // largest would lose bits to 2^-80: it goes with the quotient, all of it but the
-    // quarter that keeps that from the subnormal numbers.
+    // Squares, or their mean with eps, past float32's range: the same of the numbers
+    // times 2^-80, or 2^80 where eps is too small to hide it.  An element much smaller
+    // than the row's largest would lose bits to 2^-80: it goes with the quotient, all
+    // of it but the quarter that keeps that from the subnormal numbers.
     float before = 1, after = 1, eps = a.eps;
-    if (!(sum < __builtin_huge_valf()) || (sum < 0x1p-40f && eps < 0x1p-80f)) {
+    if (!(sum / (float)a.D + eps < __builtin_huge_valf()) || (sum < 0x1p-40f && eps < 0x1p-80f)) {
         const float by = sum < 1 ? 0x1p80f : 0x1p-80f;
         before = sum < 1 ? by : 0x1p-2f;
         after = sum < 1 ? 1.0f : 0x1p-78f;

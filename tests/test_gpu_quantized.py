@@ -672,3 +672,13 @@ def test_head_logits_mx_of_the_smallest_scales(B, D, V, states):
     got = psc.head_logits_mx(x.to(DEV), q, s, states=states, dtype=torch.float32)
     small = np.abs(xv) @ np.where(np.abs(w) < 2.0 ** -126, np.abs(w), 0).T
     close(got, xv @ w.T, head_bound(xv, w, 0, states) + small)
+
+
+@pytest.mark.parametrize("D", [64, 3000, 20000, 50000])
+@pytest.mark.parametrize("to", ["f32", "i8", "mx4"])
+def test_add_rms_norm_of_an_eps_whose_sum_passes_float32(D, to):
+    """Neither the mean nor eps does.  Bound as where squares pass it."""
+    x = torch.randn(3, D, generator=torch.Generator().manual_seed(D)).mul_(1.5e19 / D ** 0.5)
+    eps = float(np.finfo(np.float32).max)
+    _, y = normed(x, None, None, eps)
+    check_form(psc.add_rms_norm(x.to(DEV), eps=eps, to=TYPES.get(to, to)), y, to, norm_bound(D) + 4 * U)
