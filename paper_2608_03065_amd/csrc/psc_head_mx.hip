@@ -22,12 +22,13 @@
 // Few rows are bound by the weights' bytes, each read once: 1 x 128,256 x 4,096
 // takes 50 us, 5.6 TB/s, where a large copy reaches 4.7; 64 x 128,256 x 4,096 66 us of
 // states in 4 bits, 4.5 TB/s, but 118 of bfloat16, whose lines are three times the
-// weights' bytes on their way from L2 to LDS.  Many rows: 2,048 x 128,256 x 4,096
-// takes 587 us in 4 bits, 3.7 P operations a second (the library's product of that
-// size without scales' variety, a mask or a bias 820), 256 x 151,936 x 4,096 of
-// bfloat16 271.  Their matrix instructions alone would take 228 and 160; the rest is
-// about equally the waits for what is read from LDS, for the lines from L2, and
-// the stores of the logits, which all compute units write at once.
+// weights' bytes on their way from L2 to LDS.  Many rows, by box and by what ran
+// before: 2,048 x 128,256 x 4,096 takes 577 to 648 us in 4 bits, 3.3 to 3.7 P
+// operations a second (the library's product of that size without scales' variety, a
+// mask or a bias 820), 256 x 151,936 x 4,096 of bfloat16 271 to 307.  Their matrix
+// instructions alone would take 228 and 160; the rest is about equally the waits for
+// what is read from LDS, for the lines from L2, and the stores of the logits, which
+// all compute units write at once.
 #include <type_traits>
 
 #include "psc_head.hpp"
